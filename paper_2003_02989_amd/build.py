@@ -11,7 +11,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtq.so")
-SOURCES = ["kernels.hip", "program.cpp", "tq_abi.cpp", "jit.cpp"]
+SOURCES = ["kernels.hip", "program.cpp", "tq_abi.cpp", "jit.cpp",
+           "seq_abi.cpp", "seq_embed.hip", "seq_scan.hip", "seq_norm.hip", "seq_xent.hip"]
 # device code the run-time specialised kernels are compiled with, in order
 JIT_HEADERS = ["tq_internal.h", "kernel_args.h", "device_ops.h"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

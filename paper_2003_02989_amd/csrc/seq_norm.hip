@@ -1,0 +1,375 @@
+// seq_norm.hip -- layer norm of rows and its gradients.
+//
+// Bound by memory: the forward pass reads x and writes y, the backward pass
+// reads x and dy and writes dx.  A row stays in the registers of the lanes that
+// share it, so the mean, the variance about it and the output take one read.
+// The backward pass walks many rows per wavefront and keeps the sums for
+// dweight and dbias in registers over all of them; what is left is one row of
+// partial sums per workgroup, added up by a second small kernel.
+#include <algorithm>
+#include <type_traits>
+
+#include "seq.h"
+#include "seq_device.h"
+
+namespace tq {
+namespace {
+
+// A row is shared by L lanes (L <= 64: several rows per wavefront; else a whole
+// workgroup of L threads), each holding C chunks of 16 bytes, L chunks apart.
+template <int L> constexpr int kThreadsOf = L > 64 ? L : 256;
+
+// Sum over the L lanes of a row.  With L > 64 all threads of the workgroup take
+// part, through `red`, which alternates between two halves by `turn`, so that
+// one barrier per sum is enough.
+template <int L> __device__ __forceinline__ float row_sum(float v, float (*red)[16], int &turn)
+{
+    if constexpr (L <= 64) return group_sum<L>(v);
+    else {
+        constexpr int W = L / 64;
+        v = group_sum<64>(v);
+        if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = v;
+        __syncthreads();
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; w++) s += red[turn][w];
+        turn ^= 1;
+        return s;
+    }
+}
+
+template <class T, int L, int C> __global__ __launch_bounds__(kThreadsOf<L>) void k_norm(NormArgs a)
+{
+    constexpr int VE = kVec<T>, R = kThreadsOf<L> / L;
+    __shared__ float red[2][16];
+    int turn = 0;
+    const int lane = threadIdx.x % L;
+    const int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L;
+    const bool in = row < a.N;
+    const T *x = (const T *)a.x + (in ? row : 0) * a.ld_x;
+    float f[C][VE];
+    int n[C];
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; c++) {
+        const int64_t at = (int64_t)(c * L + lane) * VE;
+        n[c] = in ? (int)max((int64_t)0, min((int64_t)VE, a.D - at)) : 0;
+        load_part<VE>(x + (n[c] ? at : 0), n[c], f[c]);
+#pragma unroll
+        for (int j = 0; j < VE; j++) s += f[c][j];
+    }
+    const float mean = row_sum<L>(s, red, turn) / (float)a.D;
+    float q = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; c++)
+#pragma unroll
+        for (int j = 0; j < VE; j++) {
+            f[c][j] -= mean;
+            if (j < n[c]) q = fmaf(f[c][j], f[c][j], q);
+        }
+    const float rstd = 1.f / sqrtf(row_sum<L>(q, red, turn) / (float)a.D + a.eps);
+    if (!in) return;
+    if (a.mean && lane == 0) {
+        a.mean[row] = mean;
+        a.rstd[row] = rstd;
+    }
+    T *y = (T *)a.y + row * a.ld_y;
+#pragma unroll
+    for (int c = 0; c < C; c++) {
+        if (!n[c]) continue;
+        const int64_t at = (int64_t)(c * L + lane) * VE;
+        float w[VE], b[VE];
+        load_part<VE>((const T *)a.weight + at, n[c], w);
+        if (a.bias) load_part<VE>((const T *)a.bias + at, n[c], b);
+        else
+#pragma unroll
+            for (int j = 0; j < VE; j++) b[j] = 0.f;
+#pragma unroll
+        for (int j = 0; j < VE; j++) f[c][j] = fmaf(f[c][j] * rstd, w[j], b[j]);
+        store_part<VE>(y + at, n[c], f[c]);
+    }
+}
+
+// Rows too wide for registers: a workgroup reads its row three times, the
+// second and third time from the caches.
+constexpr int kWide = 1024;
+template <class T> __global__ __launch_bounds__(kWide) void k_norm_wide(NormArgs a)
+{
+    constexpr int VE = kVec<T>;
+    __shared__ float red[2][16];
+    int turn = 0;
+    const int64_t row = blockIdx.x;
+    const T *x = (const T *)a.x + row * a.ld_x;
+    float s = 0.f, q = 0.f;
+    for (int64_t at = (int64_t)threadIdx.x * VE; at < a.D; at += kWide * VE) {
+        float f[VE];
+        load_part<VE>(x + at, (int)min((int64_t)VE, a.D - at), f);
+#pragma unroll
+        for (int j = 0; j < VE; j++) s += f[j];
+    }
+    const float mean = row_sum<kWide>(s, red, turn) / (float)a.D;
+    for (int64_t at = (int64_t)threadIdx.x * VE; at < a.D; at += kWide * VE) {
+        float f[VE];
+        const int n = (int)min((int64_t)VE, a.D - at);
+        load_part<VE>(x + at, n, f);
+#pragma unroll
+        for (int j = 0; j < VE; j++)
+            if (j < n) q = fmaf(f[j] - mean, f[j] - mean, q);
+    }
+    const float rstd = 1.f / sqrtf(row_sum<kWide>(q, red, turn) / (float)a.D + a.eps);
+    if (a.mean && threadIdx.x == 0) {
+        a.mean[row] = mean;
+        a.rstd[row] = rstd;
+    }
+    T *y = (T *)a.y + row * a.ld_y;
+    for (int64_t at = (int64_t)threadIdx.x * VE; at < a.D; at += kWide * VE) {
+        const int n = (int)min((int64_t)VE, a.D - at);
+        float f[VE], w[VE], b[VE] = {};
+        load_part<VE>(x + at, n, f);
+        load_part<VE>((const T *)a.weight + at, n, w);
+        if (a.bias) load_part<VE>((const T *)a.bias + at, n, b);
+#pragma unroll
+        for (int j = 0; j < VE; j++) f[j] = fmaf((f[j] - mean) * rstd, w[j], b[j]);
+        store_part<VE>(y + at, n, f);
+    }
+}
+
+// ---------------------------------------------------------------- backward
+// Workgroup b takes rows b R, b R + R, ... (R rows at a time, `gridDim.x * R`
+// apart) and leaves its sums of dy xh and dy in part[b][2][D].
+template <class T, int L, int C>
+__global__ __launch_bounds__(kThreadsOf<L>) void k_norm_grad(NormArgs a, float *part)
+{
+    constexpr int VE = kVec<T>, R = kThreadsOf<L> / L;
+    __shared__ float red[2][16];
+    __shared__ float join[R > 1 ? R : 1][R > 1 ? L * VE : 1];
+    int turn = 0;
+    const int lane = threadIdx.x % L, g = threadIdx.x / L;
+    int n[C];
+    float w[C][VE], dw[C][VE], db[C][VE];
+#pragma unroll
+    for (int c = 0; c < C; c++) {
+        const int64_t at = (int64_t)(c * L + lane) * VE;
+        n[c] = (int)max((int64_t)0, min((int64_t)VE, a.D - at));
+        load_part<VE>((const T *)a.weight + (n[c] ? at : 0), n[c], w[c]);
+#pragma unroll
+        for (int j = 0; j < VE; j++) dw[c][j] = db[c][j] = 0.f;
+    }
+    const float inv = 1.f / (float)a.D;
+    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.N; r0 += (int64_t)gridDim.x * R) {
+        const int64_t row = r0 + g;
+        const bool in = row < a.N;
+        const int64_t rr = in ? row : 0;
+        const float mean = in ? a.mean_in[rr] : 0.f, rstd = in ? a.rstd_in[rr] : 0.f;
+        const T *x = (const T *)a.x + rr * a.ld_x, *dy = (const T *)a.dy + rr * a.ld_dy;
+        float f[C][VE], d[C][VE];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+            const int64_t at = n[c] ? (int64_t)(c * L + lane) * VE : 0;
+            load_part<VE>(x + at, in ? n[c] : 0, f[c]);
+            load_part<VE>(dy + at, in ? n[c] : 0, d[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < C; c++)
+#pragma unroll
+            for (int j = 0; j < VE; j++) {
+                f[c][j] = in && j < n[c] ? (f[c][j] - mean) * rstd : 0.f;  // xh
+                dw[c][j] = fmaf(d[c][j], f[c][j], dw[c][j]);
+                db[c][j] += d[c][j];
+                d[c][j] *= w[c][j];  // u
+                s1 += d[c][j];
+                s2 = fmaf(d[c][j], f[c][j], s2);
+            }
+        const float m1 = row_sum<L>(s1, red, turn) * inv;
+        const float m2 = row_sum<L>(s2, red, turn) * inv;
+        if (!in) continue;
+        T *dx = (T *)a.dx + row * a.ld_dx;
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+            if (!n[c]) continue;
+#pragma unroll
+            for (int j = 0; j < VE; j++) f[c][j] = rstd * (d[c][j] - m1 - f[c][j] * m2);
+            store_part<VE>(dx + (int64_t)(c * L + lane) * VE, n[c], f[c]);
+        }
+    }
+    // one row of sums per workgroup
+    float *out = part + (int64_t)blockIdx.x * 2 * a.D;
+#pragma unroll
+    for (int c = 0; c < C; c++)
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            float(&v)[VE] = k ? db[c] : dw[c];
+            if constexpr (R > 1) {
+#pragma unroll
+                for (int j = 0; j < VE; j++) join[g][lane * VE + j] = v[j];
+                __syncthreads();
+                for (int i = threadIdx.x; i < L * VE; i += kThreadsOf<L>) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int r = 0; r < R; r++) s += join[r][i];
+                    const int64_t at = (int64_t)c * L * VE + i;
+                    if (at < a.D) out[k * a.D + at] = s;
+                }
+                __syncthreads();
+            } else {
+                const int64_t at = (int64_t)(c * L + lane) * VE;
+                store_part<VE>(out + k * a.D + (n[c] ? at : 0), n[c], v);
+            }
+        }
+}
+
+// Wide rows: the workgroup's sums lie in its row of `part` from the first row on.
+template <class T> __global__ __launch_bounds__(kWide) void k_norm_grad_wide(NormArgs a, float *part)
+{
+    constexpr int VE = kVec<T>;
+    __shared__ float red[2][16];
+    int turn = 0;
+    float *out = part + (int64_t)blockIdx.x * 2 * a.D;
+    const float inv = 1.f / (float)a.D;
+    bool first = true;
+    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x, first = false) {
+        const float mean = a.mean_in[row], rstd = a.rstd_in[row];
+        const T *x = (const T *)a.x + row * a.ld_x, *dy = (const T *)a.dy + row * a.ld_dy;
+        float s1 = 0.f, s2 = 0.f;
+        for (int64_t at = (int64_t)threadIdx.x * VE; at < a.D; at += kWide * VE) {
+            const int n = (int)min((int64_t)VE, a.D - at);
+            float f[VE], d[VE], w[VE], pw[VE] = {}, pb[VE] = {};
+            load_part<VE>(x + at, n, f);
+            load_part<VE>(dy + at, n, d);
+            load_part<VE>((const T *)a.weight + at, n, w);
+            if (!first) {
+                load_part<VE>(out + at, n, pw);
+                load_part<VE>(out + a.D + at, n, pb);
+            }
+#pragma unroll
+            for (int j = 0; j < VE; j++) {
+                const float xh = j < n ? (f[j] - mean) * rstd : 0.f;
+                pw[j] = fmaf(d[j], xh, pw[j]);
+                pb[j] += d[j];
+                const float u = d[j] * w[j];
+                s1 += u;
+                s2 = fmaf(u, xh, s2);
+            }
+            store_part<VE>(out + at, n, pw);
+            store_part<VE>(out + a.D + at, n, pb);
+        }
+        const float m1 = row_sum<kWide>(s1, red, turn) * inv;
+        const float m2 = row_sum<kWide>(s2, red, turn) * inv;
+        T *dx = (T *)a.dx + row * a.ld_dx;
+        for (int64_t at = (int64_t)threadIdx.x * VE; at < a.D; at += kWide * VE) {
+            const int n = (int)min((int64_t)VE, a.D - at);
+            float f[VE], d[VE], w[VE];
+            load_part<VE>(x + at, n, f);
+            load_part<VE>(dy + at, n, d);
+            load_part<VE>((const T *)a.weight + at, n, w);
+#pragma unroll
+            for (int j = 0; j < VE; j++) f[j] = rstd * (d[j] * w[j] - m1 - (f[j] - mean) * rstd * m2);
+            store_part<VE>(dx + at, n, f);
+        }
+    }
+}
+
+// dweight and dbias: the sums of the `rows` rows of part, 64 columns of the 2 D
+// per workgroup, its wavefronts taking every 16th row.
+constexpr int kJoinWaves = 16;
+template <class T>
+__global__ __launch_bounds__(kJoinWaves * 64) void k_norm_join(NormArgs a, const float *part, int rows)
+{
+    __shared__ float red[kJoinWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (c < 2 * a.D)
+#pragma unroll 8
+        for (int r = wave; r < rows; r += kJoinWaves) s += part[(int64_t)r * 2 * a.D + c];
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < 2 * a.D) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < kJoinWaves; w++) t += red[w][lane];
+        if (c < a.D) ((T *)a.dweight)[c] = (T)t;
+        else if (a.dbias) ((T *)a.dbias)[c - a.D] = (T)t;
+    }
+}
+
+// Calls f with the lanes and chunks for rows of D elements, or with 0 lanes for
+// rows wider than the registers of a workgroup take.
+template <class T, class F> hipError_t by_width(int64_t D, F &&f)
+{
+#define TQ_ROW(L, C)                                                                                                   \
+    if (chunks <= (int64_t)(L) * (C)) return f(std::integral_constant<int, L>{}, std::integral_constant<int, C>{})
+    const int64_t chunks = (D + kVec<T> - 1) / kVec<T>;
+    TQ_ROW(8, 1);
+    TQ_ROW(16, 1);
+    TQ_ROW(32, 1);
+    TQ_ROW(64, 1);
+    TQ_ROW(64, 2);
+    TQ_ROW(64, 3);
+    TQ_ROW(64, 4);
+    TQ_ROW(256, 2);
+    TQ_ROW(256, 4);
+    TQ_ROW(512, 4);
+#undef TQ_ROW
+    return f(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+}
+
+// Workgroups of the backward pass: enough to fill the chip several times, few
+// enough that their rows of sums are small beside x.
+constexpr int64_t kGradBlocks = 1024;
+
+template <class T> hipError_t norm_t(const NormArgs &a, hipStream_t s)
+{
+    return by_width<T>(a.D, [&](auto l, auto c) {
+        constexpr int L = decltype(l)::value, C = decltype(c)::value;
+        if constexpr (L == 0) k_norm_wide<T><<<(unsigned)a.N, kWide, 0, s>>>(a);
+        else {
+            constexpr int R = kThreadsOf<L> / L;
+            k_norm<T, L, C><<<(unsigned)((a.N + R - 1) / R), kThreadsOf<L>, 0, s>>>(a);
+        }
+        return hipGetLastError();
+    });
+}
+
+template <class T> hipError_t norm_grad_t(const NormArgs &a, hipStream_t s)
+{
+    return by_width<T>(a.D, [&](auto l, auto c) {
+        constexpr int L = decltype(l)::value, C = decltype(c)::value;
+        float *part = (float *)a.ws;
+        int64_t blocks;
+        if constexpr (L == 0) {
+            blocks = std::min(a.N, kGradBlocks / 4);
+            if (blocks) k_norm_grad_wide<T><<<(unsigned)blocks, kWide, 0, s>>>(a, part);
+        } else {
+            constexpr int R = kThreadsOf<L> / L;
+            blocks = std::min((a.N + R - 1) / R, kGradBlocks);
+            if (blocks) k_norm_grad<T, L, C><<<(unsigned)blocks, kThreadsOf<L>, 0, s>>>(a, part);
+        }
+        k_norm_join<T><<<(unsigned)((2 * a.D + 63) / 64), kJoinWaves * 64, 0, s>>>(a, part, (int)blocks);
+        return hipGetLastError();
+    });
+}
+
+} // namespace
+
+size_t norm_grad_workspace(int64_t N, int64_t D)
+{
+    return sizeof(float) * 2 * (size_t)D * (size_t)std::min(N, kGradBlocks);
+}
+
+hipError_t launch_norm(int32_t type, const NormArgs &a, hipStream_t s)
+{
+    if (type == TQ_F32) return norm_t<float>(a, s);
+    if (type == TQ_BF16) return norm_t<__bf16>(a, s);
+    return norm_t<_Float16>(a, s);
+}
+
+hipError_t launch_norm_grad(int32_t type, const NormArgs &a, hipStream_t s)
+{
+    if (type == TQ_F32) return norm_grad_t<float>(a, s);
+    if (type == TQ_BF16) return norm_grad_t<__bf16>(a, s);
+    return norm_grad_t<_Float16>(a, s);
+}
+
+} // namespace tq

@@ -16,22 +16,20 @@
 #include <vector>
 
 #include "../../include/tq.h"
+#include "abi_util.h"
 #include "jit.h"
 #include "kernels.h"
 #include "program.h"
 
 using namespace tq;
 
-namespace {
-
-thread_local std::string g_err;
-
-[[noreturn]] void fail(int status, const std::string &m) { throw Error{status, m}; }
-
-void hip_check(hipError_t e, const char *what)
+std::string &tq::error_text()
 {
-    if (e != hipSuccess) fail(TQ_E_DEVICE, std::string(what) + ": " + hipGetErrorString(e));
+    thread_local std::string text;
+    return text;
 }
+
+namespace {
 
 // A device allocation owned by a handle, grown on demand.
 struct DevBuf {
@@ -313,24 +311,6 @@ struct tq_program_s {
 };
 
 namespace {
-
-template <class F> tq_status guarded(F &&f)
-{
-    try {
-        f();
-        g_err.clear();
-        return TQ_OK;
-    } catch (const Error &e) {
-        g_err = e.msg;
-        return (tq_status)e.status;
-    } catch (const std::bad_alloc &) {
-        g_err = "host allocation failed";
-        return TQ_E_NOMEM;
-    } catch (...) {
-        g_err = "internal error";
-        return TQ_E_DEVICE;
-    }
-}
 
 std::vector<MemberDev> device_members(const Group &g)
 {
@@ -982,7 +962,6 @@ void pauli_group(tq_program p, size_t gi, const float2 *psi, float2 *phi, const 
     }
 }
 
-hipStream_t as_stream(void *s) { return reinterpret_cast<hipStream_t>(s); }
 
 // Small circuits run as one resident kernel per call when psi (and phi), the
 // row's matrices and the accumulators fit in LDS.
@@ -1105,13 +1084,6 @@ void forward_to_ws(tq_program p, size_t gi, const float *theta, float2 *psi, hip
     }
     build_mats(p, gi, theta, g.fwd_tasks.begin, g.fwd_tasks.end, s, rr, true);
     forward(p, gi, psi, (int64_t)1 << g.n, rr.ident, s, rr);
-}
-
-
-void check_align(const void *p, size_t a, const char *name)
-{
-    if (reinterpret_cast<uintptr_t>(p) % a != 0)
-        fail(TQ_E_INVALID, std::string(name) + " must be " + std::to_string(a) + "-byte aligned");
 }
 
 void fill_levels(SampArgs &a, int n)
@@ -1833,7 +1805,7 @@ void adjoint_group(tq_program prog, size_t gi, const float *theta, int K, const 
 // ------------------------------------------------------------------- ABI
 extern "C" {
 
-const char *tq_last_error(void) { return g_err.c_str(); }
+const char *tq_last_error(void) { return error_text().c_str(); }
 const char *tq_version(void) { return "tq 0.1 (gfx950)"; }
 
 tq_status tq_program_create(const void *blob, size_t nbytes, const tq_options *opt, tq_program *out)
