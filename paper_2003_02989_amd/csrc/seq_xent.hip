@@ -5,19 +5,26 @@
 //   dhidden = diag(up) p weight,   dweight = (diag(up) p)^T hidden.
 //
 // Bound by the matrix products (2 N V D operations each): they run on the
-// matrix cores in 16 bits with fp32 sums, in one kernel for products of two
-// operands whose rows run along the summed axis (C = A B^T).  The logits are never
+// matrix cores in 16 bits with fp32 sums, in one kernel for products C = A B^T
+// whose operands may each lie along the summed axis or across it.  The logits are never
 // stored: the forward product's epilogue turns each tile of 256 (or 128) words
 // by as many tokens into one maximum and one sum of exponentials per token.  For the
 // gradient the vocabulary is taken in pieces; a piece's logits are formed a
-// second time, now with lse known, and its p is stored in 16 bits twice, along
-// the vocabulary for dhidden and along the tokens for dweight.
+// second time, now with lse known, and its p is stored in 16 bits, to be read
+// along the vocabulary for dhidden and along the tokens for dweight.
 //
 // 16-bit inputs enter the products as they are.  fp32 inputs enter as two
 // 16-bit (f16) numbers each, h + l with l the rounding error of h, after a
-// power-of-two scale per row: a b = h_a h_b + h_a l_b + l_a h_b leaves out
-// l_a l_b, 2^-22 of the product, and costs three products; fp32 matrix
-// instructions would cost sixteen times the 16-bit ones.
+// power-of-two scale: a b = h_a h_b + h_a l_b + l_a h_b leaves out l_a l_b,
+// 2^-22 of the product, and costs three products; fp32 matrix instructions
+// would cost sixteen times the 16-bit ones.
+//
+// Powers of two.  With up = f 2^e, 1 <= |f| < 2, the stored p carries f, the
+// hidden rows of dweight's product carry 2^e (relative to the largest row, so that
+// 16 bits hold them), and dhidden's rows are multiplied by 2^e at the end:
+// all exact.  fp32 rows are scaled to magnitudes of 2^13 .. 2^14 on their own
+// where the product leaves the row's axis standing; the weights of dhidden's
+// product, which sums over words, have one scale for all.
 #include <algorithm>
 #include <type_traits>
 
@@ -43,28 +50,31 @@ __device__ __forceinline__ f32x16 mfma32(frag<_Float16> a, frag<_Float16> b, f32
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// p is held as p 2^15 in 16 bits: |p| <= 1 fits f16, whose small numbers would
-// otherwise not reach the probabilities of a large vocabulary.
-constexpr float kProbScale = 32768.f;
+// p f is held times 2^14 in 16 bits: below 2^15 it fits f16, whose small numbers
+// would otherwise not reach the probabilities of a large vocabulary.
+constexpr int kProbBits = 14;
 
 // ------------------------------------------------------------ C = A B^T
-// A [M, K] and B [N, K] of 16-bit elements, K a multiple of kBK, rows 16-byte
-// aligned.  fp32 operands have two parts each, `a_part` / `b_part` elements
-// apart: `terms` products A[pa] B[pb]^T are summed.
+// Operands of 16-bit elements, rows 16-byte aligned.  Along the summed axis:
+// `extent` rows (of C, or columns of C) of K elements, K a multiple of kBK.  Across
+// it: `k_rows` rows, one per summed index, of `extent` elements, a multiple of 8.
+// What is read past `extent` is never used; past `k_rows` the last row is
+// read again, and the other operand is zero there.  fp32 operands have two
+// parts, `part` elements apart.
 constexpr int kBK = 64;
 
 struct Operand {
     const void *p;
-    int64_t ld, part;
-    int64_t rows;
+    int64_t ld, part, extent, k_rows;
 };
 
 struct ProductArgs {
     Operand a, b;
-    int terms;     // 1, or 3 for operands in two parts
-    int k_tiles;   // K / kBK
-    int splits;    // the K axis is cut into this many parts, one slab of C each
+    int terms;    // 1, or 3 for operands in two parts
+    int k_tiles;  // K / kBK
     int m_tiles, n_tiles;
+    int full;     // tiles that one workgroup computes alone; the others are
+    int splits;   // cut along K into this many
 };
 
 // Tile of C, wavefronts WM x WN, each with FM x FN blocks of 32 x 32.
@@ -83,35 +93,78 @@ __device__ __forceinline__ int block_row(int i, int lane) { return 8 * (i >> 2) 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
-// One stage of the tile in LDS: rows of kBK elements (eight 16-byte pieces), the
-// pieces of row r in the order piece ^ (r % 8), so that 32 lanes reading one piece
-// of 32 rows meet all banks.  Read straight from global memory into LDS: a
-// wavefront's 64 lanes fill eight rows.
-template <class T, int ROWS, int WAVES>
-__device__ __forceinline__ void stage(T *lds, const T *src, int64_t ld, int64_t row0, int64_t rows, int wave, int lane)
+// One stage of an operand in LDS, W rows (or columns) of C by kBK, read straight
+// from global memory, 16 bytes per lane.
+//
+// Along K: W rows of eight 16-byte pieces, the pieces of row r in the order
+// piece ^ (r % 8), so that 32 lanes reading one piece of 32 rows meet all banks.
+template <class T, int W, int WAVES>
+__device__ __forceinline__ void stage(T *lds, const T *src, const Operand &o, int64_t k0, int64_t at, int wave, int lane)
 {
 #pragma unroll
-    for (int i = 0; i < ROWS / 8 / WAVES; i++) {
+    for (int i = 0; i < W / 8 / WAVES; i++) {
         const int r8 = (i * WAVES + wave) * 8;
-        const int r = r8 + (lane >> 3);
-        // rows past the end repeat the last one: read, never used
-        const int64_t row = min(row0 + r, rows - 1);
-        const T *g = src + row * ld + ((lane & 7) ^ (lane >> 3)) * 8;
+        const int64_t row = min(at + r8 + (lane >> 3), o.extent - 1);
+        const T *g = src + row * o.ld + k0 + ((lane & 7) ^ (lane >> 3)) * 8;
         __builtin_amdgcn_global_load_lds((global_void *)g, (lds_void *)(lds + r8 * kBK), 16, 0, 0);
     }
 }
-
-template <class T> __device__ __forceinline__ frag<T> read_frag(const T *lds, int row, int piece)
+template <class T> __device__ __forceinline__ frag<T> read_frag(const T *lds, int at, int ks, int lane)
 {
+    const int row = at + (lane & 31), piece = ks * 2 + (lane >> 5);
     return *(const frag<T> *)(lds + row * kBK + ((piece ^ (row & 7)) * 8));
 }
 
-// The tile's sums over this workgroup's part of K.
-template <class T, class S>
-__device__ __forceinline__ void product(const ProductArgs &a, int64_t m0, int64_t n0, int split,
-                                        f32x16 (&acc)[S::FM][S::FN])
+// Across K: kBK rows of W elements.  The transposing LDS read gives 16 lanes
+// four rows each of 16 columns, from 8 bytes at four rows by four pieces of four
+// elements; row k has its 16-byte pieces in the order piece ^ 2 (k % 4), so
+// that the four rows lie in different banks.
+template <class T, int W, int WAVES>
+__device__ __forceinline__ void stage_t(T *lds, const T *src, const Operand &o, int64_t k0, int64_t at, int wave,
+                                        int lane)
 {
-    __shared__ alignas(1024) T A0[S::BM * kBK], B0[S::BN * kBK], A1[S::BM * kBK], B1[S::BN * kBK];
+    constexpr int PIECES = W / 8, ROWS = 64 / PIECES;  // of one instruction
+    static_assert(kBK % (ROWS * WAVES) == 0, "whole rows per wavefront");
+#pragma unroll
+    for (int i = 0; i < kBK / ROWS / WAVES; i++) {
+        const int r0 = (i * WAVES + wave) * ROWS, r = r0 + lane / PIECES;
+        const int64_t k = min(k0 + r, o.k_rows - 1);
+        int64_t col = at + ((lane % PIECES) ^ (2 * (r & 3))) * 8;
+        if (col >= o.extent) col = 0;
+        __builtin_amdgcn_global_load_lds((global_void *)(src + k * o.ld + col), (lds_void *)(lds + r0 * W), 16, 0, 0);
+    }
+}
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+template <class T, int W> __device__ __forceinline__ frag<T> read_frag_t(const T *lds, int at, int ks, int lane)
+{
+    const int i = lane & 15, g = lane >> 4;
+    const int k = ks * 16 + 8 * (g >> 1) + (i >> 2), col = at + 16 * (g & 1) + 4 * (i & 3);
+    const T *p = lds + k * W + (((col >> 3) ^ (2 * ((i >> 2) & 3))) * 8) + (col & 7);
+    union {
+        s16x4 half[2];
+        frag<T> all;
+    } u;
+    u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * W));
+    return u.all;
+}
+
+template <class T, class S> struct Stages {
+    T *a0, *b0, *a1, *b1;
+};
+// The four arrays are separate objects: the compiler then knows that reads of
+// one stage do not wait for loads into the other.
+#define TQ_STAGES(T, S, name)                                                                                          \
+    __shared__ alignas(1024) T name##_a0[S::BM * kBK], name##_b0[S::BN * kBK], name##_a1[S::BM * kBK],                 \
+        name##_b1[S::BN * kBK];                                                                                        \
+    const Stages<T, S> name{name##_a0, name##_b0, name##_a1, name##_b1}
+
+// The sums of the tile at (m0, n0) over the K tiles [k0, k1) (of all terms).
+template <class T, class S, bool TA, bool TB>
+__device__ __forceinline__ void product(const ProductArgs &a, const Stages<T, S> &l, int64_t m0, int64_t n0, int k0,
+                                        int k1, f32x16 (&acc)[S::FM][S::FN])
+{
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
 #pragma unroll
@@ -120,41 +173,46 @@ __device__ __forceinline__ void product(const ProductArgs &a, int64_t m0, int64_
         for (int j = 0; j < S::FN; j++)
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
-    const int all = a.terms * a.k_tiles;
-    const int k0 = (int)((int64_t)all * split / a.splits), k1 = (int)((int64_t)all * (split + 1) / a.splits);
     auto fetch = [&](int kt, T *la, T *lb) {
         // the small terms first: l_a h_b, h_a l_b, h_a h_b
-        const int term = kt / a.k_tiles, k = kt - term * a.k_tiles;
-        const bool low_a = a.terms == 3 && term == 0, low_b = a.terms == 3 && term == 1;
-        const T *ga = (const T *)a.a.p + (low_a ? a.a.part : 0) + (int64_t)k * kBK;
-        const T *gb = (const T *)a.b.p + (low_b ? a.b.part : 0) + (int64_t)k * kBK;
-        stage<T, S::BM, S::waves>(la, ga, a.a.ld, m0, a.a.rows, wave, lane);
-        stage<T, S::BN, S::waves>(lb, gb, a.b.ld, n0, a.b.rows, wave, lane);
+        const int term = kt / a.k_tiles;
+        const int64_t k = (int64_t)(kt - term * a.k_tiles) * kBK;
+        const T *ga = (const T *)a.a.p + (a.terms == 3 && term == 0 ? a.a.part : 0);
+        const T *gb = (const T *)a.b.p + (a.terms == 3 && term == 1 ? a.b.part : 0);
+        if constexpr (TA) stage_t<T, S::BM, S::waves>(la, ga, a.a, k, m0, wave, lane);
+        else stage<T, S::BM, S::waves>(la, ga, a.a, k, m0, wave, lane);
+        if constexpr (TB) stage_t<T, S::BN, S::waves>(lb, gb, a.b, k, n0, wave, lane);
+        else stage<T, S::BN, S::waves>(lb, gb, a.b, k, n0, wave, lane);
     };
     auto compute = [&](const T *la, const T *lb) {
 #pragma unroll
         for (int ks = 0; ks < kBK / 16; ks++) {
             frag<T> fa[S::FM], fb[S::FN];
-            const int piece = ks * 2 + (lane >> 5);
 #pragma unroll
-            for (int i = 0; i < S::FM; i++) fa[i] = read_frag<T>(la, wm + i * 32 + (lane & 31), piece);
+            for (int i = 0; i < S::FM; i++) {
+                if constexpr (TA) fa[i] = read_frag_t<T, S::BM>(la, wm + i * 32, ks, lane);
+                else fa[i] = read_frag<T>(la, wm + i * 32, ks, lane);
+            }
 #pragma unroll
-            for (int j = 0; j < S::FN; j++) fb[j] = read_frag<T>(lb, wn + j * 32 + (lane & 31), piece);
+            for (int j = 0; j < S::FN; j++) {
+                if constexpr (TB) fb[j] = read_frag_t<T, S::BN>(lb, wn + j * 32, ks, lane);
+                else fb[j] = read_frag<T>(lb, wn + j * 32, ks, lane);
+            }
 #pragma unroll
             for (int i = 0; i < S::FM; i++)
 #pragma unroll
                 for (int j = 0; j < S::FN; j++) acc[i][j] = mfma32(fa[i], fb[j], acc[i][j]);
         }
     };
-    if (k0 < k1) fetch(k0, A0, B0);
+    if (k0 < k1) fetch(k0, l.a0, l.b0);
     __syncthreads();
     for (int kt = k0; kt < k1; kt += 2) {
-        if (kt + 1 < k1) fetch(kt + 1, A1, B1);
-        compute(A0, B0);
+        if (kt + 1 < k1) fetch(kt + 1, l.a1, l.b1);
+        compute(l.a0, l.b0);
         __syncthreads();
         if (kt + 1 < k1) {
-            if (kt + 2 < k1) fetch(kt + 2, A0, B0);
-            compute(A1, B1);
+            if (kt + 2 < k1) fetch(kt + 2, l.a0, l.b0);
+            compute(l.a1, l.b1);
             __syncthreads();
         }
     }
@@ -167,22 +225,43 @@ __device__ __forceinline__ void product(const ProductArgs &a, int64_t m0, int64_
 constexpr int kXcds = 8, kGroup = 4;
 struct Tile {
     int64_t m, n;
-    int split;
+    int id, split;  // split: -1 when the workgroup has the tile to itself
 };
 __device__ __forceinline__ Tile tile_of(const ProductArgs &a)
 {
-    const int tiles = a.m_tiles * a.n_tiles, all = tiles * a.splits;
     const int blk = blockIdx.x;
-    const int per = all / kXcds, more = all % kXcds, xcd = blk % kXcds, at = blk / kXcds;
-    int id = xcd * per + min(xcd, more) + at;
     Tile t;
-    t.split = id / tiles;
-    id -= t.split * tiles;
-    const int band = kGroup * a.n_tiles, g = id / band, rows = min(kGroup, a.m_tiles - g * kGroup);
-    const int in = id - g * band;
+    if (blk < a.full) {
+        const int per = a.full / kXcds, more = a.full % kXcds, xcd = blk % kXcds;
+        t.id = xcd * per + min(xcd, more) + blk / kXcds;
+        t.split = -1;
+    } else {
+        const int left = a.m_tiles * a.n_tiles - a.full;
+        t.id = a.full + (blk - a.full) % left;
+        t.split = (blk - a.full) / left;
+    }
+    const int band = kGroup * a.n_tiles, g = t.id / band, rows = min(kGroup, a.m_tiles - g * kGroup);
+    const int in = t.id - g * band;
     t.m = g * kGroup + in % rows;
     t.n = in / rows;
     return t;
+}
+
+// Orders the LDS accesses of one wavefront's lanes (they execute in order; this
+// keeps the compiler from moving them).
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// up = f 2^e with 1 <= |f| < 2 (f below 1 for subnormal numbers; zeros, infinities
+// and NaN stay in f).
+__device__ __forceinline__ void split_up(float up, float &f, int &e)
+{
+    const int x = (int)((__float_as_uint(up) >> 23) & 255);
+    e = x == 255 ? 0 : max(x, 1) - 127;
+    f = ldexpf(up, -e);
 }
 
 // ------------------------------------------------------------ the logits
@@ -190,46 +269,65 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs &a)
 // words of one token, so that sums over words stay within a lane until the end.
 struct LogitArgs {
     ProductArgs p;
-    const float *word_scale, *token_scale;  // of fp32 operands, else NULL
+    const float *word_scale, *token_scale;  // of fp32 operands
     const uint64_t *targets;
     int64_t V, N;
-    int64_t v_base;        // first word of the piece (p.a.p points there)
-    float2 *part;          // [N, tiles]: maximum, sum of exponentials
-    float *z_target;       // [N]
-    const float *lse, *up, *up_max;
-    void *prob, *prob_t;   // [N, words] and [words, N] of the piece
-    int64_t ld_prob, ld_prob_t, prob_part, prob_t_part;
+    int64_t v_base;    // first word of the piece (p.a.p and word_scale point there)
+    float2 *part;      // [N, tiles]: maximum, sum of exponentials
+    float *z_target;   // [N]
+    const float *lse, *up;
+    void *prob;        // [tokens, words] of the piece, both up to a multiple of kBK
+    int64_t ld_prob, prob_rows, prob_part;
 };
 
 template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S::threads) void k_logits(LogitArgs a)
 {
+    TQ_STAGES(T, S, lds);
     const Tile t = tile_of(a.p);
     f32x16 acc[S::FM][S::FN];
     const int64_t m0 = t.m * S::BM, n0 = t.n * S::BN;
-    product<T, S>(a.p, m0, n0, 0, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    product<T, S, false, false>(a.p, lds, m0, n0, 0, a.p.terms * a.p.k_tiles, acc);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
-    const int64_t words = a.p.a.rows;  // of the piece
+    const int v0 = (int)m0 + wm;               // the wavefront's first word, in the piece
+    const int words = (int)a.p.a.extent - v0;  // words from there on
+    if constexpr (TWO) {
+        // back from the scaled numbers
+        float ts[S::FN];
+#pragma unroll
+        for (int j = 0; j < S::FN; j++) ts[j] = a.token_scale[min(n0 + wn + j * 32 + (lane & 31), a.N - 1)];
+#pragma unroll
+        for (int i = 0; i < S::FM; i++)
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                // four words in a row; the array goes on past the last word
+                const f32x4 ws = *(const f32x4 *)(a.word_scale + v0 + i * 32 + block_row(4 * q, lane));
+#pragma unroll
+                for (int j = 0; j < S::FN; j++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) acc[i][j][4 * q + e] *= ws[e] * ts[j];
+                __builtin_amdgcn_sched_barrier(0);  // few loads ahead: registers
+            }
+    }
     if constexpr (!GRAD) {
         __shared__ float2 join[S::WM][S::BN];
 #pragma unroll
         for (int j = 0; j < S::FN; j++) {
             const int64_t n = n0 + wn + j * 32 + (lane & 31);
-            const float ts = TWO && n < a.N ? a.token_scale[n] : 1.f;
             const uint64_t target = n < a.N ? a.targets[n] : ~(uint64_t)0;
-            float top = -INFINITY;
+            const int hit = target < (uint64_t)a.V ? (int)target - v0 : -1;
+            float top = -INFINITY, zt = 0.f;
+            bool found = false;
 #pragma unroll
             for (int i = 0; i < S::FM; i++)
 #pragma unroll
                 for (int e = 0; e < 16; e++) {
-                    const int64_t v = m0 + wm + i * 32 + block_row(e, lane);
-                    float z = acc[i][j][e];
-                    if (TWO) z *= ts * (v < words ? a.word_scale[v] : 0.f);
-                    if (v >= words) z = -INFINITY;
-                    else if ((uint64_t)v == target) a.z_target[n] = z;
-                    acc[i][j][e] = z;
-                    top = fmaxf(top, z);
+                    const int w = i * 32 + block_row(e, lane);
+                    if (w == hit) zt = acc[i][j][e], found = true;
+                    if (w >= words) acc[i][j][e] = -INFINITY;
+                    top = fmaxf(top, acc[i][j][e]);
                 }
+            if (found) a.z_target[n] = zt;
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             // without words there is nothing to add; NaN stays in the sum
             const float ref = top == -INFINITY ? 0.f : top;
@@ -252,246 +350,351 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
             if (n0 + c < a.N) a.part[(n0 + c) * a.p.m_tiles + t.m] = make_float2(top, sum);
         }
     } else {
-        const float up_inv = 1.f / *a.up_max;
 #pragma unroll
         for (int j = 0; j < S::FN; j++) {
             const int64_t n = n0 + wn + j * 32 + (lane & 31);
-            const bool in = n < a.N;
-            const float ts = TWO && in ? a.token_scale[n] : 1.f;
-            const uint64_t target = in ? a.targets[n] : ~(uint64_t)0;
+            const uint64_t target = n < a.N ? a.targets[n] : ~(uint64_t)0;
             const bool on = target < (uint64_t)a.V;
             const float lse = on ? a.lse[n] : 0.f;
-            const float share = on ? a.up[n] * up_inv : 0.f;
+            const int64_t away = on ? (int64_t)target - a.v_base - v0 : -1;
+            const int hit = away >= 0 && away < S::FM * 32 ? (int)away : -1;
+            float f = 0.f;
+            int e2;
+            if (on) split_up(a.up[n], f, e2);
+            f *= (float)(1 << kProbBits);
+            const int last = on ? words : 0;
 #pragma unroll
             for (int i = 0; i < S::FM; i++)
 #pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    // four words in a row
-                    const int64_t v = m0 + wm + i * 32 + block_row(4 * q, lane);
-                    T hi[4], lo[4];
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        float z = acc[i][j][4 * q + e];
-                        if (TWO) z *= ts * (v + e < words ? a.word_scale[v + e] : 0.f);
-                        float p = __expf(z - lse);
-                        if ((uint64_t)(a.v_base + v + e) == target) p -= 1.f;
-                        p = on && v + e < words ? p * kProbScale : 0.f;
-                        hi[e] = (T)p;
-                        if (TWO) lo[e] = (T)(p - (float)hi[e]);
-                        const float pt = p * share;
-                        if (n < a.ld_prob_t && v + e < words) {
-                            T *o = (T *)a.prob_t + (v + e) * a.ld_prob_t + n;
-                            const T ht = (T)pt;
-                            o[0] = ht;
-                            if (TWO) o[a.prob_t_part] = (T)(pt - (float)ht);
-                        }
-                    }
-                    if (in && v < a.ld_prob) {
-                        T *o = (T *)a.prob + n * a.ld_prob + v;
-                        __builtin_memcpy(o, hi, sizeof hi);
-                        if (TWO) __builtin_memcpy(o + a.prob_part, lo, sizeof lo);
-                    }
+                for (int e = 0; e < 16; e++) {
+                    const int w = i * 32 + block_row(e, lane);
+                    float p = __expf(acc[i][j][e] - lse);
+                    if (w == hit) p -= 1.f;
+                    acc[i][j][e] = w < last ? p * f : 0.f;
                 }
+        }
+        // Each wavefront turns its words x tokens through LDS (the stages are done
+        // with), tokens as rows, 16-byte pieces in the order piece ^ token, and
+        // writes whole rows.
+        constexpr int WORDS = S::FM * 32, TOKENS = S::FN * 32, PIECES = WORDS / 8, PER = S::waves / 4;
+        static_assert(PER * WORDS * TOKENS <= S::BM * kBK && PER * WORDS * TOKENS <= S::BN * kBK, "fits the stages");
+        T *const buf = (wave / PER == 0   ? lds.a0
+                        : wave / PER == 1 ? lds.b0
+                        : wave / PER == 2 ? lds.a1
+                                          : lds.b1) +
+                       wave % PER * WORDS * TOKENS;
+#pragma unroll
+        for (int part = 0; part < (TWO ? 2 : 1); part++) {
+#pragma unroll
+            for (int j = 0; j < S::FN; j++) {
+                const int row = j * 32 + (lane & 31);
+#pragma unroll
+                for (int i = 0; i < S::FM; i++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        T four[4];
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const float p = acc[i][j][4 * q + e];
+                            four[e] = (T)p;
+                            if (part == 0) acc[i][j][4 * q + e] = TWO ? p - (float)four[e] : p;
+                        }
+                        const int piece = i * 4 + q;
+                        __builtin_memcpy(__builtin_assume_aligned(buf + row * WORDS + ((piece ^ (row & (PIECES - 1))) * 8) +
+                                                                      4 * (lane >> 5),
+                                                                  8),
+                                         four, 8);
+                    }
+            }
+            wave_fence();
+            T *out = (T *)a.prob + part * a.prob_part;
+#pragma unroll
+            for (int k = 0; k < TOKENS * PIECES / 64; k++) {
+                const int row = (k * 64 + lane) / PIECES, piece = lane % PIECES;
+                const frag<T> v = *(const frag<T> *)(buf + row * WORDS + ((piece ^ (row & (PIECES - 1))) * 8));
+                const int64_t n = n0 + wn + row, w = v0 + piece * 8;
+                if (n < a.prob_rows && w < a.ld_prob) *(frag<T> *)(out + n * a.ld_prob + w) = v;
+            }
+            wave_fence();
         }
     }
 }
 
 // ------------------------------------------------------------ the products
-// out = factor diag(row_factor) C diag(col_scale), or fp32 slabs of C, one per
-// split, which later pieces add to and k_finish sums up.
+// What becomes of C: out = factor(row) C, or C is added up in fp32 over the
+// pieces of the vocabulary (`sum`), or a part of a tile goes to its slab.
 struct StoreArgs {
     ProductArgs p;
     int64_t M, N;
-    float *slabs;   // NULL: write `out`
-    bool add;       // to what the slabs hold
+    float *slabs;  // [tile past `full`][split][BM BN]
+    float *sum;    // NULL: write `out`
+    bool add;      // to what `sum` holds
     void *out;
     int64_t ld_out;
-    // of an output row or column; NULL: one
-    const float *row_up;        // upstream, where the row has a target
+    // factor: 2^(exponent of up) of the row, or 2^*e_max for all; and the scale of
+    // the second operand
+    const float *up;
     const uint64_t *targets;
     int64_t V;
-    const float *col_max;       // columns of the second operand: scale_of(col_max)
-    const float *up_max;
+    const int *e_max;
+    const float *w_max;
 };
 
 // The power of two that brings numbers of magnitude up to m into [2^13, 2^14).
-__device__ __forceinline__ float scale_of(float m)
+__device__ __forceinline__ int scale_bits(float m)
 {
-    if (!(m > 0.f)) return m == 0.f ? 1.f : m;
-    if (m > 3.4e38f) return NAN;
-    const int e = max((int)((__float_as_uint(m) >> 23) & 255) - 127, -100);
-    return __uint_as_float((uint32_t)(e - 13 + 127) << 23);
+    return max((int)((__float_as_uint(m) >> 23) & 255) - 127, -100) - 13;
 }
-__device__ __forceinline__ float inverse_of(float scale) { return 1.f / scale; }  // exact: a power of two
+__device__ __forceinline__ float two_to(int e) { return ldexpf(1.f, e); }
 
-__device__ __forceinline__ float row_factor(const StoreArgs &a, int64_t m)
+// The maximum of kMaxParts partial maxima, by one wavefront.
+constexpr int kMaxParts = 128;
+__device__ __forceinline__ float max_of(const float *part)
 {
-    float f = 1.f / kProbScale;
-    if (a.row_up) f = a.targets[m] < (uint64_t)a.V ? f * a.row_up[m] : 0.f;
-    if (a.up_max) f *= *a.up_max;
-    return f;
-}
-__device__ __forceinline__ float col_factor(const StoreArgs &a, int64_t n)
-{
-    return a.col_max ? scale_of(a.col_max[n]) : 1.f;
+    const int lane = threadIdx.x & 63;
+    float m = fmaxf(part[lane], part[lane + 64]);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    return m;
 }
 
-template <class T, class S, class Out> __global__ __launch_bounds__(S::threads) void k_product(StoreArgs a)
+struct Factor {
+    const StoreArgs &a;
+    int bits;
+    __device__ explicit Factor(const StoreArgs &s) : a(s), bits(-kProbBits)
+    {
+        if (a.w_max) bits += scale_bits(max_of(a.w_max));
+        if (a.e_max) bits += *a.e_max;
+    }
+    // c times the factor of row m; a row without a target is zero whatever the
+    // weights hold
+    __device__ float of(float c, int64_t m) const
+    {
+        if (!a.up) return ldexpf(c, bits);
+        if (a.targets[m] >= (uint64_t)a.V) return 0.f;
+        float f;
+        int e;
+        split_up(a.up[m], f, e);
+        return ldexpf(c, bits + e);
+    }
+};
+
+template <class T, class S, bool TA, bool TB, class Out>
+__global__ __launch_bounds__(S::threads) void k_product(StoreArgs a)
 {
+    TQ_STAGES(T, S, lds);
     const Tile t = tile_of(a.p);
     f32x16 acc[S::FM][S::FN];
     const int64_t m0 = t.m * S::BM, n0 = t.n * S::BN;
-    product<T, S>(a.p, m0, n0, t.split, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int all = a.p.terms * a.p.k_tiles;
+    int k0 = 0, k1 = all;
+    if (t.split >= 0) {
+        k0 = (int)((int64_t)all * t.split / a.p.splits);
+        k1 = (int)((int64_t)all * (t.split + 1) / a.p.splits);
+    }
+    product<T, S, TA, TB>(a.p, lds, m0, n0, k0, k1, acc);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
+    if (t.split >= 0) {
+        float *slab = a.slabs + ((int64_t)(t.id - a.p.full) * a.p.splits + t.split) * (S::BM * S::BN);
 #pragma unroll
-    for (int j = 0; j < S::FN; j++) {
-        const int64_t n = n0 + wn + j * 32 + (lane & 31);
-        if (n >= a.N) continue;
-        const float cf = a.slabs ? 1.f : col_factor(a, n);
+        for (int j = 0; j < S::FN; j++)
 #pragma unroll
-        for (int i = 0; i < S::FM; i++)
+            for (int i = 0; i < S::FM; i++)
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                const int64_t m = m0 + wm + i * 32 + block_row(e, lane);
-                if (m >= a.M) continue;
-                if (a.slabs) {
-                    float *o = a.slabs + ((int64_t)t.split * a.M + m) * a.N + n;
-                    *o = a.add ? *o + acc[i][j][e] : acc[i][j][e];
-                } else {
-                    const float f = row_factor(a, m);
-                    // a row without a target is zero whatever the weights hold
-                    const float c = a.row_up && f == 0.f ? 0.f : acc[i][j][e] * (f * cf);
-                    ((Out *)a.out)[m * a.ld_out + n] = (Out)c;
-                }
+                for (int e = 0; e < 16; e++)
+                    slab[(wm + i * 32 + block_row(e, lane)) * S::BN + wn + j * 32 + (lane & 31)] = acc[i][j][e];
+        return;
+    }
+    const Factor factor(a);
+#pragma unroll
+    for (int i = 0; i < S::FM; i++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+            const int64_t m = m0 + wm + i * 32 + block_row(e, lane);
+            if (m >= a.M) continue;
+#pragma unroll
+            for (int j = 0; j < S::FN; j++) {
+                const int64_t n = n0 + wn + j * 32 + (lane & 31);
+                if (n >= a.N) continue;
+                const float c = acc[i][j][e];
+                if (a.sum) {
+                    float *o = a.sum + m * a.N + n;
+                    *o = a.add ? *o + c : c;
+                } else ((Out *)a.out)[m * a.ld_out + n] = (Out)factor.of(c, m);
             }
+        }
+}
+
+// The tiles that were cut along K: their slabs, added up in order.
+template <class S, class Out> __global__ __launch_bounds__(256) void k_slabs(StoreArgs a)
+{
+    ProductArgs p = a.p;
+    // the tile's place, as tile_of gives it
+    const int id = p.full + blockIdx.x;
+    const int band = kGroup * p.n_tiles, g = id / band, rows = min(kGroup, p.m_tiles - g * kGroup);
+    const int in = id - g * band;
+    const int64_t m0 = (int64_t)(g * kGroup + in % rows) * S::BM, n0 = (int64_t)(in / rows) * S::BN;
+    const float *slab = a.slabs + (int64_t)blockIdx.x * p.splits * (S::BM * S::BN);
+    const Factor factor(a);
+    constexpr int ROWS = 16;  // of one workgroup
+#pragma unroll 4
+    for (int k = threadIdx.x; k < ROWS * S::BN; k += 256) {
+        const int r = blockIdx.y * ROWS + k / S::BN, c = k % S::BN;
+        const int64_t m = m0 + r, n = n0 + c;
+        if (m >= a.M || n >= a.N) continue;
+        float s = 0.f;
+        for (int q = 0; q < p.splits; q++) s += slab[(int64_t)q * (S::BM * S::BN) + r * S::BN + c];
+        if (a.sum) {
+            float *o = a.sum + m * a.N + n;
+            *o = a.add ? *o + s : s;
+        } else ((Out *)a.out)[m * a.ld_out + n] = (Out)factor.of(s, m);
     }
 }
 
+// out = factor(row) sum; zeros without a sum.
 template <class Out> __global__ __launch_bounds__(256) void k_finish(StoreArgs a)
 {
     const int64_t n = (int64_t)blockIdx.y * 256 + threadIdx.x, m = blockIdx.x;
+    const Factor factor(a);
     if (n >= a.N) return;
-    float s = 0.f;
-    for (int k = 0; k < a.p.splits; k++) s += a.slabs[((int64_t)k * a.M + m) * a.N + n];
-    const float f = row_factor(a, m);
-    ((Out *)a.out)[m * a.ld_out + n] = (Out)(a.row_up && f == 0.f ? 0.f : s * (f * col_factor(a, n)));
+    ((Out *)a.out)[m * a.ld_out + n] = (Out)(a.sum ? factor.of(a.sum[m * a.N + n], m) : 0.f);
 }
 
 // ------------------------------------------------------------ laying out
-// dst [parts][rows, kp] from src [rows, D]: zeros past D; in two parts with a
-// scale per row. One wavefront per row.
-template <class In, class T, bool TWO>
-__global__ __launch_bounds__(256) void k_pack(const In *src, int64_t ld, int64_t rows, int64_t D, T *dst, int64_t kp,
-                                             int64_t part, float *scale)
+// Partial maxima of the finite magnitudes of src [rows, D].
+__global__ __launch_bounds__(1024) void k_max(const float *src, int64_t ld, int64_t rows, int64_t D, float *part)
+{
+    __shared__ float red[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float top = 0.f;
+    for (int64_t r = (int64_t)blockIdx.x * 16 + wave; r < rows; r += kMaxParts * 16)
+        for (int64_t c = lane * 4; c < D; c += 256) {
+            float f[4];
+            load_part<4>(src + r * ld + c, (int)min((int64_t)4, D - c), f);
+#pragma unroll
+            for (int j = 0; j < 4; j++) top = fabsf(f[j]) < INFINITY ? fmaxf(top, fabsf(f[j])) : top;
+        }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    if (lane == 0) red[wave] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 0; w < 16; w++) top = fmaxf(top, red[w]);
+        part[blockIdx.x] = top;
+    }
+}
+
+struct PackArgs {
+    const void *src;
+    int64_t ld, rows, D;
+    void *dst;          // [parts][rows, kp], zeros past D
+    int64_t kp, part;
+    float *scale;       // fp32: a power of two per row; written unless `all` alone is wanted
+    void *all;          // fp32: a second copy with the scale of the maximum in w_max
+    const float *w_max;
+    // dst for dweight's product: zeros for rows without a target, other rows
+    // times 2^(e - *e_max), e the exponent of the row's up and scale
+    const uint64_t *targets;
+    int64_t V;
+    const float *up;
+    const int *e_max;
+};
+
+// One wavefront per row.
+template <class In, class T, bool TWO> __global__ __launch_bounds__(256) void k_pack(PackArgs a)
 {
     constexpr int VE = kVec<T>;
     const int lane = threadIdx.x & 63;
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (r >= rows) return;
-    src += r * ld;
-    float inv = 1.f;
+    const float w_max = TWO && a.all ? max_of(a.w_max) : 0.f;
+    if (r >= a.rows) return;
+    const In *src = (const In *)a.src + r * a.ld;
+    int bits = 0, bits_all = 0;
+    bool on = true;
     if constexpr (TWO) {
+        bits_all = -scale_bits(w_max);
         float top = 0.f;
-        for (int64_t c = lane * VE; c < D; c += 64 * VE) {
+        for (int64_t c = lane * VE; c < a.D; c += 64 * VE) {
             float f[VE];
-            load_part<VE>(src + c, (int)min((int64_t)VE, D - c), f);
+            load_part<VE>(src + c, (int)min((int64_t)VE, a.D - c), f);
+            // a row with infinities is NaN in the products, by any scale
 #pragma unroll
             for (int j = 0; j < VE; j++) top = fmaxf(top, fabsf(f[j]));
         }
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-        const float s = scale_of(top);
-        inv = inverse_of(s);
-        if (lane == 0) scale[r] = s;
+        bits = -scale_bits(top);
+        if (a.scale && lane == 0) a.scale[r] = two_to(-bits);
     }
-    for (int64_t c = lane * VE; c < kp; c += 64 * VE) {
-        float f[VE], lo[VE];
-        load_part<VE>(src + (c < D ? c : 0), (int)max((int64_t)0, min((int64_t)VE, D - c)), f);
-        if constexpr (TWO) {
+    if (a.up) {
+        on = a.targets[r] < (uint64_t)a.V;
+        float f;
+        int e;
+        split_up(on ? a.up[r] : 1.f, f, e);
+        // src = m 2^-bits: times 2^e, relative to the largest
+        bits = e - *a.e_max;
+    }
+    for (int64_t c = lane * VE; c < a.kp; c += 64 * VE) {
+        float f[VE], g[VE], lo[VE];
+        const int n = on ? (int)max((int64_t)0, min((int64_t)VE, a.D - c)) : 0;
+        load_part<VE>(src + (n ? c : 0), n, f);
+        T *dst = (T *)a.dst + r * a.kp + c;
 #pragma unroll
-            for (int j = 0; j < VE; j++) {
-                f[j] *= inv;
-                lo[j] = f[j] - (float)(T)f[j];
+        for (int j = 0; j < VE; j++) {
+            g[j] = TWO || a.up ? ldexpf(f[j], bits) : f[j];
+            if (TWO) lo[j] = g[j] - (float)(T)g[j];
+        }
+        store_vec<VE>(dst, g);
+        if constexpr (TWO) {
+            store_vec<VE>(dst + a.part, lo);
+            if (a.all) {
+                T *all = (T *)a.all + r * a.kp + c;
+#pragma unroll
+                for (int j = 0; j < VE; j++) {
+                    g[j] = ldexpf(f[j], bits_all);
+                    lo[j] = g[j] - (float)(T)g[j];
+                }
+                store_vec<VE>(all, g);
+                store_vec<VE>(all + a.part, lo);
             }
-            store_vec<VE>(dst + part + r * kp + c, lo);
         }
-        store_vec<VE>(dst + r * kp + c, f);
     }
 }
 
-// col_max[d] = max over rows (with a target, if targets are given) of |src[r, d]|.
-constexpr int kTile = 64;
-__global__ __launch_bounds__(256) void k_col_max(const float *src, int64_t ld, int64_t rows, int64_t D,
-                                                const uint64_t *targets, int64_t V, uint32_t *col_max)
+// e_max: the largest exponent of |up| (times the row's scale) over the rows with
+// a target whose up is finite and not zero; -(13 bits of scale) included.
+__global__ __launch_bounds__(1024) void k_up_max(const float *up, const uint64_t *targets, const float *scale, int64_t N,
+                                                int64_t V, int *e_max)
 {
-    const int64_t d = (int64_t)blockIdx.y * 64 + (threadIdx.x & 63);
-    const int64_t r0 = (int64_t)blockIdx.x * 256 + (threadIdx.x >> 6) * 64, r1 = min(r0 + 64, rows);
-    if (d >= D) return;
-    uint32_t top = 0;
-    for (int64_t r = r0; r < r1; r++)
-        if (!targets || targets[r] < (uint64_t)V) top = max(top, __float_as_uint(src[r * ld + d]) & 0x7fffffffu);
-    // bits of magnitudes order like the magnitudes, NaN above all
-    if (top) atomicMax(&col_max[d], top);
-}
-
-__global__ __launch_bounds__(256) void k_zero(uint32_t *p, int64_t n)
-{
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) p[i] = 0;
-}
-
-// dst [parts][D, rp] = src^T, zeros for rows without a target (if targets are
-// given) and for places past `rows`.
-template <class In, class T, bool TWO>
-__global__ __launch_bounds__(256) void k_pack_t(const In *src, int64_t ld, int64_t rows, int64_t D,
-                                               const uint64_t *targets, int64_t V, T *dst, int64_t rp, int64_t part,
-                                               const float *col_max)
-{
-    __shared__ float tile[kTile][kTile + 1];
-    const int64_t r0 = (int64_t)blockIdx.x * kTile, d0 = (int64_t)blockIdx.y * kTile;
-    for (int k = threadIdx.x; k < kTile * kTile; k += 256) {
-        const int64_t r = r0 + k / kTile, d = d0 + k % kTile;
-        const bool in = r < rows && d < D && (!targets || targets[r] < (uint64_t)V);
-        tile[k / kTile][k % kTile] = in ? (float)src[r * ld + d] : 0.f;
+    __shared__ int red[16];
+    int top = -1000;
+    for (int64_t i = threadIdx.x; i < N; i += 1024) {
+        float f;
+        int e;
+        const float u = up[i];
+        if (targets[i] >= (uint64_t)V || u == 0.f || !(fabsf(u) < INFINITY)) continue;
+        split_up(u, f, e);
+        if (scale) e += (int)((__float_as_uint(scale[i]) >> 23) & 255) - 127;
+        top = max(top, e);
     }
-    __syncthreads();
-    for (int k = threadIdx.x; k < kTile * kTile; k += 256) {
-        const int64_t r = r0 + k % kTile, d = d0 + k / kTile;
-        if (d >= D) continue;
-        float f = tile[k % kTile][k / kTile];
-        if constexpr (TWO) {
-            f *= inverse_of(scale_of(col_max[d]));
-            dst[part + d * rp + r] = (T)(f - (float)(T)f);
-        }
-        dst[d * rp + r] = (T)f;
-    }
-}
-
-// The largest |upstream| of a row with a target (at least 1e-30, to divide by).
-__global__ __launch_bounds__(1024) void k_up_max(const float *up, const uint64_t *targets, int64_t N, int64_t V,
-                                                float *out)
-{
-    __shared__ float red[16];
-    float top = 0.f;
-    for (int64_t i = threadIdx.x; i < N; i += 1024)
-        if (targets[i] < (uint64_t)V) top = fmaxf(top, fabsf(up[i]));
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d, 64));
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 0; w < 16; w++) top = fmaxf(top, red[w]);
-        *out = fmaxf(top, 1e-30f);
+        for (int w = 0; w < 16; w++) top = max(top, red[w]);
+        *e_max = top == -1000 ? 0 : top;
     }
 }
 
 // lse and loss of a token from its tiles' maxima and sums. One wavefront each.
-__global__ __launch_bounds__(64) void k_lse(const float2 *part, int tiles, const uint64_t *targets, int64_t V,
-                                           const float *z_target, float *loss, float *lse)
+__global__ __launch_bounds__(256) void k_lse(const float2 *part, int tiles, int64_t N, const uint64_t *targets,
+                                            int64_t V, const float *z_target, float *loss, float *lse)
 {
-    const int64_t n = blockIdx.x;
-    const int lane = threadIdx.x;
+    const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (n >= N) return;
     part += n * tiles;
     float top = -INFINITY;
     for (int k = lane; k < tiles; k += 64) top = fmaxf(top, part[k].x);
@@ -640,72 +843,97 @@ template <class T, int NT> __global__ __launch_bounds__(64 * kFewWaves) void k_f
 int64_t up_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 int64_t ceil_div(int64_t n, int64_t m) { return (n + m - 1) / m; }
 
-// Tiles of 256 x 256 run nearer to the matrix cores' rate, tiles of 128 x 128
-// leave fewer compute units idle when there are few of them.
-bool big_tiles(int64_t M, int64_t N)
-{
-    const int64_t big = ceil_div(M, Big::BM) * ceil_div(N, Big::BN);
-    const int64_t small = ceil_div(M, Small::BM) * ceil_div(N, Small::BN);
-    return ceil_div(big, 256) * 8 <= ceil_div(small, 512) * 5;
-}
-
-struct XentPlan {
-    bool two, grad, few;
-    int elem;
-    int64_t N, V, D, kp, np, vp;
-    int64_t piece;  // words of a piece
-    int max_splits_h, max_splits_w;
-    size_t hp, wp, h_scale, w_scale, wt, ht, w_max, h_max, part, z_target, up_max, prob, prob_t, slab_h, slab_w, bytes;
-
-    static int splits_of(int64_t M, int64_t N, int64_t k_tiles)
+// How C [M, N] is cut into tiles.  Tiles go to the compute units in rounds (256
+// large ones or 512 small ones, two to a compute unit, at a time); the tiles of
+// a last, incomplete round are cut along K (where that is possible) so that
+// they fill it.  The shape with fewer rounds is taken, a round of small tiles
+// counting 5/8 of one of large ones: half the work, at four fifths of the rate.
+struct Cut {
+    bool big;
+    int m_tiles, n_tiles, full, splits, tail;
+    double rounds;
+    template <class S> static Cut of(int64_t M, int64_t N, int64_t k_tiles, bool split)
     {
-        if (M == 0 || N == 0) return 1;
-        const bool big = big_tiles(M, N);
-        const int64_t tiles = big ? ceil_div(M, Big::BM) * ceil_div(N, Big::BN)
-                                  : ceil_div(M, Small::BM) * ceil_div(N, Small::BN);
-        const int64_t slots = big ? 256 : 512;
-        return (int)std::max<int64_t>(1, std::min({slots / tiles, k_tiles / 8, (int64_t)16}));
+        Cut c{};
+        c.big = std::is_same_v<S, Big>;
+        const int slots = c.big ? 256 : 512;
+        c.m_tiles = (int)ceil_div(M, S::BM);
+        c.n_tiles = (int)ceil_div(N, S::BN);
+        const int tiles = c.m_tiles * c.n_tiles;
+        c.tail = tiles % slots;
+        c.splits = 1;
+        if (split && c.tail)
+            c.splits = (int)std::max<int64_t>(1, std::min({(int64_t)(slots / c.tail), k_tiles / 4, (int64_t)16}));
+        c.rounds = tiles / slots + (c.tail ? 1.0 / c.splits + (c.splits > 1 ? 0.1 : 0.0) : 0.0);
+        if (c.splits == 1) c.tail = 0;
+        c.full = tiles - c.tail;
+        if (!c.big) c.rounds *= 0.625;
+        return c;
     }
-
-    XentPlan(int32_t type, int64_t N_, int64_t V_, int64_t D_, bool grad_)
-        : two(type == TQ_F32), grad(grad_), N(N_), V(V_), D(D_)
+    Cut() = default;
+    Cut(int64_t M, int64_t N, int64_t k_tiles, bool split)
     {
-        elem = 2 * (two ? 2 : 1);
-        few = !grad && N <= kFewTokens;
+        const Cut b = of<Big>(M, N, k_tiles, split), s = of<Small>(M, N, k_tiles, split);
+        *this = b.rounds <= s.rounds ? b : s;
+    }
+    int blocks() const { return full + tail * splits; }
+    size_t slab_bytes() const
+    {
+        const size_t tile = big ? Big::BM * Big::BN : Small::BM * Small::BN;
+        return sizeof(float) * tile * tail * splits;
+    }
+    void put(ProductArgs &p) const
+    {
+        p.m_tiles = m_tiles;
+        p.n_tiles = n_tiles;
+        p.full = full;
+        p.splits = splits;
+    }
+};
+
+// Sizes and workspace of a call.
+struct XentPlan {
+    bool two, few;
+    int terms;
+    int64_t N, V, D, kp, np;
+    int64_t piece;  // words of a piece of the vocabulary
+    size_t part, z_target, hp, wp, all, hs, h_scale, w_scale, w_max, e_max, prob, sum, slabs, bytes;
+
+    Cut cut_h(int64_t words) const { return Cut(N, D, terms * (up_to(words, kBK) / kBK), true); }
+    Cut cut_w(int64_t words) const { return Cut(words, D, terms * (np / kBK), true); }
+
+    XentPlan(int32_t type, int64_t N_, int64_t V_, int64_t D_, bool grad)
+        : two(type == TQ_F32), few(!grad && N_ <= kFewTokens), terms(two ? 3 : 1), N(N_), V(V_), D(D_)
+    {
+        const size_t elem = 2 * (two ? 2 : 1);
         kp = std::max<int64_t>(up_to(D, kBK), kBK);
         np = up_to(N, kBK);
-        vp = up_to(V, kBK);
-        // pieces long enough that the products over them fill the chip, short
-        // enough that p takes at most 2^28 elements
-        piece = up_to(V, 256);
-        if (grad && N * piece > ((int64_t)1 << 28))
-            piece = std::max<int64_t>(256, (((int64_t)1 << 28) / std::max<int64_t>(N, 1)) / 256 * 256);
+        // a piece's p takes up to about 2^28 elements
+        const int64_t most = std::max<int64_t>(256, ((int64_t)1 << 28) / std::max<int64_t>(N, 1) / 256 * 256);
+        piece = up_to(ceil_div(V, ceil_div(V, most * 9 / 8)), 256);
         Carver c;
         const int64_t tiles = few ? ceil_div(V, kFewWords) : ceil_div(V, Small::BM);
         part = c.take(sizeof(float2) * N * tiles);
         z_target = c.take(sizeof(float) * N);
-        if (few) {
-            bytes = c.used;
-            return;
+        if (!few && N) {
+            hp = c.take(elem * N * kp);
+            wp = c.take(elem * V * kp);
+            h_scale = c.take(two ? sizeof(float) * N : 0);
+            w_scale = c.take(two ? sizeof(float) * up_to(V, 256) : 0);
         }
-        hp = c.take((size_t)elem * N * kp);
-        wp = c.take((size_t)elem * V * kp);
-        h_scale = c.take(two ? sizeof(float) * N : 0);
-        w_scale = c.take(two ? sizeof(float) * V : 0);
-        if (grad) {
-            const int64_t words = std::min(piece, vp);
-            wt = c.take((size_t)elem * D * vp);
-            ht = c.take((size_t)elem * D * np);
-            w_max = c.take(two ? sizeof(float) * D : 0);
-            h_max = c.take(two ? sizeof(float) * D : 0);
-            up_max = c.take(sizeof(float));
-            prob = c.take((size_t)elem * N * words);
-            prob_t = c.take((size_t)elem * words * np);
-            const int terms = two ? 3 : 1;
-            max_splits_h = splits_of(N, D, terms * (words / kBK));
-            max_splits_w = splits_of(words, D, terms * (np / kBK));
-            slab_h = c.take(sizeof(float) * max_splits_h * N * D);
-            slab_w = c.take(max_splits_w > 1 ? sizeof(float) * max_splits_w * words * D : 0);
+        if (grad && N) {
+            const int64_t words = std::min(piece, up_to(V, kBK));
+            all = c.take(two ? elem * V * kp : 0);
+            w_max = c.take(sizeof(float) * kMaxParts);
+            e_max = c.take(sizeof(int));
+            hs = c.take(elem * N * kp);
+            prob = c.take(elem * np * words);
+            sum = c.take(piece < V ? sizeof(float) * N * D : 0);
+            size_t s = 0;
+            if (D)
+                for (int64_t w : {std::min(piece, V), V - (V - 1) / piece * piece})
+                    s = std::max({s, cut_h(w).slab_bytes(), cut_w(w).slab_bytes()});
+            slabs = c.take(s);
         }
         bytes = c.used;
     }
@@ -717,24 +945,30 @@ bool in_place(const void *p, int64_t ld, int64_t D)
     return D % kBK == 0 && D > 0 && ld % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
 }
 
-template <class T, class S, bool GRAD, bool TWO> void run_logits(LogitArgs a, hipStream_t s)
+template <class T, bool GRAD, bool TWO> int run_logits(LogitArgs a, int64_t tokens, hipStream_t s)
 {
-    a.p.m_tiles = (int)ceil_div(a.p.a.rows, S::BM);
-    a.p.n_tiles = (int)ceil_div(GRAD ? a.ld_prob_t : a.N, S::BN);
-    a.p.splits = 1;
-    k_logits<T, S, GRAD, TWO><<<(unsigned)(a.p.m_tiles * a.p.n_tiles), S::threads, 0, s>>>(a);
+    const Cut c(a.p.a.extent, tokens, a.p.terms * a.p.k_tiles, false);
+    c.put(a.p);
+    if (c.big) k_logits<T, Big, GRAD, TWO><<<(unsigned)c.blocks(), Big::threads, 0, s>>>(a);
+    else k_logits<T, Small, GRAD, TWO><<<(unsigned)c.blocks(), Small::threads, 0, s>>>(a);
+    return c.m_tiles;
 }
 
-template <class T, class Out> void run_product(StoreArgs a, bool big, hipStream_t s)
+template <class T, bool TA, class Out> void run_product(StoreArgs a, const Cut &c, hipStream_t s)
 {
+    c.put(a.p);
     auto go = [&](auto shape) {
         using S = decltype(shape);
-        a.p.m_tiles = (int)ceil_div(a.M, S::BM);
-        a.p.n_tiles = (int)ceil_div(a.N, S::BN);
-        k_product<T, S, Out><<<(unsigned)(a.p.m_tiles * a.p.n_tiles * a.p.splits), S::threads, 0, s>>>(a);
+        k_product<T, S, TA, true, Out><<<(unsigned)c.blocks(), S::threads, 0, s>>>(a);
+        if (c.tail) k_slabs<S, Out><<<dim3((unsigned)c.tail, S::BM / 16), 256, 0, s>>>(a);
     };
-    if (big) go(Big{});
+    if (c.big) go(Big{});
     else go(Small{});
+}
+
+template <class Out> void run_finish(const StoreArgs &a, hipStream_t s)
+{
+    k_finish<Out><<<dim3((unsigned)a.M, (unsigned)ceil_div(a.N, 256)), 256, 0, s>>>(a);
 }
 
 // In: type of the arrays; T: of the products' operands; TWO: in two parts.
@@ -744,143 +978,114 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     char *ws = (char *)a.ws;
     float2 *part = (float2 *)(ws + p.part);
     float *z_target = (float *)(ws + p.z_target);
-    int tiles;
+    const unsigned token_blocks = (unsigned)ceil_div(a.N, 4);
     if (p.few) {
         const FewArgs f{a.hidden, a.weight, a.ld_hidden, a.ld_weight, a.N, a.V, a.D, a.targets, part, z_target};
-        tiles = (int)ceil_div(a.V, kFewWords);
+        const int tiles = (int)ceil_div(a.V, kFewWords);
         if (a.N <= 16) k_few<In, 1><<<tiles, 64 * kFewWaves, 0, s>>>(f);
         else if (a.N <= 32) k_few<In, 2><<<tiles, 64 * kFewWaves, 0, s>>>(f);
         else k_few<In, 4><<<tiles, 64 * kFewWaves, 0, s>>>(f);
-        k_lse<<<(unsigned)a.N, 64, 0, s>>>(part, tiles, a.targets, a.V, z_target, a.loss, a.lse);
+        k_lse<<<token_blocks, 256, 0, s>>>(part, tiles, a.N, a.targets, a.V, z_target, a.loss, a.lse);
         return hipGetLastError();
     }
-    if (a.N) {
-        const bool h_direct = !TWO && in_place(a.hidden, a.ld_hidden, a.D);
-        const bool w_direct = !TWO && in_place(a.weight, a.ld_weight, a.D);
-        float *h_scale = (float *)(ws + p.h_scale), *w_scale = (float *)(ws + p.w_scale);
-        Operand h{ws + p.hp, p.kp, a.N * p.kp, a.N}, w{ws + p.wp, p.kp, a.V * p.kp, a.V};
-        if (h_direct) h.p = a.hidden, h.ld = a.ld_hidden;
-        else
-            k_pack<In, T, TWO><<<(unsigned)ceil_div(a.N, 4), 256, 0, s>>>((const In *)a.hidden, a.ld_hidden, a.N, a.D,
-                                                                        (T *)h.p, p.kp, h.part, h_scale);
-        if (w_direct) w.p = a.weight, w.ld = a.ld_weight;
-        else
-            k_pack<In, T, TWO><<<(unsigned)ceil_div(a.V, 4), 256, 0, s>>>((const In *)a.weight, a.ld_weight, a.V, a.D,
-                                                                        (T *)w.p, p.kp, w.part, w_scale);
-        const int terms = TWO ? 3 : 1;
-        LogitArgs l{};
-        l.p.a = w;
-        l.p.b = h;
-        l.p.terms = terms;
-        l.p.k_tiles = (int)(p.kp / kBK);
-        l.word_scale = w_scale;
-        l.token_scale = h_scale;
-        l.targets = a.targets;
-        l.V = a.V;
-        l.N = a.N;
-        l.part = part;
-        l.z_target = z_target;
-        if (big_tiles(a.V, a.N)) {
-            run_logits<T, Big, false, TWO>(l, s);
-            tiles = (int)ceil_div(a.V, Big::BM);
-        } else {
-            run_logits<T, Small, false, TWO>(l, s);
-            tiles = (int)ceil_div(a.V, Small::BM);
-        }
-        k_lse<<<(unsigned)a.N, 64, 0, s>>>(part, tiles, a.targets, a.V, z_target, a.loss, a.lse);
-        if (!grad) return hipGetLastError();
-        float *up_max = (float *)(ws + p.up_max);
-        k_up_max<<<1, 1024, 0, s>>>(a.upstream, a.targets, a.N, a.V, up_max);
-        if (a.D == 0) return hipGetLastError();
-        // the operands that run along words and along tokens
-        T *wt = (T *)(ws + p.wt), *ht = (T *)(ws + p.ht);
-        float *w_max = (float *)(ws + p.w_max), *h_max = (float *)(ws + p.h_max);
-        if constexpr (TWO) {
-            k_zero<<<(unsigned)ceil_div(a.D, 256), 256, 0, s>>>((uint32_t *)w_max, a.D);
-            k_zero<<<(unsigned)ceil_div(a.D, 256), 256, 0, s>>>((uint32_t *)h_max, a.D);
-            k_col_max<<<dim3((unsigned)ceil_div(a.V, 256), (unsigned)ceil_div(a.D, 64)), 256, 0, s>>>(
-                (const float *)a.weight, a.ld_weight, a.V, a.D, nullptr, a.V, (uint32_t *)w_max);
-            k_col_max<<<dim3((unsigned)ceil_div(a.N, 256), (unsigned)ceil_div(a.D, 64)), 256, 0, s>>>(
-                (const float *)a.hidden, a.ld_hidden, a.N, a.D, a.targets, a.V, (uint32_t *)h_max);
-        }
-        k_pack_t<In, T, TWO><<<dim3((unsigned)(p.vp / kTile), (unsigned)ceil_div(a.D, kTile)), 256, 0, s>>>(
-            (const In *)a.weight, a.ld_weight, a.V, a.D, nullptr, a.V, wt, p.vp, a.D * p.vp, w_max);
-        k_pack_t<In, T, TWO><<<dim3((unsigned)(p.np / kTile), (unsigned)ceil_div(a.D, kTile)), 256, 0, s>>>(
-            (const In *)a.hidden, a.ld_hidden, a.N, a.D, a.targets, a.V, ht, p.np, a.D * p.np, h_max);
-        T *prob = (T *)(ws + p.prob), *prob_t = (T *)(ws + p.prob_t);
-        float *slab_h = (float *)(ws + p.slab_h), *slab_w = (float *)(ws + p.slab_w);
-        const bool big_h = big_tiles(a.N, a.D);
-        int splits_h = 1;
-        for (int64_t v0 = 0; v0 < a.V; v0 += p.piece) {
-            const int64_t words = std::min(p.piece, a.V - v0), kv = up_to(words, kBK);
-            l.p.a.p = (const T *)w.p + v0 * w.ld;
-            l.p.a.rows = words;
-            l.word_scale = w_scale + v0;
-            l.v_base = v0;
-            l.lse = a.lse;
-            l.up = a.upstream;
-            l.up_max = up_max;
-            l.prob = prob;
-            l.ld_prob = kv;
-            l.prob_part = a.N * kv;
-            l.prob_t = prob_t;
-            l.ld_prob_t = p.np;
-            l.prob_t_part = words * p.np;
-            if (big_tiles(words, a.N)) run_logits<T, Big, true, TWO>(l, s);
-            else run_logits<T, Small, true, TWO>(l, s);
-            StoreArgs d{};
-            d.p.a = Operand{prob, kv, l.prob_part, a.N};
-            d.p.b = Operand{wt + v0, p.vp, a.D * p.vp, a.D};
-            d.p.terms = terms;
-            d.p.k_tiles = (int)(kv / kBK);
-            if (v0 == 0) splits_h = std::min(p.max_splits_h, XentPlan::splits_of(a.N, a.D, terms * (kv / kBK)));
-            d.p.splits = splits_h;
-            d.M = a.N;
-            d.N = a.D;
-            d.slabs = slab_h;
-            d.add = v0 > 0;
-            run_product<T, In>(d, big_h, s);
-            StoreArgs e{};
-            e.p.a = Operand{prob_t, p.np, l.prob_t_part, words};
-            e.p.b = Operand{ht, p.np, a.D * p.np, a.D};
-            e.p.terms = terms;
-            e.p.k_tiles = (int)(p.np / kBK);
-            e.p.splits = std::min(p.max_splits_w, XentPlan::splits_of(words, a.D, terms * (p.np / kBK)));
-            e.M = words;
-            e.N = a.D;
-            e.out = (In *)a.dweight + v0 * a.ld_dweight;
-            e.ld_out = a.ld_dweight;
-            e.col_max = TWO ? h_max : nullptr;
-            e.up_max = up_max;
-            if (e.p.splits > 1) e.slabs = slab_w;
-            run_product<T, In>(e, big_tiles(words, a.D), s);
-            if (e.slabs)
-                k_finish<In><<<dim3((unsigned)words, (unsigned)ceil_div(a.D, 256)), 256, 0, s>>>(e);
-        }
-        StoreArgs f{};
-        f.p.splits = splits_h;
-        f.M = a.N;
-        f.N = a.D;
-        f.slabs = slab_h;
-        f.out = a.dhidden;
-        f.ld_out = a.ld_dhidden;
-        f.row_up = a.upstream;
-        f.targets = a.targets;
-        f.V = a.V;
-        f.col_max = TWO ? w_max : nullptr;
-        k_finish<In><<<dim3((unsigned)a.N, (unsigned)ceil_div(a.D, 256)), 256, 0, s>>>(f);
-        return hipGetLastError();
-    }
-    // no tokens: no gradient
-    if (a.D)
-        for (int64_t v = 0; v < a.V; v += 1 << 20) {
+    if (a.N == 0) {
+        // no tokens: no gradient
+        for (int64_t v = 0; a.D && v < a.V; v += 1 << 20) {
             StoreArgs e{};
             e.M = std::min<int64_t>(a.V - v, 1 << 20);
             e.N = a.D;
             e.out = (In *)a.dweight + v * a.ld_dweight;
             e.ld_out = a.ld_dweight;
-            k_finish<In><<<dim3((unsigned)e.M, (unsigned)ceil_div(a.D, 256)), 256, 0, s>>>(e);
+            run_finish<In>(e, s);
         }
+        return hipGetLastError();
+    }
+    float *h_scale = (float *)(ws + p.h_scale), *w_scale = (float *)(ws + p.w_scale), *w_max = (float *)(ws + p.w_max);
+    Operand h{ws + p.hp, p.kp, a.N * p.kp, a.N, 0}, w{ws + p.wp, p.kp, a.V * p.kp, a.V, 0};
+    Operand w_all = w;  // for dhidden's product
+    if (TWO && grad) {
+        k_max<<<kMaxParts, 1024, 0, s>>>((const float *)a.weight, a.ld_weight, a.V, a.D, w_max);
+        w_all.p = ws + p.all;
+    }
+    PackArgs k{};
+    k.D = a.D;
+    k.kp = p.kp;
+    if (!TWO && in_place(a.hidden, a.ld_hidden, a.D)) h.p = a.hidden, h.ld = a.ld_hidden;
+    else {
+        k.src = a.hidden, k.ld = a.ld_hidden, k.rows = a.N;
+        k.dst = ws + p.hp, k.part = h.part, k.scale = h_scale;
+        k_pack<In, T, TWO><<<token_blocks, 256, 0, s>>>(k);
+    }
+    if (!TWO && in_place(a.weight, a.ld_weight, a.D)) w.p = a.weight, w.ld = a.ld_weight;
+    else {
+        k.src = a.weight, k.ld = a.ld_weight, k.rows = a.V;
+        k.dst = ws + p.wp, k.part = w.part, k.scale = w_scale;
+        if (TWO && grad) k.all = ws + p.all, k.w_max = w_max;
+        k_pack<In, T, TWO><<<(unsigned)ceil_div(a.V, 4), 256, 0, s>>>(k);
+    }
+    if (!TWO) w_all = w;
+    LogitArgs l{};
+    l.p.a = w;
+    l.p.b = h;
+    l.p.terms = p.terms;
+    l.p.k_tiles = (int)(p.kp / kBK);
+    l.word_scale = w_scale;
+    l.token_scale = h_scale;
+    l.targets = a.targets;
+    l.V = a.V;
+    l.N = a.N;
+    l.part = part;
+    l.z_target = z_target;
+    const int tiles = run_logits<T, false, TWO>(l, a.N, s);
+    k_lse<<<token_blocks, 256, 0, s>>>(part, tiles, a.N, a.targets, a.V, z_target, a.loss, a.lse);
+    if (!grad || a.D == 0) return hipGetLastError();
+
+    int *e_max = (int *)(ws + p.e_max);
+    k_up_max<<<1, 1024, 0, s>>>(a.upstream, a.targets, TWO ? h_scale : nullptr, a.N, a.V, e_max);
+    const Operand hs{ws + p.hs, p.kp, a.N * p.kp, p.kp, a.N};
+    PackArgs u{};
+    u.src = a.hidden, u.ld = a.ld_hidden, u.rows = a.N, u.D = a.D;
+    u.dst = ws + p.hs, u.kp = p.kp, u.part = hs.part;
+    u.targets = a.targets, u.V = a.V, u.up = a.upstream, u.e_max = e_max;
+    k_pack<In, T, TWO><<<token_blocks, 256, 0, s>>>(u);
+    StoreArgs d{};  // dhidden
+    d.M = a.N, d.N = a.D;
+    d.slabs = (float *)(ws + p.slabs);
+    d.sum = p.piece < a.V ? (float *)(ws + p.sum) : nullptr;
+    d.out = a.dhidden, d.ld_out = a.ld_dhidden;
+    d.up = a.upstream, d.targets = a.targets, d.V = a.V;
+    d.w_max = TWO ? w_max : nullptr;
+    for (int64_t v0 = 0; v0 < a.V; v0 += p.piece) {
+        const int64_t words = std::min(p.piece, a.V - v0), kv = up_to(words, kBK);
+        l.p.a.p = (const T *)w.p + v0 * w.ld;
+        l.p.a.extent = words;
+        l.word_scale = w_scale + v0;
+        l.v_base = v0;
+        l.lse = a.lse;
+        l.up = a.upstream;
+        l.prob = ws + p.prob;
+        l.ld_prob = kv;
+        l.prob_rows = p.np;
+        l.prob_part = p.np * kv;
+        run_logits<T, true, TWO>(l, p.np, s);
+        d.p.a = Operand{ws + p.prob, kv, l.prob_part, a.N, 0};
+        d.p.b = Operand{(const T *)w_all.p + v0 * w_all.ld, w_all.ld, w_all.part, TWO || w_all.ld == p.kp ? p.kp : a.D, words};
+        d.p.terms = p.terms;
+        d.p.k_tiles = (int)(kv / kBK);
+        d.add = v0 > 0;
+        run_product<T, false, In>(d, p.cut_h(words), s);
+        StoreArgs e{};  // dweight
+        e.M = words, e.N = a.D;
+        e.slabs = d.slabs;
+        e.out = (In *)a.dweight + v0 * a.ld_dweight, e.ld_out = a.ld_dweight;
+        e.e_max = e_max;
+        e.p.a = Operand{ws + p.prob, kv, l.prob_part, kv, p.np};
+        e.p.b = hs;
+        e.p.terms = p.terms;
+        e.p.k_tiles = (int)(p.np / kBK);
+        run_product<T, true, In>(e, p.cut_w(words), s);
+    }
+    if (d.sum) run_finish<In>(d, s);
     return hipGetLastError();
 }
 
