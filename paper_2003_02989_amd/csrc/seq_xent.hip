@@ -264,6 +264,11 @@ __device__ __forceinline__ void split_up(float up, float &f, int &e)
     f = ldexpf(up, -e);
 }
 
+// exp(z - r) from z and r log2 e, with one rounding of the exponent; that of
+// r log2 e, up to |r| 2^-23, is common to a row and of the order of lse's own.
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ __forceinline__ float exp_less(float z, float r2) { return __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -r2)); }
+
 // ------------------------------------------------------------ the logits
 // A = weight (rows: words), B = hidden (rows: tokens): a lane's registers hold
 // words of one token, so that sums over words stay within a lane until the end.
@@ -316,26 +321,40 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
             const int64_t n = n0 + wn + j * 32 + (lane & 31);
             const uint64_t target = n < a.N ? a.targets[n] : ~(uint64_t)0;
             const int hit = target < (uint64_t)a.V ? (int)target - v0 : -1;
-            float top = -INFINITY, zt = 0.f;
-            bool found = false;
+            // few tiles hold a target of theirs, or the end of the vocabulary
+            if (__any(hit >= 0 && hit < S::FM * 32)) {
+                float zt = 0.f;
+#pragma unroll
+                for (int i = 0; i < S::FM; i++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++)
+                        if (i * 32 + block_row(e, lane) == hit) zt = acc[i][j][e];
+                // the target's word is in one of the two lanes of a token
+                if (hit >= 0 && hit < S::FM * 32 && ((hit >> 2) & 1) == lane >> 5) a.z_target[n] = zt;
+            }
+            if (words < S::FM * 32)
+#pragma unroll
+                for (int i = 0; i < S::FM; i++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++)
+                        if (i * 32 + block_row(e, lane) >= words) acc[i][j][e] = -INFINITY;
+            // four at a time: no long chain of dependent operations
+            float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int i = 0; i < S::FM; i++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) {
-                    const int w = i * 32 + block_row(e, lane);
-                    if (w == hit) zt = acc[i][j][e], found = true;
-                    if (w >= words) acc[i][j][e] = -INFINITY;
-                    top = fmaxf(top, acc[i][j][e]);
-                }
-            if (found) a.z_target[n] = zt;
+                for (int e = 0; e < 16; e++) top4[e & 3] = fmaxf(top4[e & 3], acc[i][j][e]);
+            float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             // without words there is nothing to add; NaN stays in the sum
             const float ref = top == -INFINITY ? 0.f : top;
-            float sum = 0.f;
+            const float ref2 = ref * kLog2e;
+            float sum4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < S::FM; i++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) sum += __expf(acc[i][j][e] - ref);
+                for (int e = 0; e < 16; e++) sum4[e & 3] += exp_less(acc[i][j][e], ref2);
+            float sum = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
             sum += __shfl_xor(sum, 32, 64);
             if (lane < 32) join[wave / S::WN][wn + j * 32 + lane] = make_float2(top, sum);
         }
@@ -362,16 +381,30 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
             int e2;
             if (on) split_up(a.up[n], f, e2);
             f *= (float)(1 << kProbBits);
-            const int last = on ? words : 0;
+            const float lse2 = lse * kLog2e;
+            const bool some = __any(hit >= 0);
 #pragma unroll
             for (int i = 0; i < S::FM; i++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) {
-                    const int w = i * 32 + block_row(e, lane);
-                    float p = __expf(acc[i][j][e] - lse);
-                    if (w == hit) p -= 1.f;
-                    acc[i][j][e] = w < last ? p * f : 0.f;
-                }
+                for (int e = 0; e < 16; e++) acc[i][j][e] = exp_less(acc[i][j][e], lse2);
+            if (some)
+#pragma unroll
+                for (int i = 0; i < S::FM; i++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++)
+                        if (i * 32 + block_row(e, lane) == hit) acc[i][j][e] -= 1.f;
+#pragma unroll
+            for (int i = 0; i < S::FM; i++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) acc[i][j][e] *= f;
+            // what is not a word of a token with a target is zero, whatever it holds
+            const int last = on ? words : 0;
+            if (__any(last < S::FM * 32))
+#pragma unroll
+                for (int i = 0; i < S::FM; i++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++)
+                        if (i * 32 + block_row(e, lane) >= last) acc[i][j][e] = 0.f;
         }
         // Each wavefront turns its words x tokens through LDS (the stages are done
         // with), tokens as rows, 16-byte pieces in the order piece ^ token, and
@@ -537,18 +570,20 @@ template <class S, class Out> __global__ __launch_bounds__(256) void k_slabs(Sto
     const int64_t m0 = (int64_t)(g * kGroup + in % rows) * S::BM, n0 = (int64_t)(in / rows) * S::BN;
     const float *slab = a.slabs + (int64_t)blockIdx.x * p.splits * (S::BM * S::BN);
     const Factor factor(a);
-    constexpr int ROWS = 16;  // of one workgroup
+    // four columns per thread
+    const int at = (blockIdx.y * 256 + threadIdx.x) * 4, r = at / S::BN, c = at % S::BN;
+    const int64_t m = m0 + r, n = n0 + c;
+    if (m >= a.M) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int k = threadIdx.x; k < ROWS * S::BN; k += 256) {
-        const int r = blockIdx.y * ROWS + k / S::BN, c = k % S::BN;
-        const int64_t m = m0 + r, n = n0 + c;
-        if (m >= a.M || n >= a.N) continue;
-        float s = 0.f;
-        for (int q = 0; q < p.splits; q++) s += slab[(int64_t)q * (S::BM * S::BN) + r * S::BN + c];
+    for (int q = 0; q < p.splits; q++) s += *(const f32x4 *)(slab + (int64_t)q * (S::BM * S::BN) + at);
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        if (n + j >= a.N) break;
         if (a.sum) {
-            float *o = a.sum + m * a.N + n;
-            *o = a.add ? *o + s : s;
-        } else ((Out *)a.out)[m * a.ld_out + n] = (Out)factor.of(s, m);
+            float *o = a.sum + m * a.N + n + j;
+            *o = a.add ? *o + s[j] : s[j];
+        } else ((Out *)a.out)[m * a.ld_out + n + j] = (Out)factor.of(s[j], m);
     }
 }
 
@@ -960,7 +995,7 @@ template <class T, bool TA, class Out> void run_product(StoreArgs a, const Cut &
     auto go = [&](auto shape) {
         using S = decltype(shape);
         k_product<T, S, TA, true, Out><<<(unsigned)c.blocks(), S::threads, 0, s>>>(a);
-        if (c.tail) k_slabs<S, Out><<<dim3((unsigned)c.tail, S::BM / 16), 256, 0, s>>>(a);
+        if (c.tail) k_slabs<S, Out><<<dim3((unsigned)c.tail, S::BM * S::BN / 1024), 256, 0, s>>>(a);
     };
     if (c.big) go(Big{});
     else go(Small{});
