@@ -67,7 +67,8 @@ tq_status tq_embed_grad(const void *grad_out, int64_t ld_grad_out, int32_t type,
  * may be NULL; for a single step (T = 1) such calls advance the records'
  * states in place.  states, when not NULL, receives the states that
  * tq_gated_scan_grad starts from: float [B, ceil(T / TQ_SCAN_PIECE), D], the
- * state before step j * TQ_SCAN_PIECE.
+ * state before step j * TQ_SCAN_PIECE (steps past a record's length: not
+ * written).
  * h0, h_last and states are contiguous. */
 #define TQ_SCAN_PIECE 64
 tq_status tq_gated_scan_workspace(int64_t B, int64_t T, int64_t D, size_t *bytes);

@@ -56,6 +56,8 @@ struct ScanArgs {
     const int32_t *lengths;
     void *ws;
 };
+// workgroups of a scan (below 2^31), whatever the type
+int64_t scan_items(int64_t B, int64_t T, int64_t D);
 size_t scan_workspace(int64_t B, int64_t T, int64_t D);
 hipError_t launch_scan(int32_t type, const ScanArgs &a, hipStream_t s);
 hipError_t launch_scan_grad(int32_t type, const ScanArgs &a, hipStream_t s);

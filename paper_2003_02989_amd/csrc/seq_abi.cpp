@@ -77,8 +77,10 @@ void check_scan(const char *call, int type, int64_t B, int64_t T, int64_t D)
     check_size(call, "B", B);
     check_size(call, "T", T);
     check_size(call, "D", D);
-    // one workgroup per 64 channels of a record at least
-    if (B * ((D + 63) / 64) > kMaxIndex) fail(TQ_E_UNSUPPORTED, text(call, "B * ceil(D / 64) must be below 2^31"));
+    // rows x segments of 64 steps, in doubles: the product of three sizes
+    if ((double)B * (double)((D + 63) / 64) * (double)((T + 63) / 64) > kMaxIndex ||
+        scan_items(B, T, D) > kMaxIndex)
+        fail(TQ_E_UNSUPPORTED, text(call, "B * ceil(D / 64) * ceil(T / 64) must be below 2^31"));
 }
 
 } // namespace

@@ -3,20 +3,27 @@
 //   h_t = a_t h_{t-1} + c_t x_t,   a_t = sigmoid(g_t), c_t = 1 - a_t.
 //
 // Each step is the map h -> a h + b; maps compose to (A, B) pairs, so a stretch
-// of time is summed up by one pair per channel.  A workgroup takes one record,
-// 64 lanes' worth of channels and kPiece steps at a time: its wavefronts read
-// kSteps steps each into registers, exchange their pairs through LDS, and then
-// apply their steps to the state they start from, so x and g are read once and y
-// is written once.  The state of the piece's end is carried to the next piece.
-// The backward pass walks the pieces from the last one back: the pairs
-// forwards give h_{t-1} (from the saved state before the piece), and
+// of time is summed up by one pair per channel.  A workgroup takes a segment of
+// time of one record and a slab of channels: its wavefronts read kSteps steps
+// each into registers, exchange their pairs through LDS, find the state the
+// segment starts from and apply their steps to it: x and g are read once and y
+// is written once, which is what bounds it.
+//
+// The state a segment starts from comes from the pairs of the segments before
+// it, which their workgroups publish as soon as they have them, and replace by
+// (0, state at the segment's end) once they know that: looking back from the
+// nearest segment, the composition is complete as soon as A = 0.  A slot of all
+// ones is not published yet.  Workgroups take their segments in the order in which
+// they start (a ticket), earlier segments of all rows first, and wait for
+// segments with lower tickets only; the lowest ticket that is not done waits
+// for nobody, so every wait ends.
+//
+// The backward pass walks time the other way.  Pairs forwards give h_{t-1} from
+// the saved state before the piece of TQ_SCAN_PIECE steps, and
 //   l_t = dy_t + m_{t+1},  m_t = a_t l_t
 // is the same kind of recurrence backwards.
-//
-// With few records and channels the time axis is cut into segments of whole
-// pieces: a first kernel sums each segment up to its pair, a second joins the
-// pairs, and the segments then run side by side.
 #include <algorithm>
+#include <type_traits>
 
 #include "seq.h"
 #include "seq_device.h"
@@ -24,16 +31,23 @@
 namespace tq {
 namespace {
 
-constexpr int kWaves = 8, kSteps = 8, kPiece = kWaves * kSteps;
-constexpr int kThreads = 64 * kWaves;
-static_assert(kPiece == TQ_SCAN_PIECE, "states are kept per piece");
-
+// K: element type and channels per lane (16-bit elements of wide rows: two, 32
+// bits of a row).
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+template <class T_, int CV_> struct Kind {
+    using T = T_;
+    static constexpr int CV = CV_;
+    static constexpr int steps = 16 / CV, seg = kWaves * steps, slab = 64 * CV;
+    static_assert(seg % TQ_SCAN_PIECE == 0 && TQ_SCAN_PIECE % steps == 0,
+                  "segments start at pieces, wavefronts at pieces or inside them");
+};
+constexpr int kPiece = TQ_SCAN_PIECE;
 // exp(-v), v >= 0.  The product with log2 e is rounded, an error of up to
 // v 2^-24 relative; for fp32 inputs what the rounding lost is put back.
 template <class T> __device__ __forceinline__ float exp_neg(float v)
 {
     constexpr float kLog2e = 1.44269504088896341f;
-    if constexpr (sizeof(T) == 4) v = fminf(v, 1e4f);  // infinities have no remainder
+    if constexpr (sizeof(T) == 4) v = v > 1e4f ? 1e4f : v;  // infinities have no remainder; NaN stays
     const float t = -v * kLog2e;
     float e = __builtin_amdgcn_exp2f(t);
     if constexpr (sizeof(T) == 4) {
@@ -51,378 +65,429 @@ template <class T> __device__ __forceinline__ void gate(float g, float &a, float
     const float r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;
     a = g >= 0.f ? r : s;
     c = g >= 0.f ? s : r;
-    if (g != g) a = c = g;
+}
+
+// ------------------------------------------------------------ published pairs
+using Slot = unsigned long long;
+constexpr Slot kEmpty = ~(Slot)0;
+
+struct Geom {
+    int64_t rows;  // records x slabs
+    int slabs, segs;
+    Slot *slots;   // [segs][rows][kSlab]
+    unsigned *ticket;
+};
+
+// One 64-bit access per pair: a reader sees all of it or none.  Agent scope
+// reaches the other XCDs; nothing else is handed over, so no ordering is needed.
+__device__ __forceinline__ void publish(Slot *p, float a, float b)
+{
+    const uint32_t hi = a == a ? __float_as_uint(a) : 0x7fc00000u;  // a NaN, but not kEmpty
+    __hip_atomic_store(p, (Slot)hi << 32 | __float_as_uint(b), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ Slot look(const Slot *p)
+{
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// The pair at p, which was `v` when last looked at.  The count only keeps a
+// broken launch from running for good: it is a matter of seconds.
+__device__ __forceinline__ float2 await(const Slot *p, Slot v)
+{
+    for (int k = 0; v == kEmpty && k < 1 << 22; k++) {
+        __builtin_amdgcn_s_sleep(1);
+        v = look(p);
+    }
+    return make_float2(__uint_as_float((uint32_t)(v >> 32)), __uint_as_float((uint32_t)v));
+}
+
+__global__ __launch_bounds__(256) void k_scan_clear(Slot *slots, int64_t n, unsigned *ticket)
+{
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2;
+    if (i == 0) *ticket = 0;
+    if (i < n) *(ulonglong2 *)(slots + i) = make_ulonglong2(kEmpty, kEmpty);  // n is even
 }
 
 // What a workgroup works on.
-struct Place {
-    int64_t b, len;
-    int seg;
-    int64_t c0;  // the lane's first channel
-    int n;       // its channels
+template <class K> struct Place {
+    int64_t row, b;
+    int seg, wave, lane, c0, n;  // the lane's first channel and their number
+    int64_t len, t0;             // the record's length, the wavefront's first step
+    int nv;                      // its steps that the record has
+    // Segments of the row, in the order they are taken, that hold steps of the
+    // record (one at least): the others write zeros and are not waited for.
+    int seg0, seg1;
+    __device__ Place(const ScanArgs &a, const Geom &g, int item, bool back)
+    {
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        lane = threadIdx.x & 63;
+        row = item % g.rows;
+        seg = (int)(item / g.rows);
+        b = row / g.slabs;
+        c0 = (int)(row % g.slabs) * K::slab + lane * K::CV;
+        n = (int)max((int64_t)0, min((int64_t)K::CV, a.D - c0));
+        if (n == 0) c0 = 0;
+        len = a.T;
+        if (a.lengths) len = min(max((int64_t)a.lengths[b], (int64_t)0), a.T);
+        t0 = (int64_t)(back ? g.segs - 1 - seg : seg) * K::seg + wave * K::steps;
+        nv = (int)max((int64_t)0, min((int64_t)K::steps, len - t0));
+        const int some = max(1, (int)((len + K::seg - 1) / K::seg));
+        seg0 = back ? g.segs - some : 0;
+        seg1 = back ? g.segs : some;
+    }
+    __device__ bool idle() const { return seg < seg0 || seg >= seg1; }
 };
 
-template <int CV> __device__ __forceinline__ Place place_of(const ScanArgs &a, int slabs, int segs)
+__device__ __forceinline__ int take_item(const Geom &g)
 {
-    Place p;
-    const int64_t blk = blockIdx.x;
-    p.seg = (int)(blk / slabs % segs);
-    p.b = blk / slabs / segs;
-    p.c0 = ((blk % slabs) * 64 + (threadIdx.x & 63)) * CV;
-    p.n = (int)max((int64_t)0, min((int64_t)CV, a.D - p.c0));
-    if (p.n == 0) p.c0 = 0;
-    p.len = a.T;
-    if (a.lengths) p.len = min(max((int64_t)a.lengths[p.b], (int64_t)0), a.T);
-    return p;
+    if (g.segs == 1) return (int)blockIdx.x;
+    __shared__ int item;
+    if (threadIdx.x == 0) item = (int)atomicAdd(g.ticket, 1u);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(item);
 }
 
-// The raw elements of one wavefront's steps; steps past `nv` are not read.
-template <class T, int CV> struct Raw {
-    T v[kSteps][CV];
-    __device__ __forceinline__ void load(const T *p, int64_t step, int nv, int n)
+// The raw elements of one wavefront's steps.  Steps past the record's end read
+// the last step again and lanes past D the first channel: no branches between
+// the reads, and nothing is done with them.  With two channels per lane, a
+// lane that has only the row's last one reads the one before it, too, and
+// shifts (rows have more than 64 channels then).
+template <class K> struct Raw {
+    using T = typename K::T;
+    using Word = std::conditional_t<sizeof(T) * K::CV == 4, uint32_t, uint16_t>;
+    Word v[K::steps];
+    int shift;
+    __device__ __forceinline__ void load(const T *p, int64_t step, const Place<K> &at)
     {
+        const bool odd = K::CV == 2 && at.n == 1;
+        shift = odd ? 16 : 0;
+        const uint32_t c = (uint32_t)(at.c0 - (odd ? 1 : 0)) * (uint32_t)sizeof(T);
+        const char *row = (const char *)p;
+        const int64_t bytes = step * (int64_t)sizeof(T);
+        if (at.nv > 0)
 #pragma unroll
-        for (int i = 0; i < kSteps; i++) {
-            if (i >= nv) continue;
-            if (n == CV) __builtin_memcpy(v[i], p + i * step, sizeof v[i]);
-            else
-#pragma unroll
-                for (int j = 0; j < CV; j++)
-                    if (j < n) v[i][j] = p[i * step + j];
+            for (int i = 0; i < K::steps; i++) {
+                __builtin_memcpy(&v[i], row + c, sizeof(Word));
+                if (i + 1 < at.nv) row += bytes;
+            }
+    }
+    __device__ __forceinline__ void at(int i, float (&f)[K::CV]) const
+    {
+        if constexpr (K::CV == 2) {
+            const uint32_t w = v[i] >> shift;
+            T lo, hi;
+            const uint16_t l = (uint16_t)w, h = (uint16_t)(w >> 16);
+            __builtin_memcpy(&lo, &l, 2);
+            __builtin_memcpy(&hi, &h, 2);
+            f[0] = (float)lo;
+            f[1] = (float)hi;
+        } else {
+            T x;
+            __builtin_memcpy(&x, &v[i], sizeof x);
+            f[0] = (float)x;
         }
     }
 };
 
-// ------------------------------------------------------------------ forward
-// start: the states the segments start from ([B, segs, D]), or h0 with one
-// segment.  PAIRS: only the segments' pairs are wanted, [B, segs, D] (A, B).
-template <class T, int CV, bool PAIRS>
-__global__ __launch_bounds__(kThreads) void k_scan(ScanArgs a, int slabs, int segs, int seg_pieces,
-                                                  const float *start, float2 *pairs)
+// Steps [0, steps) of f, those that the record's array has.
+template <class K>
+__device__ __forceinline__ void put(typename K::T *p, int64_t step, int64_t T, const Place<K> &at,
+                                    const float (&f)[K::steps][K::CV])
 {
-    __shared__ float2 agg[2][kWaves][64 * CV];
-    const Place p = place_of<CV>(a, slabs, segs);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const T *x = (const T *)a.x + p.b * a.xb + p.c0, *g = (const T *)a.g + p.b * a.gb + p.c0;
-    T *y = (T *)a.y + p.b * a.yb + p.c0;
-    const int64_t pieces = (a.T + kPiece - 1) / kPiece;
-    const int64_t j0 = (int64_t)p.seg * seg_pieces, j1 = min(j0 + seg_pieces, pieces);
-    const int64_t last = min(j1, (p.len + kPiece - 1) / kPiece);  // pieces with steps of the record
-    float h[CV], whole[CV];
+    using E = typename K::T;
+    const int steps = (int)max((int64_t)0, min((int64_t)K::steps, T - at.t0));
+    if (at.n == K::CV) {
+        const uint32_t c = (uint32_t)at.c0 * (uint32_t)sizeof(E);
+        char *row = (char *)p;
+        const int64_t bytes = step * (int64_t)sizeof(E);
 #pragma unroll
-    for (int j = 0; j < CV; j++) {
-        h[j] = !PAIRS && start && j < p.n ? start[(p.b * segs + p.seg) * a.D + p.c0 + j] : 0.f;
-        whole[j] = 1.f;
+        for (int i = 0; i < K::steps; i++) {
+            E e[K::CV];
+#pragma unroll
+            for (int j = 0; j < K::CV; j++) e[j] = (E)f[i][j];
+            if (i < steps) __builtin_memcpy(row + c, e, sizeof e);
+            row += bytes;
+        }
+    } else if (at.n) {
+#pragma unroll
+        for (int i = 0; i < K::steps; i++)
+            if (i < steps) p[i * step + at.c0] = (E)f[i][0];
     }
-    Raw<T, CV> rx, rg;
-    auto fetch = [&](int64_t piece) {
-        const int64_t t = piece * kPiece + wave * kSteps;
-        const int nv = (int)max((int64_t)0, min((int64_t)kSteps, p.len - t));
-        rx.load(x + t * a.xs, a.xs, nv, p.n);
-        rg.load(g + t * a.gs, a.gs, nv, p.n);
-    };
-    if (j0 < last) fetch(j0);
+}
+
+// The state the segment starts from: `first` if it is the first of its row,
+// else the composition of the segments before it.  Each wavefront looks at one
+// slot of a window; all wavefronts get the same result.
+template <class K>
+__device__ __forceinline__ void look_back(const Geom &g, const Place<K> &at, float2 (*win)[kWaves][K::slab],
+                                          const float (&first)[K::CV], float (&h)[K::CV])
+{
+    constexpr int CV = K::CV;
+    float P[CV];
+#pragma unroll
+    for (int j = 0; j < CV; j++) P[j] = 1.f, h[j] = 0.f;
     int turn = 0;
-    for (int64_t piece = j0; piece < last; piece++, turn ^= 1) {
-        const int64_t t = piece * kPiece + wave * kSteps;
-        const int nv = (int)max((int64_t)0, min((int64_t)kSteps, p.len - t));
-        float ga[kSteps][CV], gb[kSteps][CV], A[CV], Bv[CV];
+    for (int top = at.seg - 1; top >= at.seg0; top -= kWaves, turn ^= 1) {
+        const int s = top - at.wave;
+        float2 q[CV];
 #pragma unroll
-        for (int j = 0; j < CV; j++) A[j] = 1.f, Bv[j] = 0.f;
+        for (int j = 0; j < CV; j++) q[j] = make_float2(1.f, 0.f);
+        if (s >= at.seg0) {
+            const Slot *p = g.slots + ((int64_t)s * g.rows + at.row) * K::slab + at.lane * CV;
+            Slot v[CV];
 #pragma unroll
-        for (int i = 0; i < kSteps; i++)
+            for (int j = 0; j < CV; j++) v[j] = look(p + j);
 #pragma unroll
-            for (int j = 0; j < CV; j++) {
-                float av = 1.f, bv = 0.f;
-                if (i < nv && j < p.n) {
-                    float c;
-                    gate<T>((float)rg.v[i][j], av, c);
-                    bv = c * (float)rx.v[i][j];
-                }
-                ga[i][j] = av;
-                gb[i][j] = bv;
-                Bv[j] = fmaf(av, Bv[j], bv);
-                A[j] *= av;
-            }
+            for (int j = 0; j < CV; j++) q[j] = await(p + j, v[j]);
+        }
 #pragma unroll
-        for (int j = 0; j < CV; j++) agg[turn][wave][lane * CV + j] = make_float2(A[j], Bv[j]);
-        if (piece + 1 < last) fetch(piece + 1);
+        for (int j = 0; j < CV; j++) win[turn][at.wave][at.lane * CV + j] = q[j];
         __syncthreads();
-        if (!PAIRS && a.states && wave == 0)
-#pragma unroll
-            for (int j = 0; j < CV; j++)
-                if (j < p.n) a.states[(p.b * pieces + piece) * a.D + p.c0 + j] = h[j];
-        float mine[CV];
-#pragma unroll
-        for (int j = 0; j < CV; j++) mine[j] = h[j];
+        bool more = false;
 #pragma unroll
         for (int w = 0; w < kWaves; w++)
 #pragma unroll
             for (int j = 0; j < CV; j++) {
-                if (!PAIRS && w == wave) mine[j] = h[j];
-                const float2 m = agg[turn][w][lane * CV + j];
-                h[j] = fmaf(m.x, h[j], m.y);
-                whole[j] *= m.x;
+                const float2 r = win[turn][w][at.lane * CV + j];
+                h[j] = fmaf(P[j], r.y, h[j]);
+                P[j] *= r.x;
             }
-        if (PAIRS) continue;
 #pragma unroll
-        for (int i = 0; i < kSteps; i++) {
-            float o[CV];
-#pragma unroll
-            for (int j = 0; j < CV; j++) {
-                mine[j] = fmaf(ga[i][j], mine[j], gb[i][j]);
-                o[j] = i < nv ? mine[j] : 0.f;
-            }
-            if (t + i < a.T) store_part<CV>(y + (t + i) * a.ys, p.n, o);
-        }
+        for (int j = 0; j < CV; j++) more = more || P[j] != 0.f;
+        if (!__any(more)) return;  // the same in every wavefront
     }
-    if (PAIRS) {
-        if (wave == 0)
 #pragma unroll
-            for (int j = 0; j < CV; j++)
-                if (j < p.n) pairs[(p.b * segs + p.seg) * a.D + p.c0 + j] = make_float2(whole[j], h[j]);
+    for (int j = 0; j < CV; j++) h[j] = fmaf(P[j], first[j], h[j]);
+}
+
+// ------------------------------------------------------------------ forward
+template <class K> __global__ __launch_bounds__(kThreads, 6) void k_scan(ScanArgs a, Geom g)
+{
+    using T = typename K::T;
+    constexpr int CV = K::CV, L = K::steps;
+    __shared__ float2 agg[kWaves][K::slab], win[2][kWaves][K::slab];
+    const Place<K> at(a, g, take_item(g), false);
+    T *y = (T *)a.y + at.b * a.yb + at.t0 * a.ys;
+    float ga[L][CV], gb[L][CV], A[CV], B[CV];
+    if (at.idle()) {
+#pragma unroll
+        for (int i = 0; i < L; i++)
+#pragma unroll
+            for (int j = 0; j < CV; j++) ga[i][j] = 0.f;
+        put<K>(y, a.ys, a.T, at, ga);
         return;
     }
-    if (a.h_last && wave == 0 && p.seg == segs - 1)
+    Raw<K> rx, rg;
+    rg.load((const T *)a.g + at.b * a.gb + at.t0 * a.gs, a.gs, at);
+    rx.load((const T *)a.x + at.b * a.xb + at.t0 * a.xs, a.xs, at);
+    float first[CV];
 #pragma unroll
-        for (int j = 0; j < CV; j++)
-            if (j < p.n) a.h_last[p.b * a.D + p.c0 + j] = h[j];
-    // pieces past the record's end
-    const float zero[CV] = {};
-    for (int64_t piece = max(last, j0); piece < j1; piece++) {
-        if (a.states && wave == 0)
+    for (int j = 0; j < CV; j++) first[j] = a.h0 && j < at.n ? a.h0[at.b * a.D + at.c0 + j] : 0.f;
 #pragma unroll
-            for (int j = 0; j < CV; j++)
-                if (j < p.n) a.states[(p.b * pieces + piece) * a.D + p.c0 + j] = h[j];
+    for (int j = 0; j < CV; j++) A[j] = 1.f, B[j] = 0.f;
+    auto gates = [&](auto all) {
 #pragma unroll
-        for (int i = 0; i < kSteps; i++) {
-            const int64_t t = piece * kPiece + wave * kSteps + i;
-            if (t < a.T) store_part<CV>(y + t * a.ys, p.n, zero);
+        for (int i = 0; i < L; i++) {
+            const bool on = all.value || i < at.nv;
+            float xv[CV], gv[CV];
+            rx.at(i, xv);
+            rg.at(i, gv);
+#pragma unroll
+            for (int j = 0; j < CV; j++) {
+                float c;
+                gate<T>(gv[j], ga[i][j], c);
+                gb[i][j] = c * xv[j];
+                if (!on) ga[i][j] = 1.f, gb[i][j] = 0.f;
+                B[j] = fmaf(ga[i][j], B[j], gb[i][j]);
+                A[j] *= ga[i][j];
+            }
+        }
+    };
+    if (at.nv == L) gates(std::true_type{});
+    else gates(std::false_type{});
+#pragma unroll
+    for (int j = 0; j < CV; j++) agg[at.wave][at.lane * CV + j] = make_float2(A[j], B[j]);
+    __syncthreads();
+    const bool shared = at.seg + 1 < at.seg1 && at.wave == 0;  // later segments will ask
+    Slot *slot = g.slots + ((int64_t)at.seg * g.rows + at.row) * K::slab + at.lane * CV;
+    float wholeA[CV], wholeB[CV];
+    if (shared) {
+#pragma unroll
+        for (int j = 0; j < CV; j++) wholeA[j] = 1.f, wholeB[j] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; w++)
+#pragma unroll
+            for (int j = 0; j < CV; j++) {
+                const float2 q = agg[w][at.lane * CV + j];
+                wholeB[j] = fmaf(q.x, wholeB[j], q.y);
+                wholeA[j] *= q.x;
+            }
+#pragma unroll
+        for (int j = 0; j < CV; j++) {
+            if (j >= at.n) wholeA[j] = wholeB[j] = 0.f;  // lanes past D ask for nothing more
+            if (at.seg > at.seg0) publish(slot + j, wholeA[j], wholeB[j]);
         }
     }
+    float h[CV];
+    look_back<K>(g, at, win, first, h);
+    if (shared)
+#pragma unroll
+        for (int j = 0; j < CV; j++) publish(slot + j, 0.f, fmaf(wholeA[j], h[j], wholeB[j]));
+    for (int w = 0; w < at.wave; w++)
+#pragma unroll
+        for (int j = 0; j < CV; j++) {
+            const float2 q = agg[w][at.lane * CV + j];
+            h[j] = fmaf(q.x, h[j], q.y);
+        }
+    if (a.states && at.t0 % kPiece == 0 && at.nv > 0) {
+        float *st = a.states + (at.b * ((a.T + kPiece - 1) / kPiece) + at.t0 / kPiece) * a.D;
+#pragma unroll
+        for (int j = 0; j < CV; j++)
+            if (j < at.n) st[at.c0 + j] = h[j];
+    }
+#pragma unroll
+    for (int i = 0; i < L; i++)
+#pragma unroll
+        for (int j = 0; j < CV; j++) {
+            h[j] = fmaf(ga[i][j], h[j], gb[i][j]);
+            ga[i][j] = i < at.nv ? h[j] : 0.f;
+        }
+    put<K>(y, a.ys, a.T, at, ga);
+    if (a.h_last && at.seg == at.seg1 - 1 && at.wave == kWaves - 1)
+#pragma unroll
+        for (int j = 0; j < CV; j++)
+            if (j < at.n) a.h_last[at.b * a.D + at.c0 + j] = h[j];
 }
 
 // ----------------------------------------------------------------- backward
-// end: what the segments' last steps receive from the steps after them
-// ([B, segs, D]), or dh_last with one segment.
-template <class T, int CV>
-__global__ __launch_bounds__(kThreads) void k_scan_grad(ScanArgs a, int slabs, int segs, int seg_pieces,
-                                                       const float *end)
+template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(ScanArgs a, Geom g)
 {
-    __shared__ float2 fwd[2][kWaves][64 * CV];
-    __shared__ float rev[2][kWaves][64 * CV];
-    const Place p = place_of<CV>(a, slabs, segs);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const T *x = (const T *)a.x + p.b * a.xb + p.c0, *g = (const T *)a.g + p.b * a.gb + p.c0;
-    const T *dy = (const T *)a.dy + p.b * a.dyb + p.c0;
-    T *dx = (T *)a.dx + p.b * a.dxb + p.c0, *dg = (T *)a.dg + p.b * a.dgb + p.c0;
-    const int64_t pieces = (a.T + kPiece - 1) / kPiece;
-    const int64_t j0 = (int64_t)p.seg * seg_pieces, j1 = min(j0 + seg_pieces, pieces);
-    const int64_t last = min(j1, (p.len + kPiece - 1) / kPiece);
-    float m[CV];
+    using T = typename K::T;
+    constexpr int CV = K::CV, L = K::steps, kBefore = kPiece / L;  // wavefronts of a piece
+    __shared__ float2 agg[kWaves][K::slab], win[2][kWaves][K::slab];
+    __shared__ float rev[kWaves][K::slab];
+    const Place<K> at(a, g, take_item(g), true);
+    T *dx = (T *)a.dx + at.b * a.dxb + at.t0 * a.dxs, *dg = (T *)a.dg + at.b * a.dgb + at.t0 * a.dgs;
+    float ga[L][CV], gc[L][CV], A[CV], Bf[CV], Br[CV];
+    if (at.idle()) {
 #pragma unroll
-    for (int j = 0; j < CV; j++) m[j] = end && j < p.n ? end[(p.b * segs + p.seg) * a.D + p.c0 + j] : 0.f;
-    Raw<T, CV> rx, rg, rd;
-    float h_next[CV];  // the state before the piece that is fetched
-    auto fetch = [&](int64_t piece) {
-        const int64_t t = piece * kPiece + wave * kSteps;
-        const int nv = (int)max((int64_t)0, min((int64_t)kSteps, p.len - t));
-        rx.load(x + t * a.xs, a.xs, nv, p.n);
-        rg.load(g + t * a.gs, a.gs, nv, p.n);
-        rd.load(dy + t * a.dys, a.dys, nv, p.n);
+        for (int i = 0; i < L; i++)
 #pragma unroll
-        for (int j = 0; j < CV; j++)
-            h_next[j] = j < p.n ? a.states_in[(p.b * pieces + piece) * a.D + p.c0 + j] : 0.f;
-    };
-    if (j0 < last) fetch(last - 1);
-    int turn = 0;
-    for (int64_t piece = last - 1; piece >= j0; piece--, turn ^= 1) {
-        const int64_t t = piece * kPiece + wave * kSteps;
-        const int nv = (int)max((int64_t)0, min((int64_t)kSteps, p.len - t));
-        float ga[kSteps][CV], gc[kSteps][CV], xv[kSteps][CV], dv[kSteps][CV], A[CV], Bf[CV], Br[CV], h[CV];
+            for (int j = 0; j < CV; j++) ga[i][j] = 0.f;
+        put<K>(dx, a.dxs, a.T, at, ga);
+        put<K>(dg, a.dgs, a.T, at, ga);
+        return;
+    }
+    Raw<K> rx, rg, rd;
+    rg.load((const T *)a.g + at.b * a.gb + at.t0 * a.gs, a.gs, at);
+    rx.load((const T *)a.x + at.b * a.xb + at.t0 * a.xs, a.xs, at);
+    rd.load((const T *)a.dy + at.b * a.dyb + at.t0 * a.dys, a.dys, at);
+    float last[CV], h[CV];
 #pragma unroll
-        for (int j = 0; j < CV; j++) A[j] = 1.f, Bf[j] = Br[j] = 0.f, h[j] = h_next[j];
+    for (int j = 0; j < CV; j++) {
+        last[j] = a.dh_last && j < at.n ? a.dh_last[at.b * a.D + at.c0 + j] : 0.f;
+        h[j] = 0.f;
+        if (at.nv > 0 && j < at.n)
+            h[j] = a.states_in[(at.b * ((a.T + kPiece - 1) / kPiece) + at.t0 / kPiece) * a.D + at.c0 + j];
+    }
 #pragma unroll
-        for (int i = 0; i < kSteps; i++)
+    for (int j = 0; j < CV; j++) A[j] = 1.f, Bf[j] = Br[j] = 0.f;
+    auto gates = [&](auto all) {
+#pragma unroll
+        for (int i = 0; i < L; i++) {
+            const bool on = all.value || i < at.nv;
+            float xv[CV], gv[CV];
+            rx.at(i, xv);
+            rg.at(i, gv);
 #pragma unroll
             for (int j = 0; j < CV; j++) {
-                float av = 1.f, cv = 0.f, xx = 0.f, d = 0.f;
-                if (i < nv && j < p.n) {
-                    gate<T>((float)rg.v[i][j], av, cv);
-                    xx = (float)rx.v[i][j];
-                    d = (float)rd.v[i][j];
-                }
-                ga[i][j] = av;
-                gc[i][j] = cv;
-                xv[i][j] = xx;
-                dv[i][j] = d;
-                Bf[j] = fmaf(av, Bf[j], cv * xx);
-                A[j] *= av;
+                gate<T>(gv[j], ga[i][j], gc[i][j]);
+                float b = gc[i][j] * xv[j];
+                if (!on) ga[i][j] = 1.f, gc[i][j] = b = 0.f;
+                Bf[j] = fmaf(ga[i][j], Bf[j], b);
+                A[j] *= ga[i][j];
             }
+        }
 #pragma unroll
-        for (int i = kSteps - 1; i >= 0; i--)
+        for (int i = L - 1; i >= 0; i--) {
+            const bool on = all.value || i < at.nv;
+            float d[CV];
+            rd.at(i, d);
 #pragma unroll
-            for (int j = 0; j < CV; j++) Br[j] = ga[i][j] * (Br[j] + dv[i][j]);
+            for (int j = 0; j < CV; j++) Br[j] = on ? ga[i][j] * (Br[j] + d[j]) : Br[j];
+        }
+    };
+    if (at.nv == L) gates(std::true_type{});
+    else gates(std::false_type{});
+#pragma unroll
+    for (int j = 0; j < CV; j++) {
+        agg[at.wave][at.lane * CV + j] = make_float2(A[j], Bf[j]);
+        rev[at.wave][at.lane * CV + j] = Br[j];
+    }
+    __syncthreads();
+    const bool shared = at.seg + 1 < at.seg1 && at.wave == 0;
+    Slot *slot = g.slots + ((int64_t)at.seg * g.rows + at.row) * K::slab + at.lane * CV;
+    float wholeA[CV], wholeB[CV];
+    if (at.wave == 0) {
+#pragma unroll
+        for (int j = 0; j < CV; j++) wholeA[j] = 1.f, wholeB[j] = 0.f;
+#pragma unroll
+        for (int w = kWaves - 1; w >= 0; w--)
+#pragma unroll
+            for (int j = 0; j < CV; j++) {
+                const float q = agg[w][at.lane * CV + j].x;
+                wholeB[j] = fmaf(q, wholeB[j], rev[w][at.lane * CV + j]);
+                wholeA[j] *= q;
+            }
 #pragma unroll
         for (int j = 0; j < CV; j++) {
-            fwd[turn][wave][lane * CV + j] = make_float2(A[j], Bf[j]);
-            rev[turn][wave][lane * CV + j] = Br[j];
-        }
-        if (piece > j0) fetch(piece - 1);
-        __syncthreads();
-        float mine[CV];
-#pragma unroll
-        for (int j = 0; j < CV; j++) mine[j] = m[j];
-#pragma unroll
-        for (int w = kWaves - 1; w >= 0; w--)
-#pragma unroll
-            for (int j = 0; j < CV; j++) {
-                if (w == wave) mine[j] = m[j];
-                m[j] = fmaf(fwd[turn][w][lane * CV + j].x, m[j], rev[turn][w][lane * CV + j]);
-            }
-        for (int w = 0; w < wave; w++)
-#pragma unroll
-            for (int j = 0; j < CV; j++) {
-                const float2 f = fwd[turn][w][lane * CV + j];
-                h[j] = fmaf(f.x, h[j], f.y);
-            }
-        // forwards: x becomes h_{t-1} - x
-#pragma unroll
-        for (int i = 0; i < kSteps; i++)
-#pragma unroll
-            for (int j = 0; j < CV; j++) {
-                const float b = gc[i][j] * xv[i][j];
-                xv[i][j] = h[j] - xv[i][j];
-                h[j] = fmaf(ga[i][j], h[j], b);
-            }
-#pragma unroll
-        for (int i = kSteps - 1; i >= 0; i--) {
-            float ox[CV], og[CV];
-#pragma unroll
-            for (int j = 0; j < CV; j++) {
-                const float l = dv[i][j] + mine[j];
-                mine[j] = ga[i][j] * l;
-                ox[j] = i < nv ? gc[i][j] * l : 0.f;
-                og[j] = i < nv ? gc[i][j] * mine[j] * xv[i][j] : 0.f;
-            }
-            if (t + i < a.T) {
-                store_part<CV>(dx + (t + i) * a.dxs, p.n, ox);
-                store_part<CV>(dg + (t + i) * a.dgs, p.n, og);
-            }
+            if (j >= at.n) wholeA[j] = wholeB[j] = 0.f;
+            if (shared && at.seg > at.seg0) publish(slot + j, wholeA[j], wholeB[j]);
         }
     }
-    if (a.dh0 && wave == 0 && p.seg == 0)
+    float m[CV];
+    look_back<K>(g, at, win, last, m);
+    if (at.wave == 0)
 #pragma unroll
-        for (int j = 0; j < CV; j++)
-            if (j < p.n) a.dh0[p.b * a.D + p.c0 + j] = m[j];
-    const float zero[CV] = {};
-    for (int64_t piece = max(last, j0); piece < j1; piece++)
-#pragma unroll
-        for (int i = 0; i < kSteps; i++) {
-            const int64_t t = piece * kPiece + wave * kSteps + i;
-            if (t < a.T) {
-                store_part<CV>(dx + t * a.dxs, p.n, zero);
-                store_part<CV>(dg + t * a.dgs, p.n, zero);
-            }
+        for (int j = 0; j < CV; j++) {
+            const float out = fmaf(wholeA[j], m[j], wholeB[j]);
+            if (shared) publish(slot + j, 0.f, out);
+            if (a.dh0 && at.seg == g.segs - 1 && j < at.n) a.dh0[at.b * a.D + at.c0 + j] = out;
         }
-}
-
-// The segments' pairs backwards: (A, B) with B what a segment hands to the one
-// before it when it receives nothing.
-template <class T, int CV>
-__global__ __launch_bounds__(kThreads) void k_scan_grad_pairs(ScanArgs a, int slabs, int segs, int seg_pieces,
-                                                             float2 *pairs)
-{
-    __shared__ float2 agg[2][kWaves][64 * CV];
-    const Place p = place_of<CV>(a, slabs, segs);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const T *g = (const T *)a.g + p.b * a.gb + p.c0, *dy = (const T *)a.dy + p.b * a.dyb + p.c0;
-    const int64_t pieces = (a.T + kPiece - 1) / kPiece;
-    const int64_t j0 = (int64_t)p.seg * seg_pieces, j1 = min(j0 + seg_pieces, pieces);
-    const int64_t last = min(j1, (p.len + kPiece - 1) / kPiece);
-    float m[CV], whole[CV];
+    for (int w = kWaves - 1; w > at.wave; w--)
 #pragma unroll
-    for (int j = 0; j < CV; j++) m[j] = 0.f, whole[j] = 1.f;
-    Raw<T, CV> rg, rd;
-    auto fetch = [&](int64_t piece) {
-        const int64_t t = piece * kPiece + wave * kSteps;
-        const int nv = (int)max((int64_t)0, min((int64_t)kSteps, p.len - t));
-        rg.load(g + t * a.gs, a.gs, nv, p.n);
-        rd.load(dy + t * a.dys, a.dys, nv, p.n);
-    };
-    if (j0 < last) fetch(last - 1);
-    int turn = 0;
-    for (int64_t piece = last - 1; piece >= j0; piece--, turn ^= 1) {
-        const int64_t t = piece * kPiece + wave * kSteps;
-        const int nv = (int)max((int64_t)0, min((int64_t)kSteps, p.len - t));
-        float A[CV], B[CV];
+        for (int j = 0; j < CV; j++) m[j] = fmaf(agg[w][at.lane * CV + j].x, m[j], rev[w][at.lane * CV + j]);
+    for (int w = at.wave / kBefore * kBefore; w < at.wave; w++)
 #pragma unroll
-        for (int j = 0; j < CV; j++) A[j] = 1.f, B[j] = 0.f;
-#pragma unroll
-        for (int i = kSteps - 1; i >= 0; i--)
-#pragma unroll
-            for (int j = 0; j < CV; j++) {
-                float av = 1.f, cv, d = 0.f;
-                if (i < nv && j < p.n) {
-                    gate<T>((float)rg.v[i][j], av, cv);
-                    d = (float)rd.v[i][j];
-                }
-                A[j] *= av;
-                B[j] = av * (B[j] + d);
-            }
-#pragma unroll
-        for (int j = 0; j < CV; j++) agg[turn][wave][lane * CV + j] = make_float2(A[j], B[j]);
-        if (piece > j0) fetch(piece - 1);
-        __syncthreads();
-#pragma unroll
-        for (int w = kWaves - 1; w >= 0; w--)
-#pragma unroll
-            for (int j = 0; j < CV; j++) {
-                const float2 q = agg[turn][w][lane * CV + j];
-                m[j] = fmaf(q.x, m[j], q.y);
-                whole[j] *= q.x;
-            }
-    }
-    if (wave == 0)
-#pragma unroll
-        for (int j = 0; j < CV; j++)
-            if (j < p.n) pairs[(p.b * segs + p.seg) * a.D + p.c0 + j] = make_float2(whole[j], m[j]);
-}
-
-// What each segment starts from: state[b, s] from the pairs of the segments
-// before s (BACK: after s) and first[b] (NULL: zeros).  The workgroup's
-// wavefronts take consecutive parts of the segments.
-constexpr int kJoinWaves = 16;
-template <bool BACK>
-__global__ __launch_bounds__(64 * kJoinWaves) void k_scan_join(const float2 *pairs, const float *first, float *state,
-                                                              int64_t D, int segs)
-{
-    __shared__ float2 agg[kJoinWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t slabs = (D + 63) / 64, b = blockIdx.x / slabs, c = blockIdx.x % slabs * 64 + lane;
-    const bool in = c < D;
-    const int per = (segs + kJoinWaves - 1) / kJoinWaves;
-    const int s0 = min(wave * per, segs), s1 = min(s0 + per, segs);
-    auto at = [&](int s) { return (b * segs + (BACK ? segs - 1 - s : s)) * D + c; };
-    float2 q = make_float2(1.f, 0.f);
-    if (in)
-#pragma unroll 8
-        for (int s = s0; s < s1; s++) {
-            const float2 v = pairs[at(s)];
-            q.y = fmaf(v.x, q.y, v.y);
-            q.x *= v.x;
+        for (int j = 0; j < CV; j++) {
+            const float2 q = agg[w][at.lane * CV + j];
+            h[j] = fmaf(q.x, h[j], q.y);
         }
-    agg[wave][lane] = q;
-    __syncthreads();
-    if (!in) return;
-    float h = first ? first[b * D + c] : 0.f;
-    for (int w = 0; w < wave; w++) h = fmaf(agg[w][lane].x, h, agg[w][lane].y);
-#pragma unroll 8
-    for (int s = s0; s < s1; s++) {
-        const float2 v = pairs[at(s)];
-        state[at(s)] = h;
-        h = fmaf(v.x, h, v.y);
+    float away[L][CV];  // h_{t-1} - x_t, then dg
+#pragma unroll
+    for (int i = 0; i < L; i++) {
+        float xv[CV];
+        rx.at(i, xv);
+#pragma unroll
+        for (int j = 0; j < CV; j++) {
+            away[i][j] = h[j] - xv[j];
+            h[j] = fmaf(ga[i][j], h[j], gc[i][j] * xv[j]);
+        }
     }
+#pragma unroll
+    for (int i = L - 1; i >= 0; i--) {
+        const bool on = i < at.nv;
+        float d[CV];
+        rd.at(i, d);
+#pragma unroll
+        for (int j = 0; j < CV; j++) {
+            const float l = d[j] + m[j];
+            m[j] = on ? ga[i][j] * l : m[j];
+            away[i][j] = on ? gc[i][j] * m[j] * away[i][j] : 0.f;
+            gc[i][j] = on ? gc[i][j] * l : 0.f;
+        }
+    }
+    put<K>(dx, a.dxs, a.T, at, gc);
+    put<K>(dg, a.dgs, a.T, at, away);
 }
 
 // ------------------------------------------------------------------- a few steps
@@ -442,7 +507,7 @@ template <class T> __global__ __launch_bounds__(256) void k_scan_few(ScanArgs a,
     T *y = (T *)a.y + b * a.yb + c;
     float h[VE] = {};
     if (a.h0) load_part<VE>(a.h0 + b * a.D + c, n, h);
-    if (a.states && a.T) store_part<VE>(a.states + b * a.D + c, n, h);
+    if (a.states && len) store_part<VE>(a.states + b * a.D + c, n, h);
     for (int64_t t = 0; t < a.T; t++) {
         float o[VE] = {};
         if (t < len) {
@@ -461,51 +526,43 @@ template <class T> __global__ __launch_bounds__(256) void k_scan_few(ScanArgs a,
     if (a.h_last) store_part<VE>(a.h_last + b * a.D + c, n, h);
 }
 
-// How a scan is cut: channels per lane, and segments of the time axis.
-struct Cut {
-    int cv, segs, seg_pieces;
-    int64_t slabs, pieces;
-    Cut(int64_t B, int64_t T, int64_t D)
+// ------------------------------------------------------------------ launches
+// Rows (records x slabs) and segments of a scan of kind K.
+template <class K> struct Layout {
+    int64_t rows, items;
+    int slabs, segs;
+    size_t ticket, slots, bytes;
+    Layout(int64_t B, int64_t T, int64_t D)
     {
-        pieces = (T + kPiece - 1) / kPiece;
-        const int64_t want = 1024;  // workgroups that fill the chip
-        cv = B * ((D + 127) / 128) >= want / 2 ? 2 : 1;
-        slabs = (D + 64 * cv - 1) / (64 * cv);
-        const int64_t rows = std::max<int64_t>(1, B * slabs);
-        int64_t s = rows >= want / 2 ? 1 : std::min(want / rows, (pieces + 1) / 2);
-        s = std::max<int64_t>(s, 1);
-        seg_pieces = (int)std::max<int64_t>(1, (pieces + s - 1) / s);
-        segs = (int)std::max<int64_t>(1, (pieces + seg_pieces - 1) / seg_pieces);
+        slabs = (int)((D + K::slab - 1) / K::slab);
+        rows = B * slabs;
+        segs = (int)std::max<int64_t>(1, (T + K::seg - 1) / K::seg);
+        items = rows * segs;
+        Carver c;
+        ticket = c.take(segs > 1 ? sizeof(unsigned) : 0);
+        slots = c.take(segs > 1 ? sizeof(Slot) * items * K::slab : 0);
+        bytes = c.used;
+    }
+    // workspace and the call's first kernel
+    Geom start(void *ws, hipStream_t s) const
+    {
+        Geom g{};
+        g.rows = rows, g.slabs = slabs, g.segs = segs;
+        if (segs == 1) return g;
+        g.slots = (Slot *)((char *)ws + slots);
+        g.ticket = (unsigned *)((char *)ws + ticket);
+        const int64_t n = items * K::slab;
+        k_scan_clear<<<(unsigned)((n + 511) / 512), 256, 0, s>>>(g.slots, n, g.ticket);
+        return g;
     }
 };
 
-struct ScanSpace {
-    size_t pairs, state, bytes;
-    ScanSpace(const Cut &c, int64_t B, int64_t D)
-    {
-        Carver k;
-        const size_t n = c.segs > 1 ? (size_t)B * c.segs * D : 0;
-        pairs = k.take(sizeof(float2) * n);
-        state = k.take(sizeof(float) * n);
-        bytes = k.used;
-    }
-};
-
-template <class T, int CV> hipError_t scan_cv(const ScanArgs &a, const Cut &c, hipStream_t s)
+// Calls f with the kind of a scan.
+template <class T, class F> auto by_kind(int64_t D, F &&f)
 {
-    const ScanSpace w(c, a.B, a.D);
-    float2 *pairs = (float2 *)((char *)a.ws + w.pairs);
-    float *state = (float *)((char *)a.ws + w.state);
-    const unsigned grid = (unsigned)(a.B * c.slabs * c.segs);
-    const float *start = a.h0;
-    if (c.segs > 1) {
-        k_scan<T, CV, true><<<grid, kThreads, 0, s>>>(a, (int)c.slabs, c.segs, c.seg_pieces, nullptr, pairs);
-        k_scan_join<false><<<(unsigned)(a.B * ((a.D + 63) / 64)), 64 * kJoinWaves, 0, s>>>(pairs, a.h0, state, a.D,
-                                                                                        c.segs);
-        start = state;
-    }
-    k_scan<T, CV, false><<<grid, kThreads, 0, s>>>(a, (int)c.slabs, c.segs, c.seg_pieces, start, nullptr);
-    return hipGetLastError();
+    if constexpr (sizeof(T) == 2)
+        if (D > 64) return f(Kind<T, 2>{});
+    return f(Kind<T, 1>{});
 }
 
 template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
@@ -515,36 +572,41 @@ template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
         k_scan_few<T><<<(unsigned)((a.B * chunks + 255) / 256), 256, 0, s>>>(a, chunks);
         return hipGetLastError();
     }
-    const Cut c(a.B, a.T, a.D);
-    return c.cv == 2 ? scan_cv<T, 2>(a, c, s) : scan_cv<T, 1>(a, c, s);
-}
-
-template <class T, int CV> hipError_t scan_grad_cv(const ScanArgs &a, const Cut &c, hipStream_t s)
-{
-    const ScanSpace w(c, a.B, a.D);
-    float2 *pairs = (float2 *)((char *)a.ws + w.pairs);
-    float *state = (float *)((char *)a.ws + w.state);
-    const unsigned grid = (unsigned)(a.B * c.slabs * c.segs);
-    const float *end = a.dh_last;
-    if (c.segs > 1) {
-        k_scan_grad_pairs<T, CV><<<grid, kThreads, 0, s>>>(a, (int)c.slabs, c.segs, c.seg_pieces, pairs);
-        k_scan_join<true><<<(unsigned)(a.B * ((a.D + 63) / 64)), 64 * kJoinWaves, 0, s>>>(pairs, a.dh_last, state, a.D,
-                                                                                       c.segs);
-        end = state;
-    }
-    k_scan_grad<T, CV><<<grid, kThreads, 0, s>>>(a, (int)c.slabs, c.segs, c.seg_pieces, end);
-    return hipGetLastError();
+    return by_kind<T>(a.D, [&](auto kind) {
+        using K = decltype(kind);
+        const Layout<K> l(a.B, a.T, a.D);
+        k_scan<K><<<(unsigned)l.items, kThreads, 0, s>>>(a, l.start(a.ws, s));
+        return hipGetLastError();
+    });
 }
 
 template <class T> hipError_t scan_grad_t(const ScanArgs &a, hipStream_t s)
 {
-    const Cut c(a.B, a.T, a.D);
-    return c.cv == 2 ? scan_grad_cv<T, 2>(a, c, s) : scan_grad_cv<T, 1>(a, c, s);
+    return by_kind<T>(a.D, [&](auto kind) {
+        using K = decltype(kind);
+        const Layout<K> l(a.B, a.T, a.D);
+        k_scan_grad<K><<<(unsigned)l.items, kThreads, 0, s>>>(a, l.start(a.ws, s));
+        return hipGetLastError();
+    });
+}
+
+// The larger of what fp32 and 16-bit arrays take.
+template <class F> auto larger(int64_t D, F &&f)
+{
+    return std::max(by_kind<float>(D, f), by_kind<__bf16>(D, f));
 }
 
 } // namespace
 
-size_t scan_workspace(int64_t B, int64_t T, int64_t D) { return ScanSpace(Cut(B, T, D), B, D).bytes; }
+int64_t scan_items(int64_t B, int64_t T, int64_t D)
+{
+    return larger(D, [&](auto kind) { return Layout<decltype(kind)>(B, T, D).items; });
+}
+
+size_t scan_workspace(int64_t B, int64_t T, int64_t D)
+{
+    return larger(D, [&](auto kind) { return Layout<decltype(kind)>(B, T, D).bytes; });
+}
 
 hipError_t launch_scan(int32_t type, const ScanArgs &a, hipStream_t s)
 {

@@ -157,7 +157,9 @@ def test_gated_scan_and_gradients(ty, ragged, B, T, D):
     check("y", y, wy, rounded(wy, k * my, u, tiny))
     check("h_last", h, wh, rounded(wh, k * mh, U, 0))
     ws = before[:, ::seq.SCAN_PIECE]
-    check("states", states, ws, rounded(ws, k * (np.abs(ws) + mh.max() + 4), U, 0))
+    kept = np.arange(ws.shape[1])[None] * seq.SCAN_PIECE < (np.full(B, T) if n is None else n)[:, None]
+    states_kept = torch.where(torch.as_tensor(kept[..., None]).cuda(), states, torch.zeros((), device="cuda"))
+    check("states", states_kept, ws * kept[..., None], rounded(ws, k * (np.abs(ws) + mh.max() + 4), U, 0))
     assert torch.equal(y, seq.gated_scan(x, g, h0, lengths=lengths)[0])
     # gradients
     dy, dyv = put(rng.standard_normal((B, T, D)), dtype)
