@@ -5,7 +5,12 @@
 // their positions (a stable radix sort, so that each id's positions ascend),
 // which turns the sums into sums over runs of the sorted list: no atomics on
 // floating-point numbers, one fixed order, each row of dout read once and each
-// row of grad written once.
+// row of grad written once.  The list is cut into equal chunks, whatever the
+// runs, so that a few bitstrings that hold most shots of a peaked distribution
+// are no different from many that hold one each.
+#include <algorithm>
+#include <type_traits>
+
 #include "seq.h"
 #include "seq_device.h"
 
@@ -14,58 +19,76 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Columns go to lanes W at a time.  The last lane with any takes the row's last
+// W, some of them for the second time, so that every access is whole: the same
+// numbers are formed and written twice.  W is one 16-byte piece, or 1 for rows
+// shorter than that.
+template <int W> __device__ __forceinline__ int64_t column(int64_t nominal, int64_t D)
+{
+    return min(nominal, D - W);
+}
+
 // ------------------------------------------------------------------ lookup
-// L lanes share a row in 16-byte pieces; a group of them takes kRows rows at a
-// time, so that several reads are in flight behind the token reads.
+// L lanes share a row; a group of them takes kRows rows at a time, so that
+// several reads are in flight behind the token reads.
 constexpr int kRows = 4;
 
-template <class T, int L> __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a)
+template <class T, int W, int L> __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a)
 {
-    constexpr int VE = kVec<T>;
     const int lane = threadIdx.x % L;
     const int64_t group = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
     const int64_t i0 = group * kRows;
     if (i0 >= a.N) return;
-    const T *table = (const T *)a.table;
-    T *out = (T *)a.out;
     uint64_t t[kRows];
+    const T *from[kRows];
+    T *to[kRows];
 #pragma unroll
-    for (int r = 0; r < kRows; r++) t[r] = i0 + r < a.N ? a.tokens[i0 + r] : ~(uint64_t)0;
-    for (int64_t c = (int64_t)lane * VE; c < a.D; c += L * VE) {
-        const int n = (int)min((int64_t)VE, a.D - c);
-        float f[kRows][VE];
+    for (int r = 0; r < kRows; r++) {
+        // groups past the end repeat the last row; ids without a row read the first
+        const int64_t i = min(i0 + r, a.N - 1);
+        t[r] = a.tokens[i];
+        from[r] = (const T *)a.table + (int64_t)(t[r] < (uint64_t)a.V ? t[r] : 0) * a.ld_table;
+        to[r] = (T *)a.out + i * a.ld_out;
+    }
+    const bool some = a.V > 0;
+    for (int64_t c0 = (int64_t)lane * W; c0 < a.D; c0 += L * W) {
+        const int64_t c = column<W>(c0, a.D);
+        float f[kRows][W];
+#pragma unroll
+        for (int r = 0; r < kRows; r++)
+            if (some) load_vec<W>(from[r] + c, f[r]);
 #pragma unroll
         for (int r = 0; r < kRows; r++) {
-            if (t[r] < (uint64_t)a.V) load_part<VE>(table + (int64_t)t[r] * a.ld_table + c, n, f[r]);
-            else
+            // an id without a row gives zeros whatever the table holds
+            const bool on = t[r] < (uint64_t)a.V;
 #pragma unroll
-                for (int j = 0; j < VE; j++) f[r][j] = 0.f;
-        }
-#pragma unroll
-        for (int r = 0; r < kRows; r++) {
-            if (i0 + r >= a.N) break;
-            // an id without a row gives zeros whatever the scale
-            if (t[r] < (uint64_t)a.V)
-#pragma unroll
-                for (int j = 0; j < VE; j++) f[r][j] *= a.scale;
-            store_part<VE>(out + (i0 + r) * a.ld_out + c, n, f[r]);
+            for (int j = 0; j < W; j++) f[r][j] = on ? f[r][j] * a.scale : 0.f;
+            store_vec<W>(to[r] + c, f[r]);
         }
     }
 }
 
+// Calls f with the elements of a lane and the lanes of a row of D elements.
+template <class T, class F> void by_width(int64_t D, F &&f)
+{
+    using One = std::integral_constant<int, 1>;
+    using Whole = std::integral_constant<int, kVec<T>>;
+    const int64_t lanes = (D + kVec<T> - 1) / kVec<T>;
+    if (D < kVec<T>) f(One{}, std::integral_constant<int, 8>{});
+    else if (lanes <= 8) f(Whole{}, std::integral_constant<int, 8>{});
+    else if (lanes <= 16) f(Whole{}, std::integral_constant<int, 16>{});
+    else if (lanes <= 32) f(Whole{}, std::integral_constant<int, 32>{});
+    else f(Whole{}, std::integral_constant<int, 64>{});
+}
+
 template <class T> hipError_t embed_t(const EmbedArgs &a, hipStream_t s)
 {
-    const int64_t chunks = (a.D + kVec<T> - 1) / kVec<T>;
-    auto go = [&](auto kernel, int L) {
-        const int64_t groups = (a.N + kRows - 1) / kRows;
-        const int64_t per = kThreads / L;
-        kernel<<<(unsigned)((groups + per - 1) / per), kThreads, 0, s>>>(a);
-        return hipGetLastError();
-    };
-    if (chunks <= 8) return go(k_embed<T, 8>, 8);
-    if (chunks <= 16) return go(k_embed<T, 16>, 16);
-    if (chunks <= 32) return go(k_embed<T, 32>, 32);
-    return go(k_embed<T, 64>, 64);
+    by_width<T>(a.D, [&](auto w, auto l) {
+        constexpr int L = decltype(l)::value;
+        const int64_t groups = (a.N + kRows - 1) / kRows, per = kThreads / L;
+        k_embed<T, decltype(w)::value, L><<<(unsigned)((groups + per - 1) / per), kThreads, 0, s>>>(a);
+    });
+    return hipGetLastError();
 }
 
 // ------------------------------------------------------------------- sort
@@ -77,7 +100,7 @@ template <class T> hipError_t embed_t(const EmbedArgs &a, hipStream_t s)
 // of equal digits is kept at every level.
 constexpr int kSortThreads = 512;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortItems = 4096;
+constexpr int kSortItems = 2048;
 constexpr int kSortSteps = kSortItems / kSortThreads;
 constexpr int kMaxBits = 11;
 
@@ -98,309 +121,374 @@ __device__ __forceinline__ void wave_fence()
     __builtin_amdgcn_wave_barrier();
 }
 
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(v, d, 64);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
 // counts[digit][block]
 __global__ __launch_bounds__(kSortThreads) void k_sort_count(const uint64_t *tokens, const uint32_t *ids, int64_t N,
                                                             uint32_t V, int shift, int bits, uint32_t *counts)
 {
     extern __shared__ uint32_t bins[];
     const int nb = 1 << bits;
+    const int64_t i0 = (int64_t)blockIdx.x * kSortItems + threadIdx.x;
+    uint32_t id[kSortSteps];
+#pragma unroll
+    for (int k = 0; k < kSortSteps; k++)
+        id[k] = i0 + k * kSortThreads < N ? id_of(tokens, ids, i0 + k * kSortThreads, V) : 0;
     for (int d = threadIdx.x; d < nb; d += kSortThreads) bins[d] = 0;
     __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * kSortItems;
-    for (int k = 0; k < kSortSteps; k++) {
-        const int64_t i = i0 + k * kSortThreads + threadIdx.x;
-        if (i < N) atomicAdd(&bins[(id_of(tokens, ids, i, V) >> shift) & (nb - 1)], 1u);
-    }
+#pragma unroll
+    for (int k = 0; k < kSortSteps; k++)
+        if (i0 + k * kSortThreads < N) atomicAdd(&bins[(id[k] >> shift) & (nb - 1)], 1u);
     __syncthreads();
     for (int d = threadIdx.x; d < nb; d += kSortThreads) counts[(int64_t)d * gridDim.x + blockIdx.x] = bins[d];
 }
 
 // One wavefront per digit: counts[digit][*] become exclusive prefix sums over
 // the blocks, totals[digit] their sum.
-__global__ __launch_bounds__(64) void k_sort_scan(uint32_t *counts, int blocks, uint32_t *totals)
+__global__ __launch_bounds__(64) void k_sort_scan(uint32_t *counts, int blocks, uint32_t *totals, uint32_t *n_long)
 {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *n_long = 0;  // for k_embed_sums
     uint32_t *row = counts + (int64_t)blockIdx.x * blocks;
     const int lane = threadIdx.x;
     uint32_t carry = 0;
-    for (int b0 = 0; b0 < blocks; b0 += 64) {
-        const uint32_t v = b0 + lane < blocks ? row[b0 + lane] : 0;
-        uint32_t s = v;
+    for (int b0 = 0; b0 < blocks; b0 += 256) {
+        uint32_t v[4];
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(s, d, 64);
-            if (lane >= d) s += o;
+        for (int k = 0; k < 4; k++) v[k] = b0 + k * 64 + lane < blocks ? row[b0 + k * 64 + lane] : 0;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const uint32_t s = wave_prefix(v[k]);
+            if (b0 + k * 64 + lane < blocks) row[b0 + k * 64 + lane] = carry + s - v[k];
+            carry += __shfl(s, 63, 64);
         }
-        if (b0 + lane < blocks) row[b0 + lane] = carry + s - v;
-        carry += __shfl(s, 63, 64);
     }
     if (lane == 0) totals[blockIdx.x] = carry;
 }
 
+// PER: digits per thread, 2^bits <= PER * kSortThreads.
+template <int PER>
 __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(const uint64_t *tokens, const uint32_t *ids,
                                                               const uint32_t *pos, int64_t N, uint32_t V, int shift,
                                                               int bits, const uint32_t *counts, const uint32_t *totals,
                                                               uint32_t *ids_out, uint32_t *pos_out)
 {
-    // per wavefront and digit a counter, then one offset per digit
-    extern __shared__ uint32_t lds[];
-    __shared__ uint32_t wave_sum[kSortWaves];
-    const int nb = 1 << bits;
-    uint16_t *cnt = (uint16_t *)lds;
-    uint32_t *base = lds + (kSortWaves * nb) / 2;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int d = threadIdx.x; d < kSortWaves * nb / 2; d += kSortThreads) lds[d] = 0;
-    // exclusive prefix sums of the digits' totals: a contiguous part per thread
-    {
-        const int per = (nb + kSortThreads - 1) / kSortThreads;
-        const int d0 = threadIdx.x * per;
-        uint32_t own = 0;
-        for (int j = 0; j < per; j++) own += d0 + j < nb ? totals[d0 + j] : 0;
-        uint32_t s = own;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(s, d, 64);
-            if (lane >= d) s += o;
-        }
-        if (lane == 63) wave_sum[wave] = s;
-        __syncthreads();
-        uint32_t run = s - own;
-        for (int w = 0; w < wave; w++) run += wave_sum[w];
-        for (int j = 0; j < per; j++) {
-            const int d = d0 + j;
-            if (d < nb) {
-                base[d] = run + counts[(int64_t)d * gridDim.x + blockIdx.x];
-                run += totals[d];
-            }
-        }
-    }
-    __syncthreads();
+    constexpr int NB = PER * kSortThreads;
+    __shared__ uint16_t cnt[kSortWaves][NB];
+    __shared__ uint32_t base[NB], wave_sum[kSortWaves];
+    const int nb = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d0 = threadIdx.x * PER;
     const int64_t i0 = (int64_t)blockIdx.x * kSortItems + wave * (kSortSteps * 64);
-    uint16_t *mine = cnt + wave * nb;
-    uint32_t id[kSortSteps], at[kSortSteps];
-    uint16_t rank[kSortSteps];
+    uint32_t id[kSortSteps], at[kSortSteps], total[PER], before[PER];
 #pragma unroll
     for (int k = 0; k < kSortSteps; k++) {
         const int64_t i = i0 + k * 64 + lane;
-        const bool in = i < N;
-        id[k] = in ? id_of(tokens, ids, i, V) : 0;
-        at[k] = in ? (pos ? pos[i] : (uint32_t)i) : 0;
+        id[k] = i < N ? id_of(tokens, ids, i, V) : 0;
+        at[k] = i < N ? (pos ? pos[i] : (uint32_t)i) : 0;
     }
+#pragma unroll
+    for (int j = 0; j < PER; j++) {
+        total[j] = d0 + j < nb ? totals[d0 + j] : 0;
+        before[j] = d0 + j < nb ? counts[(int64_t)(d0 + j) * gridDim.x + blockIdx.x] : 0;
+    }
+    for (int d = threadIdx.x; d < kSortWaves * NB / 2; d += kSortThreads) ((uint32_t *)cnt)[d] = 0;
+    // exclusive prefix sums of the digits' totals
+    uint32_t own = 0;
+#pragma unroll
+    for (int j = 0; j < PER; j++) own += total[j];
+    const uint32_t s = wave_prefix(own);
+    if (lane == 63) wave_sum[wave] = s;
+    __syncthreads();
+    uint32_t run = s - own;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; w++) run += w < wave ? wave_sum[w] : 0;
+#pragma unroll
+    for (int j = 0; j < PER; j++) {
+        base[d0 + j] = run + before[j];
+        run += total[j];
+    }
+    uint16_t *mine = cnt[wave];
+    uint32_t rank[kSortSteps];
 #pragma unroll
     for (int k = 0; k < kSortSteps; k++) {
         const bool in = i0 + k * 64 + lane < N;
         const int d = (id[k] >> shift) & (nb - 1);
         uint64_t same = __ballot(in);
         for (int b = 0; b < bits; b++) {
-            const uint64_t m = __ballot((d >> b) & 1);
-            same &= ((d >> b) & 1) ? m : ~m;
+            const bool set = (d >> b) & 1;
+            const uint64_t m = __ballot(set);
+            same &= set ? m : ~m;
         }
-        const int before = __popcll(same & (((uint64_t)1 << lane) - 1));
+        const int lower = __popcll(same & (((uint64_t)1 << lane) - 1));
         // all lanes read the counters before the first lane of each digit moves
         // its counter on, and those writes come before the next step's reads
         const int seen = in ? mine[d] : 0;
-        rank[k] = (uint16_t)(seen + before);
+        rank[k] = seen + lower;
         wave_fence();
-        if (in && before == 0) mine[d] = (uint16_t)(seen + __popcll(same));
+        if (in && lower == 0) mine[d] = (uint16_t)(seen + __popcll(same));
         wave_fence();
     }
     __syncthreads();
     for (int d = threadIdx.x; d < nb; d += kSortThreads) {
-        uint32_t run = 0;
+        uint32_t sum = base[d];
+#pragma unroll
         for (int w = 0; w < kSortWaves; w++) {
-            const uint16_t c = cnt[w * nb + d];
-            cnt[w * nb + d] = (uint16_t)run;
-            run += c;
+            const uint16_t c = cnt[w][d];
+            cnt[w][d] = (uint16_t)(sum - base[d]);
+            sum += c;
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kSortSteps; k++) {
+    for (int k = 0; k < kSortSteps; k++)
         if (i0 + k * 64 + lane < N) {
             const int d = (id[k] >> shift) & (nb - 1);
             const uint32_t o = base[d] + mine[d] + rank[k];
             ids_out[o] = id[k];
             pos_out[o] = at[k];
         }
-    }
 }
 
 // ------------------------------------------------------------------- sums
-// Runs of equal ids in the sorted list.  A run of at most kShort places is
-// summed by one group of lanes.  A longer one (a few bitstrings hold most shots
-// of a peaked distribution) is cut into pieces of `piece` places, each summed
-// into a row of fp32 partial sums of its own, which k_embed_join adds up.
-constexpr int kShort = 64;
-constexpr int kAhead = 8;  // rows in flight per group
+// The sorted list is cut into chunks.  A group of L lanes walks a chunk, kAhead
+// rows in flight, and adds up its runs of equal ids.  A run that goes at most
+// kOver places past the chunk it begins in is finished there, and passed over by
+// the group of the next chunk.  Longer runs leave a partial sum per chunk, in
+// row 2c + 1 where they begin and 2c where they go on, and k_embed_join adds
+// these up; the chunks that long runs begin in are entered into a list (the
+// order of the entries is a matter of chance, what is summed is not).
+constexpr int kAhead = 8, kOver = 64;
 
-struct LongRun {
-    uint32_t v, start, count, first;  // first: its first row of partial sums
+struct SumArgs {
+    EmbedGradArgs a;
+    const uint32_t *ids, *pos;
+    int64_t chunks;
+    int chunk, chunk_blocks;
+    float *partial;
+    uint32_t *n_long, *longs;
 };
 
-// starts[v], v in [0, V]: the first place of an id >= v in the sorted list.
-// Long runs are entered into a list; `tally` holds (runs << 32 | pieces), one
-// addition per entry, so that the entries' first pieces ascend.  Where an entry
-// lands depends on the order of these additions, what is summed does not.
-__global__ __launch_bounds__(kThreads) void k_embed_runs(const uint32_t *ids, int64_t N, int64_t V, int piece,
-                                                        uint32_t *starts, unsigned long long *tally, LongRun *runs)
+// Whether the run of `id`, which goes on at place e, the end of a chunk, goes
+// on for more than kOver places.
+__device__ __forceinline__ bool goes_far(const SumArgs &s, int64_t e, uint32_t id)
 {
-    const int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (v > V) return;
-    auto place = [&](int64_t id) {
-        int64_t lo = 0, hi = N;
-        while (lo < hi) {
-            const int64_t m = (lo + hi) >> 1;
-            if (ids[m] < (uint32_t)id) lo = m + 1;
-            else hi = m;
-        }
-        return (uint32_t)lo;
-    };
-    const uint32_t b = place(v);
-    starts[v] = b;
-    if (v == V) return;
-    // a run longer than kShort has its id kShort places on
-    if ((int64_t)b + kShort < N && ids[b + kShort] == (uint32_t)v) {
-        const uint32_t count = place(v + 1) - b;
-        const uint32_t np = (count + piece - 1) / piece;
-        const unsigned long long t = atomicAdd(tally, ((unsigned long long)1 << 32) | np);
-        runs[t >> 32] = LongRun{(uint32_t)v, b, count, (uint32_t)t};
-    }
+    return e + kOver < s.a.N && s.ids[e + kOver] == id;
 }
 
-// Sum of the rows at places [b, e) of the list, in their order.
-template <class T>
-__device__ __forceinline__ void sum_rows(const T *dout, int64_t ld, const uint32_t *pos, uint32_t b, uint32_t e, int n,
-                                         float (&acc)[kVec<T>])
+template <class T, int W>
+__device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t c, int64_t col, bool first_lane)
 {
-    constexpr int VE = kVec<T>;
+    const EmbedGradArgs &a = s.a;
+    const uint32_t N = (uint32_t)a.N, V = (uint32_t)a.V;
+    const uint32_t b = (uint32_t)(c * s.chunk), e = min(b + (uint32_t)s.chunk, N);
+    const T *dout = (const T *)a.dout + col;
+    uint32_t cur = s.ids[b], i = b, end = e;
+    bool began = b == 0 || s.ids[b - 1] != cur;
+    if (!began) {
+        // passed over, unless it is long: by where it began and how far it goes
+        const bool there = b == (uint32_t)s.chunk || s.ids[b - s.chunk - 1] != cur;
+        if (there && !goes_far(s, b, cur)) {
+            began = true;
+            while (i < e && s.ids[i] == cur) i++;
+            if (i == e) return;
+            cur = s.ids[i];
+        }
+    }
+    if (cur >= V) return;
+    const uint32_t last = s.ids[e - 1];
+    bool whole = true;  // the chunk's last run ends here
+    if (last < V && e < N && s.ids[e] == last) {
+        whole = !goes_far(s, e, last) && (s.ids[b] != last || b == 0 || s.ids[b - 1] != last);
+        if (whole) end = min(e + (uint32_t)kOver, N);
+    }
+    float acc[W];
 #pragma unroll
-    for (int j = 0; j < VE; j++) acc[j] = 0.f;
-    for (uint32_t i = b; i < e; i += kAhead) {
-        float f[kAhead][VE];
+    for (int j = 0; j < W; j++) acc[j] = 0.f;
+    auto flush = [&](bool ended) {
+        if (began && ended) {
+#pragma unroll
+            for (int j = 0; j < W; j++) acc[j] *= a.scale;
+            store_vec<W>((T *)a.grad + (int64_t)cur * a.ld_grad + col, acc);
+        } else {
+            store_vec<W>(s.partial + (2 * c + (began ? 1 : 0)) * a.D + col, acc);
+            if (began && first_lane) s.longs[atomicAdd(s.n_long, 1u)] = (uint32_t)c;
+        }
+#pragma unroll
+        for (int j = 0; j < W; j++) acc[j] = 0.f;
+    };
+    for (; i < end; i += kAhead) {
+        uint32_t id[kAhead], from[kAhead];
+        float f[kAhead][W];
 #pragma unroll
         for (int r = 0; r < kAhead; r++) {
-            if (i + r < e) load_part<VE>(dout + (int64_t)pos[i + r] * ld, n, f[r]);
-            else
-#pragma unroll
-                for (int j = 0; j < VE; j++) f[r][j] = 0.f;
+            const uint32_t k = min(i + r, end - 1);
+            id[r] = s.ids[k];
+            from[r] = s.pos[k];
         }
 #pragma unroll
-        for (int r = 0; r < kAhead; r++)
+        for (int r = 0; r < kAhead; r++) load_vec<W>(dout + (int64_t)from[r] * a.ld_dout, f[r]);
 #pragma unroll
-            for (int j = 0; j < VE; j++) acc[j] += f[r][j];
+        for (int r = 0; r < kAhead; r++) {
+            if (i + r >= end) break;
+            if (id[r] != cur) {
+                flush(true);
+                began = true;
+                cur = id[r];
+                if (cur >= V || i + r >= e) return;  // past the chunk only its last run
+            }
+#pragma unroll
+            for (int j = 0; j < W; j++) acc[j] += f[r][j];
+        }
     }
+    flush(whole);
 }
 
-// Workgroups [0, piece_blocks) sum the pieces of long runs, the others the
-// short runs, kThreads / L rows of grad each; absent ids get zeros.
-template <class T, int L>
-__global__ __launch_bounds__(kThreads) void k_embed_sums(EmbedGradArgs a, const uint32_t *pos, const uint32_t *starts,
-                                                        const unsigned long long *tally, const LongRun *runs,
-                                                        float *partial, int piece, int piece_blocks)
+// The first `chunk_blocks` workgroups sum chunks, the others write the zeros of
+// ids that no token has: each of their wavefronts looks 64 ids up in the list.
+template <class T, int W, int L> __global__ __launch_bounds__(kThreads) void k_embed_sums(SumArgs s)
 {
-    constexpr int VE = kVec<T>, G = kThreads / L;
-    __shared__ float part[G][L * VE];
-    const int lane = threadIdx.x % L, g = threadIdx.x / L;
-    const T *dout = (const T *)a.dout;
-    if ((int)blockIdx.x >= piece_blocks) {
-        const int64_t v = (int64_t)(blockIdx.x - piece_blocks) * G + g;
-        if (v >= a.V) return;
-        const uint32_t b = starts[v], e = starts[v + 1];
-        if (e - b > kShort) return;
-        for (int64_t c = (int64_t)lane * VE; c < a.D; c += L * VE) {
-            const int n = (int)min((int64_t)VE, a.D - c);
-            float acc[VE];
-            sum_rows<T>(dout + c, a.ld_dout, pos, b, e, n, acc);
-            if (b < e)
-#pragma unroll
-                for (int j = 0; j < VE; j++) acc[j] *= a.scale;
-            store_part<VE>((T *)a.grad + v * a.ld_grad + c, n, acc);
-        }
+    constexpr int G = kThreads / L;
+    const EmbedGradArgs &a = s.a;
+    if ((int)blockIdx.x < s.chunk_blocks) {
+        int g = threadIdx.x / L;
+        if constexpr (L == 64) g = __builtin_amdgcn_readfirstlane(g);  // addresses and branches are scalar
+        const int64_t c = (int64_t)blockIdx.x * G + g;
+        if (c >= s.chunks) return;
+        for (int64_t c0 = (int64_t)(threadIdx.x % L) * W; c0 < a.D; c0 += L * W)
+            sum_chunk<T, W>(s, c, column<W>(c0, a.D), c0 == 0);
         return;
     }
-    const unsigned long long t = *tally;
-    const uint32_t n_runs = (uint32_t)(t >> 32), n_pieces = (uint32_t)t;
-    for (uint32_t p = blockIdx.x; p < n_pieces; p += piece_blocks) {
-        uint32_t lo = 0, hi = n_runs;  // the last run with first <= p
-        while (hi - lo > 1) {
-            const uint32_t m = (lo + hi) >> 1;
-            if (runs[m].first <= p) lo = m;
-            else hi = m;
-        }
-        const LongRun r = runs[lo];
-        const uint32_t b0 = r.start + (p - r.first) * piece;
-        const uint32_t e0 = min(b0 + (uint32_t)piece, r.start + r.count);
-        // the groups take equal parts of the piece; their sums are added in order
-        const uint32_t per = (e0 - b0 + G - 1) / G;
-        const uint32_t b = min(b0 + g * per, e0), e = min(b + per, e0);
-        for (int64_t c0 = 0; c0 < a.D; c0 += L * VE) {
-            const int64_t c = c0 + lane * VE;
-            const int n = (int)max((int64_t)0, min((int64_t)VE, a.D - c));
-            float acc[VE];
-            sum_rows<T>(dout + (n ? c : 0), a.ld_dout, pos, b, n ? e : b, n, acc);
-#pragma unroll
-            for (int j = 0; j < VE; j++) part[g][lane * VE + j] = acc[j];
-            __syncthreads();
-            for (int j = threadIdx.x; j < L * VE; j += kThreads) {
-                float s = 0.f;
-                for (int k = 0; k < G; k++) s += part[k][j];
-                if (c0 + j < a.D) partial[(int64_t)p * a.D + c0 + j] = s;
-            }
-            __syncthreads();
-        }
+    const int lane = threadIdx.x & 63;
+    const int64_t v0 = ((int64_t)(blockIdx.x - s.chunk_blocks) * (kThreads / 64) + (threadIdx.x >> 6)) * 64;
+    const uint32_t v = (uint32_t)min(v0 + lane, a.V - 1);
+    uint32_t lo = 0, hi = (uint32_t)a.N;
+    while (lo < hi) {
+        const uint32_t m = (lo + hi) >> 1;
+        if (s.ids[m] < v) lo = m + 1;
+        else hi = m;
+    }
+    const bool absent = v0 + lane < a.V && (lo == (uint32_t)a.N || s.ids[lo] != v);
+    const float zero[W] = {};
+    for (uint64_t m = __ballot(absent); m; m &= m - 1) {
+        T *row = (T *)a.grad + (v0 + __ffsll((unsigned long long)m) - 1) * a.ld_grad;
+        for (int64_t c0 = (int64_t)lane * W; c0 < a.D; c0 += 64 * W) store_vec<W>(row + column<W>(c0, a.D), zero);
     }
 }
 
-// The partial sums of each long run, added up: the workgroup's wavefronts take
-// equal parts of the run's pieces, 64 columns at a time.
+// The long runs: the partial sum of the chunk a run begins in and those of the
+// chunks after it that begin with the same id.  64 columns per workgroup; its
+// wavefronts take equal parts of those chunks.
 constexpr int kJoinWaves = 16;
-template <class T>
-__global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradArgs a, const unsigned long long *tally,
-                                                               const LongRun *runs, const float *partial, int piece)
+template <class T> __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(SumArgs s)
 {
     __shared__ float part[kJoinWaves][64];
+    const EmbedGradArgs &a = s.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t n_runs = (uint32_t)(*tally >> 32);
-    const int64_t c = (int64_t)blockIdx.y * 64 + lane;
-    for (uint32_t k = blockIdx.x; k < n_runs; k += gridDim.x) {
-        const LongRun r = runs[k];
-        const uint32_t np = (r.count + piece - 1) / piece;
-        const uint32_t per = (np + kJoinWaves - 1) / kJoinWaves;
-        const uint32_t b = min(wave * per, np), e = min(b + per, np);
-        float s = 0.f;
-        if (c < a.D)
-#pragma unroll 8
-            for (uint32_t p = b; p < e; p++) s += partial[(int64_t)(r.first + p) * a.D + c];
-        part[wave][lane] = s;
+    const uint32_t n_long = *s.n_long;
+    for (uint32_t q = blockIdx.x; q < n_long; q += gridDim.x) {
+        const int64_t c = s.longs[q];
+        const uint32_t id = s.ids[(c + 1) * s.chunk];
+        // n: the chunks after c that begin with it, 64 places tried at a time
+        int64_t n = 0, hi = s.chunks - c - 1;
+        while (n < hi) {
+            const int64_t step = (hi - n + 63) / 64, k = n + lane * step;
+            const uint64_t m = __ballot(k < hi && s.ids[(c + 1 + min(k, hi - 1)) * s.chunk] == id);
+            const int yes = __popcll(m);  // the first `yes` places begin with it
+            if (yes == 0) break;
+            hi = min(hi, n + yes * step);
+            n += (yes - 1) * step + 1;
+        }
+        const int64_t col = (int64_t)blockIdx.y * 64 + lane, per = (n + kJoinWaves - 1) / kJoinWaves;
+        const int64_t k0 = min(wave * per, n), k1 = min(k0 + per, n);
+        float t = 0.f;
+        if (col < a.D) {
+            if (wave == 0) t = s.partial[(2 * c + 1) * a.D + col];
+#pragma unroll 16
+            for (int64_t k = k0; k < k1; k++) t += s.partial[2 * (c + 1 + k) * a.D + col];
+        }
+        part[wave][lane] = t;
         __syncthreads();
-        if (wave == 0 && c < a.D) {
-            float t = 0.f;
+        if (wave == 0 && col < a.D) {
+            t = 0.f;
 #pragma unroll
             for (int w = 0; w < kJoinWaves; w++) t += part[w][lane];
-            ((T *)a.grad)[(int64_t)r.v * a.ld_grad + c] = (T)(t * a.scale);
+            ((T *)a.grad)[(int64_t)id * a.ld_grad + col] = (T)(t * a.scale);
         }
         __syncthreads();
     }
 }
 
-__global__ void k_clear_tally(unsigned long long *tally) { *tally = 0; }
+// ------------------------------------------------------------- a few tokens
+// Up to kFewTokens tokens need no sort: a wavefront per row of grad compares
+// its id with all of them.  One launch in place of five or eight.
+constexpr int kFewTokens = 512;
+template <class T, int W> __global__ __launch_bounds__(kThreads) void k_embed_few(EmbedGradArgs a)
+{
+    __shared__ uint32_t tok[kFewTokens];
+    const int lane = threadIdx.x & 63, N = (int)a.N;
+    for (int i = threadIdx.x; i < (N + 63) / 64 * 64; i += kThreads)
+        tok[i] = i < N ? id_of(a.tokens, nullptr, i, (uint32_t)a.V) : (uint32_t)a.V;
+    __syncthreads();
+    for (int64_t v = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); v < a.V;
+         v += (int64_t)gridDim.x * (kThreads / 64))
+        for (int64_t c0 = 0; c0 < a.D; c0 += 64 * W) {
+            // lanes past the last column sum it again
+            const int64_t col = column<W>(c0 + lane * W, a.D);
+            const T *dout = (const T *)a.dout + col;
+            float acc[W];
+#pragma unroll
+            for (int j = 0; j < W; j++) acc[j] = 0.f;
+            for (int t0 = 0; t0 < N; t0 += 64) {
+                uint64_t m = __ballot(tok[t0 + lane] == (uint32_t)v);
+                while (m) {
+                    float f[kAhead][W];
+                    int n = 0, at = 0;
+#pragma unroll
+                    for (int r = 0; r < kAhead; r++) {
+                        if (m) at = t0 + __ffsll((unsigned long long)m) - 1, n = r + 1;
+                        m &= m - 1;
+                        load_vec<W>(dout + (int64_t)at * a.ld_dout, f[r]);
+                    }
+#pragma unroll
+                    for (int r = 0; r < kAhead; r++)
+                        if (r < n)
+#pragma unroll
+                            for (int j = 0; j < W; j++) acc[j] += f[r][j];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < W; j++) acc[j] = acc[j] == 0.f ? 0.f : acc[j] * a.scale;
+            store_vec<W>((T *)a.grad + v * a.ld_grad + col, acc);
+        }
+}
 
 // What a gradient call needs beside its arrays.
 struct GradPlan {
-    int bits, passes, piece;
-    int64_t blocks, max_runs, max_pieces;
-    size_t ids[2], pos[2], counts, totals, starts, tally, runs, partial, bytes;
+    bool few;
+    int bits, passes, chunk;
+    int64_t blocks, chunks;
+    size_t ids[2], pos[2], counts, totals, partial, n_long, longs, bytes;
     GradPlan(int64_t V, int64_t D, int64_t N)
     {
+        bytes = 0;
+        few = N <= kFewTokens;
+        if (few) return;
         int all = 1;
         while (((int64_t)1 << all) <= V) all++;  // ids 0 .. V
         passes = (all + kMaxBits - 1) / kMaxBits;
         bits = (all + passes - 1) / passes;
         blocks = (N + kSortItems - 1) / kSortItems;
-        // pieces of a run: at most about a thousand
-        piece = 128;
-        while (piece < 4096 && (int64_t)piece * 1024 < N) piece *= 2;
-        max_runs = N / (kShort + 1);
-        max_pieces = max_runs ? N / piece + max_runs : 0;
+        // About four thousand chunks fill the chip; sums of more, shorter ones
+        // would only add to the partial sums.
+        chunk = (int)std::max<int64_t>(16, (N / 4096 + kAhead - 1) / kAhead * kAhead);
+        chunks = (N + chunk - 1) / chunk;
         Carver c;
         for (int k = 0; k < 2; k++) {
             ids[k] = c.take(4 * N);
@@ -408,10 +496,9 @@ struct GradPlan {
         }
         counts = c.take(((size_t)4 << bits) * blocks);
         totals = c.take((size_t)4 << bits);
-        starts = c.take(4 * (V + 1));
-        tally = c.take(8);
-        runs = c.take(sizeof(LongRun) * max_runs);
-        partial = c.take(sizeof(float) * max_pieces * D);
+        partial = c.take(sizeof(float) * 2 * chunks * D);
+        n_long = c.take(sizeof(uint32_t));
+        longs = c.take(sizeof(uint32_t) * chunks);
         bytes = c.used;
     }
 };
@@ -419,6 +506,13 @@ struct GradPlan {
 template <class T> hipError_t embed_grad_t(const EmbedGradArgs &a, hipStream_t s)
 {
     const GradPlan p(a.V, a.D, a.N);
+    if (p.few) {
+        const int64_t blocks = (a.V + kThreads / 64 - 1) / (kThreads / 64);
+        by_width<T>(a.D, [&](auto w, auto) {
+            k_embed_few<T, decltype(w)::value><<<(unsigned)std::min<int64_t>(blocks, 8192), kThreads, 0, s>>>(a);
+        });
+        return hipGetLastError();
+    }
     char *ws = (char *)a.ws;
     uint32_t *ids[2], *pos[2];
     for (int k = 0; k < 2; k++) {
@@ -426,42 +520,33 @@ template <class T> hipError_t embed_grad_t(const EmbedGradArgs &a, hipStream_t s
         pos[k] = (uint32_t *)(ws + p.pos[k]);
     }
     uint32_t *counts = (uint32_t *)(ws + p.counts), *totals = (uint32_t *)(ws + p.totals);
-    uint32_t *starts = (uint32_t *)(ws + p.starts);
-    unsigned long long *tally = (unsigned long long *)(ws + p.tally);
-    LongRun *runs = (LongRun *)(ws + p.runs);
-    float *partial = (float *)(ws + p.partial);
     const size_t nb = (size_t)1 << p.bits;
-    int cur = 0;
+    const uint32_t V = (uint32_t)a.V;
     for (int k = 0; k < p.passes; k++) {
         const int shift = k * p.bits;
-        const uint32_t *in_ids = k ? ids[cur] : nullptr, *in_pos = k ? pos[cur] : nullptr;
-        if (p.blocks) {
-            k_sort_count<<<p.blocks, kSortThreads, 4 * nb, s>>>(a.tokens, in_ids, a.N, (uint32_t)a.V, shift, p.bits,
-                                                               counts);
-            k_sort_scan<<<nb, 64, 0, s>>>(counts, (int)p.blocks, totals);
-            k_sort_scatter<<<p.blocks, kSortThreads, 2 * kSortWaves * nb + 4 * nb, s>>>(
-                a.tokens, in_ids, in_pos, a.N, (uint32_t)a.V, shift, p.bits, counts, totals, ids[1 - cur],
-                pos[1 - cur]);
-        }
-        cur = 1 - cur;
+        const uint32_t *in_ids = k ? ids[(k - 1) & 1] : nullptr, *in_pos = k ? pos[(k - 1) & 1] : nullptr;
+        k_sort_count<<<p.blocks, kSortThreads, 4 * nb, s>>>(a.tokens, in_ids, a.N, V, shift, p.bits, counts);
+        k_sort_scan<<<nb, 64, 0, s>>>(counts, (int)p.blocks, totals, (uint32_t *)(ws + p.n_long));
+        auto scatter = [&](auto kernel) {
+            kernel<<<p.blocks, kSortThreads, 0, s>>>(a.tokens, in_ids, in_pos, a.N, V, shift, p.bits, counts, totals,
+                                                     ids[k & 1], pos[k & 1]);
+        };
+        if (nb <= kSortThreads) scatter(k_sort_scatter<1>);
+        else if (nb <= 2 * kSortThreads) scatter(k_sort_scatter<2>);
+        else scatter(k_sort_scatter<4>);
     }
-    k_clear_tally<<<1, 1, 0, s>>>(tally);
-    k_embed_runs<<<(a.V + kThreads) / kThreads, kThreads, 0, s>>>(ids[cur], a.N, a.V, p.piece, starts, tally, runs);
-    const int64_t chunks = (a.D + kVec<T> - 1) / kVec<T>;
-    const int pb = (int)(p.max_pieces < 2048 ? p.max_pieces : 2048);
-    auto go = [&](auto kernel, int L) {
-        const int64_t per = kThreads / L;
-        kernel<<<(unsigned)(pb + (a.V + per - 1) / per), kThreads, 0, s>>>(a, pos[cur], starts, tally, runs, partial,
-                                                                          p.piece, pb);
-    };
-    if (chunks <= 8) go(k_embed_sums<T, 8>, 8);
-    else if (chunks <= 16) go(k_embed_sums<T, 16>, 16);
-    else if (chunks <= 32) go(k_embed_sums<T, 32>, 32);
-    else go(k_embed_sums<T, 64>, 64);
-    if (p.max_runs) {
-        const dim3 grid((unsigned)(p.max_runs < 256 ? p.max_runs : 256), (unsigned)((a.D + 63) / 64));
-        k_embed_join<T><<<grid, kJoinWaves * 64, 0, s>>>(a, tally, runs, partial, p.piece);
-    }
+    SumArgs u{a, ids[(p.passes - 1) & 1], pos[(p.passes - 1) & 1], p.chunks, p.chunk, 0, (float *)(ws + p.partial),
+              (uint32_t *)(ws + p.n_long), (uint32_t *)(ws + p.longs)};
+    by_width<T>(a.D, [&](auto w, auto l) {
+        constexpr int L = decltype(l)::value;
+        const int64_t per = kThreads / L, zeros = (a.V + kThreads - 1) / kThreads;
+        u.chunk_blocks = (int)((p.chunks + per - 1) / per);
+        k_embed_sums<T, decltype(w)::value, L><<<(unsigned)(u.chunk_blocks + zeros), kThreads, 0, s>>>(u);
+    });
+    // a long run has more than kOver places
+    const int64_t most = a.N / kOver;
+    k_embed_join<T><<<dim3((unsigned)std::min<int64_t>(most, 128), (unsigned)((a.D + 63) / 64)), kJoinWaves * 64, 0,
+                     s>>>(u);
     return hipGetLastError();
 }
 
