@@ -38,55 +38,91 @@ template <int L> __device__ __forceinline__ float row_sum(float v, float (*red)[
     }
 }
 
-template <class T, int L, int C> __global__ __launch_bounds__(kThreadsOf<L>) void k_norm(NormArgs a)
+// Which columns a lane holds: C pieces of W elements, L pieces apart.  A piece
+// that would go past the row's end is the row's last W columns instead, so
+// that every access is whole and no branch stands between the reads; the
+// columns it shares with the lane before it count there alone, and are formed
+// and written twice.  W is one 16-byte piece, or 1 for rows shorter than that.
+template <int L, int C, int W> struct Columns {
+    int64_t at[C];
+    int skip[C];  // elements that do not count here (W: the lane has none)
+    __device__ explicit Columns(int64_t D)
+    {
+        const int lane = threadIdx.x % L;
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+            const int64_t nominal = (int64_t)(c * L + lane) * W;
+            at[c] = min(nominal, D - W);
+            skip[c] = (int)min(nominal - at[c], (int64_t)W);
+        }
+    }
+    // v where element j of piece c counts, else 0
+    __device__ float count(int c, int j, float v) const { return j >= skip[c] ? v : 0.f; }
+};
+
+template <class T, int C, int W> struct Pieces {
+    T v[C][W];
+    template <class Cols> __device__ __forceinline__ void load(const T *row, const Cols &k)
+    {
+#pragma unroll
+        for (int c = 0; c < C; c++) __builtin_memcpy(v[c], row + k.at[c], sizeof v[c]);
+    }
+};
+
+// Workgroups walk the rows, the weights in registers, the next row's reads on
+// their way while a row is worked on.
+template <class T, int L, int C, int W> __global__ __launch_bounds__(kThreadsOf<L>) void k_norm(NormArgs a)
 {
-    constexpr int VE = kVec<T>, R = kThreadsOf<L> / L;
+    constexpr int R = kThreadsOf<L> / L;
     __shared__ float red[2][16];
     int turn = 0;
+    const Columns<L, C, W> k(a.D);
     const int lane = threadIdx.x % L;
-    const int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L;
-    const bool in = row < a.N;
-    const T *x = (const T *)a.x + (in ? row : 0) * a.ld_x;
-    float f[C][VE];
-    int n[C];
-    float s = 0.f;
+    float w[C][W], b[C][W];
 #pragma unroll
     for (int c = 0; c < C; c++) {
-        const int64_t at = (int64_t)(c * L + lane) * VE;
-        n[c] = in ? (int)max((int64_t)0, min((int64_t)VE, a.D - at)) : 0;
-        load_part<VE>(x + (n[c] ? at : 0), n[c], f[c]);
+        load_vec<W>((const T *)a.weight + k.at[c], w[c]);
 #pragma unroll
-        for (int j = 0; j < VE; j++) s += f[c][j];
+        for (int j = 0; j < W; j++) b[c][j] = 0.f;
+        if (a.bias) load_vec<W>((const T *)a.bias + k.at[c], b[c]);
     }
-    const float mean = row_sum<L>(s, red, turn) / (float)a.D;
-    float q = 0.f;
+    const float inv = 1.f / (float)a.D;
+    const int64_t step = (int64_t)gridDim.x * R;
+    int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L;
+    Pieces<T, C, W> x;
+    x.load((const T *)a.x + min(row, a.N - 1) * a.ld_x, k);
+    // all threads of a workgroup take the same number of turns
+    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.N; r0 += step, row += step) {
+        float f[C][W], s = 0.f, q = 0.f;
 #pragma unroll
-    for (int c = 0; c < C; c++)
+        for (int c = 0; c < C; c++)
 #pragma unroll
-        for (int j = 0; j < VE; j++) {
-            f[c][j] -= mean;
-            if (j < n[c]) q = fmaf(f[c][j], f[c][j], q);
+            for (int j = 0; j < W; j++) {
+                f[c][j] = (float)x.v[c][j];
+                s += k.count(c, j, f[c][j]);
+            }
+        if (r0 + step < a.N) x.load((const T *)a.x + min(row + step, a.N - 1) * a.ld_x, k);
+        const float mean = row_sum<L>(s, red, turn) * inv;
+#pragma unroll
+        for (int c = 0; c < C; c++)
+#pragma unroll
+            for (int j = 0; j < W; j++) {
+                f[c][j] -= mean;
+                q += k.count(c, j, f[c][j] * f[c][j]);
+            }
+        const float rstd = 1.f / sqrtf(row_sum<L>(q, red, turn) * inv + a.eps);
+        if (row >= a.N) continue;
+        if (a.mean && lane == 0) {
+            a.mean[row] = mean;
+            a.rstd[row] = rstd;
         }
-    const float rstd = 1.f / sqrtf(row_sum<L>(q, red, turn) / (float)a.D + a.eps);
-    if (!in) return;
-    if (a.mean && lane == 0) {
-        a.mean[row] = mean;
-        a.rstd[row] = rstd;
-    }
-    T *y = (T *)a.y + row * a.ld_y;
+        T *y = (T *)a.y + row * a.ld_y;
 #pragma unroll
-    for (int c = 0; c < C; c++) {
-        if (!n[c]) continue;
-        const int64_t at = (int64_t)(c * L + lane) * VE;
-        float w[VE], b[VE];
-        load_part<VE>((const T *)a.weight + at, n[c], w);
-        if (a.bias) load_part<VE>((const T *)a.bias + at, n[c], b);
-        else
+        for (int c = 0; c < C; c++) {
 #pragma unroll
-            for (int j = 0; j < VE; j++) b[j] = 0.f;
-#pragma unroll
-        for (int j = 0; j < VE; j++) f[c][j] = fmaf(f[c][j] * rstd, w[j], b[j]);
-        store_part<VE>(y + at, n[c], f[c]);
+            for (int j = 0; j < W; j++) f[c][j] = fmaf(f[c][j] * rstd, w[c][j], b[c][j]);
+            if (k.skip[c] < W) store_vec<W>(y + k.at[c], f[c]);
+        }
     }
 }
 
@@ -135,62 +171,66 @@ template <class T> __global__ __launch_bounds__(kWide) void k_norm_wide(NormArgs
 }
 
 // ---------------------------------------------------------------- backward
-// Workgroup b takes rows b R, b R + R, ... (R rows at a time, `gridDim.x * R`
-// apart) and leaves its sums of dy xh and dy in part[b][2][D].
-template <class T, int L, int C>
+// Workgroup b takes R rows at a time, gridDim.x R apart, and leaves its sums of
+// dy xh and dy in part[b][2][D].
+template <class T, int L, int C, int W>
 __global__ __launch_bounds__(kThreadsOf<L>) void k_norm_grad(NormArgs a, float *part)
 {
-    constexpr int VE = kVec<T>, R = kThreadsOf<L> / L;
+    constexpr int R = kThreadsOf<L> / L;
     __shared__ float red[2][16];
-    __shared__ float join[R > 1 ? R : 1][R > 1 ? L * VE : 1];
+    __shared__ float join[R > 1 ? R : 1][R > 1 ? L * W : 1];
     int turn = 0;
+    const Columns<L, C, W> k(a.D);
     const int lane = threadIdx.x % L, g = threadIdx.x / L;
-    int n[C];
-    float w[C][VE], dw[C][VE], db[C][VE];
+    float w[C][W], dw[C][W], db[C][W];
 #pragma unroll
     for (int c = 0; c < C; c++) {
-        const int64_t at = (int64_t)(c * L + lane) * VE;
-        n[c] = (int)max((int64_t)0, min((int64_t)VE, a.D - at));
-        load_part<VE>((const T *)a.weight + (n[c] ? at : 0), n[c], w[c]);
+        load_vec<W>((const T *)a.weight + k.at[c], w[c]);
 #pragma unroll
-        for (int j = 0; j < VE; j++) dw[c][j] = db[c][j] = 0.f;
+        for (int j = 0; j < W; j++) dw[c][j] = db[c][j] = 0.f;
     }
     const float inv = 1.f / (float)a.D;
-    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.N; r0 += (int64_t)gridDim.x * R) {
-        const int64_t row = r0 + g;
+    const int64_t step = (int64_t)gridDim.x * R;
+    int64_t row = (int64_t)blockIdx.x * R + g;
+    Pieces<T, C, W> x, y;
+    float mean, rstd;
+    auto fetch = [&](int64_t r) {
+        r = min(r, a.N - 1);
+        x.load((const T *)a.x + r * a.ld_x, k);
+        y.load((const T *)a.dy + r * a.ld_dy, k);
+        mean = a.mean_in[r];
+        rstd = a.rstd_in[r];
+    };
+    fetch(row);
+    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.N; r0 += step, row += step) {
         const bool in = row < a.N;
-        const int64_t rr = in ? row : 0;
-        const float mean = in ? a.mean_in[rr] : 0.f, rstd = in ? a.rstd_in[rr] : 0.f;
-        const T *x = (const T *)a.x + rr * a.ld_x, *dy = (const T *)a.dy + rr * a.ld_dy;
-        float f[C][VE], d[C][VE];
-        float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-        for (int c = 0; c < C; c++) {
-            const int64_t at = n[c] ? (int64_t)(c * L + lane) * VE : 0;
-            load_part<VE>(x + at, in ? n[c] : 0, f[c]);
-            load_part<VE>(dy + at, in ? n[c] : 0, d[c]);
-        }
+        float f[C][W], d[C][W], s1 = 0.f, s2 = 0.f;
+        const float rs = rstd;
 #pragma unroll
         for (int c = 0; c < C; c++)
 #pragma unroll
-            for (int j = 0; j < VE; j++) {
-                f[c][j] = in && j < n[c] ? (f[c][j] - mean) * rstd : 0.f;  // xh
-                dw[c][j] = fmaf(d[c][j], f[c][j], dw[c][j]);
-                db[c][j] += d[c][j];
+            for (int j = 0; j < W; j++) {
+                f[c][j] = ((float)x.v[c][j] - mean) * rstd;  // xh
+                d[c][j] = (float)y.v[c][j];
+                if (in) {
+                    dw[c][j] = fmaf(d[c][j], f[c][j], dw[c][j]);
+                    db[c][j] += d[c][j];
+                }
                 d[c][j] *= w[c][j];  // u
-                s1 += d[c][j];
-                s2 = fmaf(d[c][j], f[c][j], s2);
+                const float u = k.count(c, j, d[c][j]);
+                s1 += u;
+                s2 = fmaf(u, f[c][j], s2);
             }
+        if (r0 + step < a.N) fetch(row + step);
         const float m1 = row_sum<L>(s1, red, turn) * inv;
         const float m2 = row_sum<L>(s2, red, turn) * inv;
         if (!in) continue;
         T *dx = (T *)a.dx + row * a.ld_dx;
 #pragma unroll
         for (int c = 0; c < C; c++) {
-            if (!n[c]) continue;
 #pragma unroll
-            for (int j = 0; j < VE; j++) f[c][j] = rstd * (d[c][j] - m1 - f[c][j] * m2);
-            store_part<VE>(dx + (int64_t)(c * L + lane) * VE, n[c], f[c]);
+            for (int j = 0; j < W; j++) f[c][j] = rs * (d[c][j] - m1 - f[c][j] * m2);
+            if (k.skip[c] < W) store_vec<W>(dx + k.at[c], f[c]);
         }
     }
     // one row of sums per workgroup
@@ -198,24 +238,23 @@ __global__ __launch_bounds__(kThreadsOf<L>) void k_norm_grad(NormArgs a, float *
 #pragma unroll
     for (int c = 0; c < C; c++)
 #pragma unroll
-        for (int k = 0; k < 2; k++) {
-            float(&v)[VE] = k ? db[c] : dw[c];
+        for (int t = 0; t < 2; t++) {
+            float(&v)[W] = t ? db[c] : dw[c];
             if constexpr (R > 1) {
 #pragma unroll
-                for (int j = 0; j < VE; j++) join[g][lane * VE + j] = v[j];
+                for (int j = 0; j < W; j++) join[g][lane * W + j] = v[j];
                 __syncthreads();
-                for (int i = threadIdx.x; i < L * VE; i += kThreadsOf<L>) {
-                    float s = 0.f;
+                if (g == 0 && k.skip[c] < W) {
 #pragma unroll
-                    for (int r = 0; r < R; r++) s += join[r][i];
-                    const int64_t at = (int64_t)c * L * VE + i;
-                    if (at < a.D) out[k * a.D + at] = s;
+                    for (int j = 0; j < W; j++) {
+                        v[j] = 0.f;
+#pragma unroll
+                        for (int r = 0; r < R; r++) v[j] += join[r][lane * W + j];
+                    }
+                    store_vec<W>(out + t * a.D + k.at[c], v);
                 }
                 __syncthreads();
-            } else {
-                const int64_t at = (int64_t)(c * L + lane) * VE;
-                store_part<VE>(out + k * a.D + (n[c] ? at : 0), n[c], v);
-            }
+            } else if (k.skip[c] < W) store_vec<W>(out + t * a.D + k.at[c], v);
         }
 }
 
@@ -294,26 +333,33 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_norm_join(NormArgs a, const
     }
 }
 
-// Calls f with the lanes and chunks for rows of D elements, or with 0 lanes for
-// rows wider than the registers of a workgroup take.
-template <class T, class F> hipError_t by_width(int64_t D, F &&f)
+// Calls f with the lanes, pieces and elements of a piece for rows of D elements,
+// or with 0 lanes for rows wider than the registers of a workgroup take (the
+// backward pass holds five times as much per element).
+template <class T, bool BACK, class F> hipError_t by_width(int64_t D, F &&f)
 {
-#define TQ_ROW(L, C)                                                                                                   \
-    if (chunks <= (int64_t)(L) * (C)) return f(std::integral_constant<int, L>{}, std::integral_constant<int, C>{})
-    const int64_t chunks = (D + kVec<T> - 1) / kVec<T>;
-    TQ_ROW(8, 1);
-    TQ_ROW(16, 1);
-    TQ_ROW(32, 1);
-    TQ_ROW(64, 1);
-    TQ_ROW(64, 2);
-    TQ_ROW(64, 3);
-    TQ_ROW(64, 4);
-    TQ_ROW(256, 2);
-    TQ_ROW(256, 4);
-    TQ_ROW(512, 4);
+#define TQ_ROW(L, C, W)                                                                                                \
+    if (D <= (int64_t)(L) * (C) * (W))                                                                                 \
+    return f(std::integral_constant<int, L>{}, std::integral_constant<int, C>{}, std::integral_constant<int, W>{})
+    constexpr int VE = kVec<T>;
+    if (D < VE) TQ_ROW(8, 1, 1);
+    TQ_ROW(8, 1, VE);
+    TQ_ROW(16, 1, VE);
+    TQ_ROW(32, 1, VE);
+    TQ_ROW(64, 1, VE);
+    TQ_ROW(64, 2, VE);
+    TQ_ROW(64, 3, VE);
+    TQ_ROW(64, 4, VE);
+    TQ_ROW(256, 2, VE);
+    TQ_ROW(256, 4, VE);
+    if constexpr (!BACK) TQ_ROW(1024, 2, VE);
 #undef TQ_ROW
-    return f(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+    return f(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
 }
+
+// Workgroups of the forward pass: as many as the chip holds, and more for its
+// schedulers to even out.
+constexpr int64_t kBlocks = 4096;
 
 // Workgroups of the backward pass: enough to fill the chip several times, few
 // enough that their rows of sums are small beside x.
@@ -321,12 +367,12 @@ constexpr int64_t kGradBlocks = 1024;
 
 template <class T> hipError_t norm_t(const NormArgs &a, hipStream_t s)
 {
-    return by_width<T>(a.D, [&](auto l, auto c) {
-        constexpr int L = decltype(l)::value, C = decltype(c)::value;
+    return by_width<T, false>(a.D, [&](auto l, auto c, auto w) {
+        constexpr int L = decltype(l)::value, C = decltype(c)::value, W = decltype(w)::value;
         if constexpr (L == 0) k_norm_wide<T><<<(unsigned)a.N, kWide, 0, s>>>(a);
         else {
             constexpr int R = kThreadsOf<L> / L;
-            k_norm<T, L, C><<<(unsigned)((a.N + R - 1) / R), kThreadsOf<L>, 0, s>>>(a);
+            k_norm<T, L, C, W><<<(unsigned)std::min((a.N + R - 1) / R, kBlocks), kThreadsOf<L>, 0, s>>>(a);
         }
         return hipGetLastError();
     });
@@ -334,8 +380,8 @@ template <class T> hipError_t norm_t(const NormArgs &a, hipStream_t s)
 
 template <class T> hipError_t norm_grad_t(const NormArgs &a, hipStream_t s)
 {
-    return by_width<T>(a.D, [&](auto l, auto c) {
-        constexpr int L = decltype(l)::value, C = decltype(c)::value;
+    return by_width<T, true>(a.D, [&](auto l, auto c, auto w) {
+        constexpr int L = decltype(l)::value, C = decltype(c)::value, W = decltype(w)::value;
         float *part = (float *)a.ws;
         int64_t blocks;
         if constexpr (L == 0) {
@@ -344,7 +390,7 @@ template <class T> hipError_t norm_grad_t(const NormArgs &a, hipStream_t s)
         } else {
             constexpr int R = kThreadsOf<L> / L;
             blocks = std::min((a.N + R - 1) / R, kGradBlocks);
-            if (blocks) k_norm_grad<T, L, C><<<(unsigned)blocks, kThreadsOf<L>, 0, s>>>(a, part);
+            if (blocks) k_norm_grad<T, L, C, W><<<(unsigned)blocks, kThreadsOf<L>, 0, s>>>(a, part);
         }
         k_norm_join<T><<<(unsigned)((2 * a.D + 63) / 64), kJoinWaves * 64, 0, s>>>(a, part, (int)blocks);
         return hipGetLastError();
