@@ -31,13 +31,13 @@
 namespace tq {
 namespace {
 
-// K: element type and channels per lane (16-bit elements of wide rows: two, 32
-// bits of a row).
+// K: element type, channels per lane (16-bit elements of wide rows: two, 32 bits
+// of a row), steps per wavefront.
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-template <class T_, int CV_> struct Kind {
+template <class T_, int CV_, int STEPS> struct Kind {
     using T = T_;
     static constexpr int CV = CV_;
-    static constexpr int steps = 16 / CV, seg = kWaves * steps, slab = 64 * CV;
+    static constexpr int steps = STEPS, seg = kWaves * steps, slab = 64 * CV;
     static_assert(seg % TQ_SCAN_PIECE == 0 && TQ_SCAN_PIECE % steps == 0,
                   "segments start at pieces, wavefronts at pieces or inside them");
 };
@@ -72,8 +72,8 @@ using Slot = unsigned long long;
 constexpr Slot kEmpty = ~(Slot)0;
 
 struct Geom {
-    int64_t rows;  // records x slabs
-    int slabs, segs;
+    uint32_t rows, slabs;  // rows: records x slabs
+    int segs;
     Slot *slots;   // [segs][rows][kSlab]
     unsigned *ticket;
 };
@@ -109,21 +109,25 @@ __global__ __launch_bounds__(256) void k_scan_clear(Slot *slots, int64_t n, unsi
 
 // What a workgroup works on.
 template <class K> struct Place {
-    int64_t row, b;
+    uint32_t row;
+    int64_t b;
     int seg, wave, lane, c0, n;  // the lane's first channel and their number
     int64_t len, t0;             // the record's length, the wavefront's first step
     int nv;                      // its steps that the record has
     // Segments of the row, in the order they are taken, that hold steps of the
     // record (one at least): the others write zeros and are not waited for.
     int seg0, seg1;
-    __device__ Place(const ScanArgs &a, const Geom &g, int item, bool back)
+    __device__ Place(const ScanArgs &a, const Geom &g, uint32_t item, bool back)
     {
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         lane = threadIdx.x & 63;
-        row = item % g.rows;
-        seg = (int)(item / g.rows);
-        b = row / g.slabs;
-        c0 = (int)(row % g.slabs) * K::slab + lane * K::CV;
+        // in 32 bits: a division of 64 is a hundred instructions
+        const uint32_t s = item / g.rows;
+        row = item - s * g.rows;
+        seg = (int)s;
+        const uint32_t record = row / g.slabs;
+        b = record;
+        c0 = (int)(row - record * g.slabs) * K::slab + lane * K::CV;
         n = (int)max((int64_t)0, min((int64_t)K::CV, a.D - c0));
         if (n == 0) c0 = 0;
         len = a.T;
@@ -137,11 +141,11 @@ template <class K> struct Place {
     __device__ bool idle() const { return seg < seg0 || seg >= seg1; }
 };
 
-__device__ __forceinline__ int take_item(const Geom &g)
+__device__ __forceinline__ uint32_t take_item(const Geom &g)
 {
-    if (g.segs == 1) return (int)blockIdx.x;
-    __shared__ int item;
-    if (threadIdx.x == 0) item = (int)atomicAdd(g.ticket, 1u);
+    if (g.segs == 1) return blockIdx.x;
+    __shared__ uint32_t item;
+    if (threadIdx.x == 0) item = atomicAdd(g.ticket, 1u);
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(item);
 }
@@ -260,7 +264,7 @@ __device__ __forceinline__ void look_back(const Geom &g, const Place<K> &at, flo
 }
 
 // ------------------------------------------------------------------ forward
-template <class K> __global__ __launch_bounds__(kThreads, 6) void k_scan(ScanArgs a, Geom g)
+template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a, Geom g)
 {
     using T = typename K::T;
     constexpr int CV = K::CV, L = K::steps;
@@ -547,7 +551,7 @@ template <class K> struct Layout {
     Geom start(void *ws, hipStream_t s) const
     {
         Geom g{};
-        g.rows = rows, g.slabs = slabs, g.segs = segs;
+        g.rows = (uint32_t)rows, g.slabs = (uint32_t)slabs, g.segs = segs;
         if (segs == 1) return g;
         g.slots = (Slot *)((char *)ws + slots);
         g.ticket = (unsigned *)((char *)ws + ticket);
@@ -558,11 +562,11 @@ template <class K> struct Layout {
 };
 
 // Calls f with the kind of a scan.
-template <class T, class F> auto by_kind(int64_t D, F &&f)
+template <class T, bool BACK, class F> auto by_kind(int64_t D, F &&f)
 {
     if constexpr (sizeof(T) == 2)
-        if (D > 64) return f(Kind<T, 2>{});
-    return f(Kind<T, 1>{});
+        if (D > 64) return f(Kind<T, 2, BACK ? 8 : 16>{});
+    return f(Kind<T, 1, 16>{});
 }
 
 template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
@@ -572,7 +576,7 @@ template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
         k_scan_few<T><<<(unsigned)((a.B * chunks + 255) / 256), 256, 0, s>>>(a, chunks);
         return hipGetLastError();
     }
-    return by_kind<T>(a.D, [&](auto kind) {
+    return by_kind<T, false>(a.D, [&](auto kind) {
         using K = decltype(kind);
         const Layout<K> l(a.B, a.T, a.D);
         k_scan<K><<<(unsigned)l.items, kThreads, 0, s>>>(a, l.start(a.ws, s));
@@ -582,7 +586,7 @@ template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
 
 template <class T> hipError_t scan_grad_t(const ScanArgs &a, hipStream_t s)
 {
-    return by_kind<T>(a.D, [&](auto kind) {
+    return by_kind<T, true>(a.D, [&](auto kind) {
         using K = decltype(kind);
         const Layout<K> l(a.B, a.T, a.D);
         k_scan_grad<K><<<(unsigned)l.items, kThreads, 0, s>>>(a, l.start(a.ws, s));
@@ -590,22 +594,23 @@ template <class T> hipError_t scan_grad_t(const ScanArgs &a, hipStream_t s)
     });
 }
 
-// The larger of what fp32 and 16-bit arrays take.
-template <class F> auto larger(int64_t D, F &&f)
+// The largest of what the directions and types take.
+template <class F> auto largest(int64_t D, F &&f)
 {
-    return std::max(by_kind<float>(D, f), by_kind<__bf16>(D, f));
+    return std::max({by_kind<float, false>(D, f), by_kind<__bf16, false>(D, f), by_kind<float, true>(D, f),
+                     by_kind<__bf16, true>(D, f)});
 }
 
 } // namespace
 
 int64_t scan_items(int64_t B, int64_t T, int64_t D)
 {
-    return larger(D, [&](auto kind) { return Layout<decltype(kind)>(B, T, D).items; });
+    return largest(D, [&](auto kind) { return Layout<decltype(kind)>(B, T, D).items; });
 }
 
 size_t scan_workspace(int64_t B, int64_t T, int64_t D)
 {
-    return larger(D, [&](auto kind) { return Layout<decltype(kind)>(B, T, D).bytes; });
+    return largest(D, [&](auto kind) { return Layout<decltype(kind)>(B, T, D).bytes; });
 }
 
 hipError_t launch_scan(int32_t type, const ScanArgs &a, hipStream_t s)
