@@ -19,12 +19,13 @@
 // 2^-22 of the product, and costs three products; fp32 matrix instructions
 // would cost sixteen times the 16-bit ones.
 //
-// Powers of two.  With up = f 2^e, 1 <= |f| < 2, the stored p carries f, the
-// hidden rows of dweight's product carry 2^e (relative to the largest row, so that
-// 16 bits hold them), and dhidden's rows are multiplied by 2^e at the end:
-// all exact.  fp32 rows are scaled to magnitudes of 2^13 .. 2^14 on their own
-// where the product leaves the row's axis standing; the weights of dhidden's
-// product, which sums over words, have one scale for all.
+// The stored p is p itself, up to a power of two: its largest entries are near -1,
+// and a factor common to all tokens would put the same rounding error into each.
+// upstream multiplies dhidden's rows at the end, in fp32, and enters dweight
+// through the hidden rows, relative to the largest, so that the mean's equal
+// weights change nothing there.  fp32 rows are scaled to magnitudes of 2^13 ..
+// 2^14 on their own where the product leaves the row's axis standing; the
+// operands that a product sums over the rows of have one scale for all.
 #include <algorithm>
 #include <type_traits>
 
@@ -50,9 +51,9 @@ __device__ __forceinline__ f32x16 mfma32(frag<_Float16> a, frag<_Float16> b, f32
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// p f is held times 2^14 in 16 bits: below 2^15 it fits f16, whose small numbers
+// p is held times 2^15 in 16 bits: at most 2^15 fits f16, whose small numbers
 // would otherwise not reach the probabilities of a large vocabulary.
-constexpr int kProbBits = 14;
+constexpr int kProbBits = 15;
 
 // ------------------------------------------------------------ C = A B^T
 // Operands of 16-bit elements, rows 16-byte aligned.  Along the summed axis:
@@ -255,14 +256,9 @@ __device__ __forceinline__ void wave_fence()
     __builtin_amdgcn_wave_barrier();
 }
 
-// up = f 2^e with 1 <= |f| < 2 (f below 1 for subnormal numbers; zeros, infinities
-// and NaN stay in f).
-__device__ __forceinline__ void split_up(float up, float &f, int &e)
-{
-    const int x = (int)((__float_as_uint(up) >> 23) & 255);
-    e = x == 255 ? 0 : max(x, 1) - 127;
-    f = ldexpf(up, -e);
-}
+// Exponent of |v|, finite and not zero (subnormal numbers count as the smallest
+// normal ones).
+__device__ __forceinline__ int exponent(float v) { return max((int)((__float_as_uint(v) >> 23) & 255), 1) - 127; }
 
 // exp(z - r) from z and r log2 e, with one rounding of the exponent; that of
 // r log2 e, up to |r| 2^-23, is common to a row and of the order of lse's own.
@@ -280,7 +276,7 @@ struct LogitArgs {
     int64_t v_base;    // first word of the piece (p.a.p and word_scale point there)
     float2 *part;      // [N, tiles]: maximum, sum of exponentials
     float *z_target;   // [N]
-    const float *lse, *up;
+    const float *lse;
     void *prob;        // [tokens, words] of the piece, both up to a multiple of kBK
     int64_t ld_prob, prob_rows, prob_part;
 };
@@ -377,10 +373,6 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
             const float lse = on ? a.lse[n] : 0.f;
             const int64_t away = on ? (int64_t)target - a.v_base - v0 : -1;
             const int hit = away >= 0 && away < S::FM * 32 ? (int)away : -1;
-            float f = 0.f;
-            int e2;
-            if (on) split_up(a.up[n], f, e2);
-            f *= (float)(1 << kProbBits);
             const float lse2 = lse * kLog2e;
             const bool some = __any(hit >= 0);
 #pragma unroll
@@ -396,7 +388,7 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
 #pragma unroll
             for (int i = 0; i < S::FM; i++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) acc[i][j][e] *= f;
+                for (int e = 0; e < 16; e++) acc[i][j][e] *= (float)(1 << kProbBits);
             // what is not a word of a token with a target is zero, whatever it holds
             const int last = on ? words : 0;
             if (__any(last < S::FM * 32))
@@ -454,6 +446,12 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
 }
 
 // ------------------------------------------------------------ the products
+// The largest |up|, and the power of two that dweight's hidden rows are scaled by.
+struct UpMax {
+    float up;
+    int bits;
+};
+
 // What becomes of C: out = factor(row) C, or C is added up in fp32 over the
 // pieces of the vocabulary (`sum`), or a part of a tile goes to its slab.
 struct StoreArgs {
@@ -464,12 +462,12 @@ struct StoreArgs {
     bool add;      // to what `sum` holds
     void *out;
     int64_t ld_out;
-    // factor: 2^(exponent of up) of the row, or 2^*e_max for all; and the scale of
-    // the second operand
+    // factor: the row's up, or the largest one and the scale for all; and the
+    // scale of the second operand
     const float *up;
     const uint64_t *targets;
     int64_t V;
-    const int *e_max;
+    const UpMax *up_max;
     const float *w_max;
 };
 
@@ -494,21 +492,21 @@ __device__ __forceinline__ float max_of(const float *part)
 struct Factor {
     const StoreArgs &a;
     int bits;
-    __device__ explicit Factor(const StoreArgs &s) : a(s), bits(-kProbBits)
+    float all;
+    __device__ explicit Factor(const StoreArgs &s) : a(s), bits(-kProbBits), all(1.f)
     {
         if (a.w_max) bits += scale_bits(max_of(a.w_max));
-        if (a.e_max) bits += *a.e_max;
+        if (a.up_max) {
+            all = a.up_max->up;
+            bits += a.up_max->bits;
+        }
     }
     // c times the factor of row m; a row without a target is zero whatever the
     // weights hold
     __device__ float of(float c, int64_t m) const
     {
-        if (!a.up) return ldexpf(c, bits);
-        if (a.targets[m] >= (uint64_t)a.V) return 0.f;
-        float f;
-        int e;
-        split_up(a.up[m], f, e);
-        return ldexpf(c, bits + e);
+        if (!a.up) return ldexpf(c, bits) * all;
+        return a.targets[m] < (uint64_t)a.V ? ldexpf(c, bits) * a.up[m] : 0.f;
     }
 };
 
@@ -629,11 +627,11 @@ struct PackArgs {
     void *all;          // fp32: a second copy with the scale of the maximum in w_max
     const float *w_max;
     // dst for dweight's product: zeros for rows without a target, other rows
-    // times 2^(e - *e_max), e the exponent of the row's up and scale
+    // times up, relative to the largest, and 2^-bits
     const uint64_t *targets;
     int64_t V;
     const float *up;
-    const int *e_max;
+    const UpMax *up_max;
 };
 
 // One wavefront per row.
@@ -662,13 +660,11 @@ template <class In, class T, bool TWO> __global__ __launch_bounds__(256) void k_
         bits = -scale_bits(top);
         if (a.scale && lane == 0) a.scale[r] = two_to(-bits);
     }
+    float share = 1.f;
     if (a.up) {
         on = a.targets[r] < (uint64_t)a.V;
-        float f;
-        int e;
-        split_up(on ? a.up[r] : 1.f, f, e);
-        // src = m 2^-bits: times 2^e, relative to the largest
-        bits = e - *a.e_max;
+        share = on ? a.up[r] / a.up_max->up : 0.f;
+        bits = -a.up_max->bits;
     }
     for (int64_t c = lane * VE; c < a.kp; c += 64 * VE) {
         float f[VE], g[VE], lo[VE];
@@ -677,7 +673,7 @@ template <class In, class T, bool TWO> __global__ __launch_bounds__(256) void k_
         T *dst = (T *)a.dst + r * a.kp + c;
 #pragma unroll
         for (int j = 0; j < VE; j++) {
-            g[j] = TWO || a.up ? ldexpf(f[j], bits) : f[j];
+            g[j] = TWO ? ldexpf(f[j] * share, bits) : f[j] * share;
             if (TWO) lo[j] = g[j] - (float)(T)g[j];
         }
         store_vec<VE>(dst, g);
@@ -697,29 +693,33 @@ template <class In, class T, bool TWO> __global__ __launch_bounds__(256) void k_
     }
 }
 
-// e_max: the largest exponent of |up| (times the row's scale) over the rows with
-// a target whose up is finite and not zero; -(13 bits of scale) included.
+// The largest finite |up| of a row with a target (1 if there is none); with
+// fp32 rows of scale `scale`, bits brings the largest of up times the scale to
+// that of the largest up.
 __global__ __launch_bounds__(1024) void k_up_max(const float *up, const uint64_t *targets, const float *scale, int64_t N,
-                                                int64_t V, int *e_max)
+                                                int64_t V, UpMax *out)
 {
-    __shared__ int red[16];
-    int top = -1000;
+    __shared__ float reds[16];
+    __shared__ int rede[16];
+    float top = 0.f;
+    int e = -1000;
     for (int64_t i = threadIdx.x; i < N; i += 1024) {
-        float f;
-        int e;
-        const float u = up[i];
-        if (targets[i] >= (uint64_t)V || u == 0.f || !(fabsf(u) < INFINITY)) continue;
-        split_up(u, f, e);
-        if (scale) e += (int)((__float_as_uint(scale[i]) >> 23) & 255) - 127;
-        top = max(top, e);
+        const float u = fabsf(up[i]);
+        if (targets[i] >= (uint64_t)V || u == 0.f || !(u < INFINITY)) continue;
+        top = fmaxf(top, u);
+        if (scale) e = max(e, exponent(u) + exponent(scale[i]));
     }
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d, 64));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+    for (int d = 32; d > 0; d >>= 1) {
+        top = fmaxf(top, __shfl_xor(top, d, 64));
+        e = max(e, __shfl_xor(e, d, 64));
+    }
+    if ((threadIdx.x & 63) == 0) reds[threadIdx.x >> 6] = top, rede[threadIdx.x >> 6] = e;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 0; w < 16; w++) top = max(top, red[w]);
-        *e_max = top == -1000 ? 0 : top;
+        for (int w = 0; w < 16; w++) top = fmaxf(top, reds[w]), e = max(e, rede[w]);
+        if (top == 0.f) top = 1.f, e = 0;
+        *out = UpMax{top, scale ? e - exponent(top) : 0};
     }
 }
 
@@ -932,7 +932,7 @@ struct XentPlan {
     int terms;
     int64_t N, V, D, kp, np;
     int64_t piece;  // words of a piece of the vocabulary
-    size_t part, z_target, hp, wp, all, hs, h_scale, w_scale, w_max, e_max, prob, sum, slabs, bytes;
+    size_t part, z_target, hp, wp, all, hs, h_scale, w_scale, w_max, up_max, prob, sum, slabs, bytes;
 
     Cut cut_h(int64_t words) const { return Cut(N, D, terms * (up_to(words, kBK) / kBK), true); }
     Cut cut_w(int64_t words) const { return Cut(words, D, terms * (np / kBK), true); }
@@ -960,7 +960,7 @@ struct XentPlan {
             const int64_t words = std::min(piece, up_to(V, kBK));
             all = c.take(two ? elem * V * kp : 0);
             w_max = c.take(sizeof(float) * kMaxParts);
-            e_max = c.take(sizeof(int));
+            up_max = c.take(sizeof(UpMax));
             hs = c.take(elem * N * kp);
             prob = c.take(elem * np * words);
             sum = c.take(piece < V ? sizeof(float) * N * D : 0);
@@ -1075,13 +1075,13 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     k_lse<<<token_blocks, 256, 0, s>>>(part, tiles, a.N, a.targets, a.V, z_target, a.loss, a.lse);
     if (!grad || a.D == 0) return hipGetLastError();
 
-    int *e_max = (int *)(ws + p.e_max);
-    k_up_max<<<1, 1024, 0, s>>>(a.upstream, a.targets, TWO ? h_scale : nullptr, a.N, a.V, e_max);
+    UpMax *up_max = (UpMax *)(ws + p.up_max);
+    k_up_max<<<1, 1024, 0, s>>>(a.upstream, a.targets, TWO ? h_scale : nullptr, a.N, a.V, up_max);
     const Operand hs{ws + p.hs, p.kp, a.N * p.kp, p.kp, a.N};
     PackArgs u{};
     u.src = a.hidden, u.ld = a.ld_hidden, u.rows = a.N, u.D = a.D;
     u.dst = ws + p.hs, u.kp = p.kp, u.part = hs.part;
-    u.targets = a.targets, u.V = a.V, u.up = a.upstream, u.e_max = e_max;
+    u.targets = a.targets, u.V = a.V, u.up = a.upstream, u.up_max = up_max;
     k_pack<In, T, TWO><<<token_blocks, 256, 0, s>>>(u);
     StoreArgs d{};  // dhidden
     d.M = a.N, d.N = a.D;
@@ -1097,7 +1097,6 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
         l.word_scale = w_scale + v0;
         l.v_base = v0;
         l.lse = a.lse;
-        l.up = a.upstream;
         l.prob = ws + p.prob;
         l.ld_prob = kv;
         l.prob_rows = p.np;
@@ -1113,7 +1112,7 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
         e.M = words, e.N = a.D;
         e.slabs = d.slabs;
         e.out = (In *)a.dweight + v0 * a.ld_dweight, e.ld_out = a.ld_dweight;
-        e.e_max = e_max;
+        e.up_max = up_max;
         e.p.a = Operand{ws + p.prob, kv, l.prob_part, kv, p.np};
         e.p.b = hs;
         e.p.terms = p.terms;
