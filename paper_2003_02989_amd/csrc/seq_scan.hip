@@ -530,6 +530,56 @@ template <class T> __global__ __launch_bounds__(256) void k_scan_few(ScanArgs a,
     if (a.h_last) store_part<VE>(a.h_last + b * a.D + c, n, h);
 }
 
+// The gradients of a few steps: the lane keeps the states it passes forwards.
+template <class T> __global__ __launch_bounds__(256) void k_scan_grad_few(ScanArgs a, int64_t chunks)
+{
+    constexpr int VE = 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.B * chunks) return;
+    const int64_t b = i / chunks, c = i % chunks * VE;
+    const int n = (int)min((int64_t)VE, a.D - c);
+    int64_t len = a.T;
+    if (a.lengths) len = min(max((int64_t)a.lengths[b], (int64_t)0), a.T);
+    const T *x = (const T *)a.x + b * a.xb + c, *g = (const T *)a.g + b * a.gb + c, *dy = (const T *)a.dy + b * a.dyb + c;
+    T *dx = (T *)a.dx + b * a.dxb + c, *dg = (T *)a.dg + b * a.dgb + c;
+    float m[VE] = {}, h[kFew][VE], ga[kFew][VE], gc[kFew][VE], xv[kFew][VE];
+    if (a.dh_last) load_part<VE>(a.dh_last + b * a.D + c, n, m);
+    float s[VE] = {};
+    if (len) load_part<VE>(a.states_in + b * a.D + c, n, s);
+#pragma unroll
+    for (int t = 0; t < kFew; t++) {
+        if (t >= len) break;
+        float gv[VE];
+        load_part<VE>(x + t * a.xs, n, xv[t]);
+        load_part<VE>(g + t * a.gs, n, gv);
+#pragma unroll
+        for (int j = 0; j < VE; j++) {
+            gate<T>(gv[j], ga[t][j], gc[t][j]);
+            h[t][j] = s[j];
+            s[j] = fmaf(ga[t][j], s[j], gc[t][j] * xv[t][j]);
+        }
+    }
+#pragma unroll
+    for (int t = kFew - 1; t >= 0; t--) {
+        if (t >= a.T) continue;
+        float ox[VE] = {}, og[VE] = {};
+        if (t < len) {
+            float d[VE];
+            load_part<VE>(dy + t * a.dys, n, d);
+#pragma unroll
+            for (int j = 0; j < VE; j++) {
+                const float l = d[j] + m[j];
+                m[j] = ga[t][j] * l;
+                ox[j] = gc[t][j] * l;
+                og[j] = gc[t][j] * m[j] * (h[t][j] - xv[t][j]);
+            }
+        }
+        store_part<VE>(dx + t * a.dxs, n, ox);
+        store_part<VE>(dg + t * a.dgs, n, og);
+    }
+    if (a.dh0) store_part<VE>(a.dh0 + b * a.D + c, n, m);
+}
+
 // ------------------------------------------------------------------ launches
 // Rows (records x slabs) and segments of a scan of kind K.
 template <class K> struct Layout {
@@ -586,6 +636,11 @@ template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
 
 template <class T> hipError_t scan_grad_t(const ScanArgs &a, hipStream_t s)
 {
+    if (a.T <= kFew) {
+        const int64_t chunks = (a.D + 3) / 4;
+        k_scan_grad_few<T><<<(unsigned)((a.B * chunks + 255) / 256), 256, 0, s>>>(a, chunks);
+        return hipGetLastError();
+    }
     return by_kind<T, true>(a.D, [&](auto kind) {
         using K = decltype(kind);
         const Layout<K> l(a.B, a.T, a.D);
