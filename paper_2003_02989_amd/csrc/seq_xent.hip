@@ -228,9 +228,8 @@ struct Tile {
     int64_t m, n;
     int id, split;  // split: -1 when the workgroup has the tile to itself
 };
-__device__ __forceinline__ Tile tile_of(const ProductArgs &a)
+__device__ __forceinline__ Tile tile_of(const ProductArgs &a, int blk)
 {
-    const int blk = blockIdx.x;
     Tile t;
     if (blk < a.full) {
         const int per = a.full / kXcds, more = a.full % kXcds, xcd = blk % kXcds;
@@ -284,7 +283,7 @@ struct LogitArgs {
 template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S::threads) void k_logits(LogitArgs a)
 {
     TQ_STAGES(T, S, lds);
-    const Tile t = tile_of(a.p);
+    const Tile t = tile_of(a.p, blockIdx.x);
     f32x16 acc[S::FM][S::FN];
     const int64_t m0 = t.m * S::BM, n0 = t.n * S::BN;
     product<T, S, false, false>(a.p, lds, m0, n0, 0, a.p.terms * a.p.k_tiles, acc);
@@ -446,11 +445,33 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
 }
 
 // ------------------------------------------------------------ the products
-// The largest |up|, and the power of two that dweight's hidden rows are scaled by.
+// Partial maxima, by kUpParts workgroups, over the rows with a target and a finite
+// up that is not zero: of |up|, and of the exponents of up times the row's scale.
+constexpr int kUpParts = 64;
+struct UpParts {
+    float up[kUpParts];
+    int bits[kUpParts];
+};
+// The largest |up| (1 if there is none), and the power of two that dweight's
+// hidden rows are scaled by, 0 for 16-bit rows: it brings the largest of up
+// times the scale to that of the largest up.
 struct UpMax {
     float up;
     int bits;
 };
+__device__ __forceinline__ UpMax up_max_of(const UpParts *p)
+{
+    const int lane = threadIdx.x & 63;
+    float u = p->up[lane];
+    int e = p->bits[lane];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        u = fmaxf(u, __shfl_xor(u, d, 64));
+        e = max(e, __shfl_xor(e, d, 64));
+    }
+    if (u == 0.f) return UpMax{1.f, 0};
+    return UpMax{u, e > -1000 ? e - exponent(u) : 0};
+}
 
 // What becomes of C: out = factor(row) C, or C is added up in fp32 over the
 // pieces of the vocabulary (`sum`), or a part of a tile goes to its slab.
@@ -467,7 +488,7 @@ struct StoreArgs {
     const float *up;
     const uint64_t *targets;
     int64_t V;
-    const UpMax *up_max;
+    const UpParts *up_max;
     const float *w_max;
 };
 
@@ -479,11 +500,11 @@ __device__ __forceinline__ int scale_bits(float m)
 __device__ __forceinline__ float two_to(int e) { return ldexpf(1.f, e); }
 
 // The maximum of kMaxParts partial maxima, by one wavefront.
-constexpr int kMaxParts = 128;
+constexpr int kMaxParts = 256;
 __device__ __forceinline__ float max_of(const float *part)
 {
     const int lane = threadIdx.x & 63;
-    float m = fmaxf(part[lane], part[lane + 64]);
+    float m = fmaxf(fmaxf(part[lane], part[lane + 64]), fmaxf(part[lane + 128], part[lane + 192]));
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
     return m;
@@ -497,8 +518,9 @@ struct Factor {
     {
         if (a.w_max) bits += scale_bits(max_of(a.w_max));
         if (a.up_max) {
-            all = a.up_max->up;
-            bits += a.up_max->bits;
+            const UpMax u = up_max_of(a.up_max);
+            all = u.up;
+            bits += u.bits;
         }
     }
     // c times the factor of row m; a row without a target is zero whatever the
@@ -510,11 +532,10 @@ struct Factor {
     }
 };
 
-template <class T, class S, bool TA, bool TB, class Out>
-__global__ __launch_bounds__(S::threads) void k_product(StoreArgs a)
+template <class T, class S, bool TA, class Out>
+__device__ __forceinline__ void product_tile(const StoreArgs &a, const Stages<T, S> &lds, int blk)
 {
-    TQ_STAGES(T, S, lds);
-    const Tile t = tile_of(a.p);
+    const Tile t = tile_of(a.p, blk);
     f32x16 acc[S::FM][S::FN];
     const int64_t m0 = t.m * S::BM, n0 = t.n * S::BN;
     const int all = a.p.terms * a.p.k_tiles;
@@ -523,7 +544,7 @@ __global__ __launch_bounds__(S::threads) void k_product(StoreArgs a)
         k0 = (int)((int64_t)all * t.split / a.p.splits);
         k1 = (int)((int64_t)all * (t.split + 1) / a.p.splits);
     }
-    product<T, S, TA, TB>(a.p, lds, m0, n0, k0, k1, acc);
+    product<T, S, TA, true>(a.p, lds, m0, n0, k0, k1, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
     if (t.split >= 0) {
@@ -557,16 +578,28 @@ __global__ __launch_bounds__(S::threads) void k_product(StoreArgs a)
         }
 }
 
-// The tiles that were cut along K: their slabs, added up in order.
-template <class S, class Out> __global__ __launch_bounds__(256) void k_slabs(StoreArgs a)
+// dhidden's product in the first h_blocks workgroups and dweight's, whose tiles
+// fill what the former's last round leaves free, in the others.
+template <class T, class S, class Out>
+__global__ __launch_bounds__(S::threads) void k_products(StoreArgs h, StoreArgs w, int h_blocks)
 {
-    ProductArgs p = a.p;
+    TQ_STAGES(T, S, lds);
+    if ((int)blockIdx.x < h_blocks) product_tile<T, S, false, Out>(h, lds, blockIdx.x);
+    else product_tile<T, S, true, Out>(w, lds, blockIdx.x - h_blocks);
+}
+
+// The tiles that were cut along K: their slabs, added up in order.
+template <class S, class Out> __global__ __launch_bounds__(256) void k_slabs(StoreArgs h, StoreArgs w, int h_tail)
+{
+    const StoreArgs &a = (int)blockIdx.x < h_tail ? h : w;
+    const int tail = (int)blockIdx.x < h_tail ? blockIdx.x : blockIdx.x - h_tail;
+    const ProductArgs &p = a.p;
     // the tile's place, as tile_of gives it
-    const int id = p.full + blockIdx.x;
+    const int id = p.full + tail;
     const int band = kGroup * p.n_tiles, g = id / band, rows = min(kGroup, p.m_tiles - g * kGroup);
     const int in = id - g * band;
     const int64_t m0 = (int64_t)(g * kGroup + in % rows) * S::BM, n0 = (int64_t)(in / rows) * S::BN;
-    const float *slab = a.slabs + (int64_t)blockIdx.x * p.splits * (S::BM * S::BN);
+    const float *slab = a.slabs + (int64_t)tail * p.splits * (S::BM * S::BN);
     const Factor factor(a);
     // four columns per thread
     const int at = (blockIdx.y * 256 + threadIdx.x) * 4, r = at / S::BN, c = at % S::BN;
@@ -595,13 +628,14 @@ template <class Out> __global__ __launch_bounds__(256) void k_finish(StoreArgs a
 }
 
 // ------------------------------------------------------------ laying out
-// Partial maxima of the finite magnitudes of src [rows, D].
-__global__ __launch_bounds__(1024) void k_max(const float *src, int64_t ld, int64_t rows, int64_t D, float *part)
+// Partial maxima of the finite magnitudes of src [rows, D], by kMaxParts
+// workgroups.
+__device__ __forceinline__ void max_part(const float *src, int64_t ld, int64_t rows, int64_t D, float *part, int blk)
 {
-    __shared__ float red[16];
+    __shared__ float red[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float top = 0.f;
-    for (int64_t r = (int64_t)blockIdx.x * 16 + wave; r < rows; r += kMaxParts * 16)
+    for (int64_t r = (int64_t)blk * 4 + wave; r < rows; r += kMaxParts * 4)
         for (int64_t c = lane * 4; c < D; c += 256) {
             float f[4];
             load_part<4>(src + r * ld + c, (int)min((int64_t)4, D - c), f);
@@ -612,10 +646,7 @@ __global__ __launch_bounds__(1024) void k_max(const float *src, int64_t ld, int6
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     if (lane == 0) red[wave] = top;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 0; w < 16; w++) top = fmaxf(top, red[w]);
-        part[blockIdx.x] = top;
-    }
+    if (threadIdx.x == 0) part[blk] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
 }
 
 struct PackArgs {
@@ -631,16 +662,17 @@ struct PackArgs {
     const uint64_t *targets;
     int64_t V;
     const float *up;
-    const UpMax *up_max;
+    const UpParts *up_max;
 };
 
-// One wavefront per row.
-template <class In, class T, bool TWO> __global__ __launch_bounds__(256) void k_pack(PackArgs a)
+// One wavefront per row, four rows per workgroup.
+template <class In, class T, bool TWO> __device__ __forceinline__ void pack_rows(const PackArgs &a, int blk)
 {
     constexpr int VE = kVec<T>;
     const int lane = threadIdx.x & 63;
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t r = (int64_t)blk * 4 + (threadIdx.x >> 6);
     const float w_max = TWO && a.all ? max_of(a.w_max) : 0.f;
+    const UpMax largest = a.up ? up_max_of(a.up_max) : UpMax{1.f, 0};
     if (r >= a.rows) return;
     const In *src = (const In *)a.src + r * a.ld;
     int bits = 0, bits_all = 0;
@@ -663,8 +695,8 @@ template <class In, class T, bool TWO> __global__ __launch_bounds__(256) void k_
     float share = 1.f;
     if (a.up) {
         on = a.targets[r] < (uint64_t)a.V;
-        share = on ? a.up[r] / a.up_max->up : 0.f;
-        bits = -a.up_max->bits;
+        share = on ? a.up[r] / largest.up : 0.f;
+        bits = -largest.bits;
     }
     for (int64_t c = lane * VE; c < a.kp; c += 64 * VE) {
         float f[VE], g[VE], lo[VE];
@@ -693,21 +725,23 @@ template <class In, class T, bool TWO> __global__ __launch_bounds__(256) void k_
     }
 }
 
-// The largest finite |up| of a row with a target (1 if there is none); with
-// fp32 rows of scale `scale`, bits brings the largest of up times the scale to
-// that of the largest up.
-__global__ __launch_bounds__(1024) void k_up_max(const float *up, const uint64_t *targets, const float *scale, int64_t N,
-                                                int64_t V, UpMax *out)
+struct UpArgs {
+    const float *up, *scale;  // scale: of fp32 rows
+    const uint64_t *targets;
+    int64_t N, V;
+    UpParts *out;
+};
+__device__ __forceinline__ void up_max(const UpArgs &a, int blk)
 {
-    __shared__ float reds[16];
-    __shared__ int rede[16];
+    __shared__ float reds[4];
+    __shared__ int rede[4];
     float top = 0.f;
     int e = -1000;
-    for (int64_t i = threadIdx.x; i < N; i += 1024) {
-        const float u = fabsf(up[i]);
-        if (targets[i] >= (uint64_t)V || u == 0.f || !(u < INFINITY)) continue;
-        top = fmaxf(top, u);
-        if (scale) e = max(e, exponent(u) + exponent(scale[i]));
+    for (int64_t i = (int64_t)blk * 256 + threadIdx.x; i < a.N; i += 256 * kUpParts) {
+        const float u = fabsf(a.up[i]);
+        const bool on = a.targets[i] < (uint64_t)a.V && u > 0.f && u < INFINITY;
+        top = on ? fmaxf(top, u) : top;
+        if (a.scale) e = on ? max(e, exponent(u) + exponent(a.scale[i])) : e;
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
@@ -717,31 +751,64 @@ __global__ __launch_bounds__(1024) void k_up_max(const float *up, const uint64_t
     if ((threadIdx.x & 63) == 0) reds[threadIdx.x >> 6] = top, rede[threadIdx.x >> 6] = e;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 0; w < 16; w++) top = fmaxf(top, reds[w]), e = max(e, rede[w]);
-        if (top == 0.f) top = 1.f, e = 0;
-        *out = UpMax{top, scale ? e - exponent(top) : 0};
+        for (int w = 0; w < 4; w++) top = fmaxf(top, reds[w]), e = max(e, rede[w]);
+        a.out->up[blk] = top;
+        a.out->bits[blk] = e;
     }
 }
 
+struct LseArgs {
+    const float2 *part;  // [N, tiles]
+    int tiles;
+    int64_t N, V;
+    const uint64_t *targets;
+    const float *z_target;
+    float *loss, *lse;
+};
 // lse and loss of a token from its tiles' maxima and sums. One wavefront each.
-__global__ __launch_bounds__(256) void k_lse(const float2 *part, int tiles, int64_t N, const uint64_t *targets,
-                                            int64_t V, const float *z_target, float *loss, float *lse)
+__device__ __forceinline__ void lse_rows(const LseArgs &a, int blk)
 {
-    const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t n = (int64_t)blk * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
-    if (n >= N) return;
-    part += n * tiles;
+    if (n >= a.N) return;
+    const float2 *part = a.part + n * a.tiles;
     float top = -INFINITY;
-    for (int k = lane; k < tiles; k += 64) top = fmaxf(top, part[k].x);
+    for (int k = lane; k < a.tiles; k += 64) top = fmaxf(top, part[k].x);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     float sum = 0.f;
-    for (int k = lane; k < tiles; k += 64) sum += part[k].y * __expf(part[k].x - top);
+    for (int k = lane; k < a.tiles; k += 64) sum += part[k].y * __expf(part[k].x - top);
     sum = group_sum<64>(sum);
     if (lane) return;
     const float l = top + logf(sum);
-    lse[n] = l;
-    loss[n] = targets[n] < (uint64_t)V ? l - z_target[n] : 0.f;
+    a.lse[n] = l;
+    a.loss[n] = a.targets[n] < (uint64_t)a.V ? l - a.z_target[n] : 0.f;
+}
+
+// Small steps that do not wait for one another share a launch.
+//
+// Before the logits: hidden's rows laid out, and what the weights' layout needs
+// (their partial maxima).
+template <class In, class T, bool TWO>
+__global__ __launch_bounds__(256) void k_lay_hidden(PackArgs h, int h_blocks, const float *w, int64_t ld_w, int64_t V,
+                                                   float *w_max)
+{
+    if ((int)blockIdx.x < h_blocks) pack_rows<In, T, TWO>(h, blockIdx.x);
+    else max_part(w, ld_w, V, h.D, w_max, blockIdx.x - h_blocks);
+}
+// The weights' rows laid out, and the largest upstream.
+template <class In, class T, bool TWO>
+__global__ __launch_bounds__(256) void k_lay_weight(PackArgs w, int w_blocks, UpArgs u)
+{
+    if ((int)blockIdx.x < w_blocks) pack_rows<In, T, TWO>(w, blockIdx.x);
+    else up_max(u, blockIdx.x - w_blocks);
+}
+// After the logits: lse and loss, and hidden's rows laid out for dweight.
+template <class In, class T, bool TWO>
+__global__ __launch_bounds__(256) void k_lse(LseArgs l, int l_blocks, PackArgs h)
+{
+    if ((int)blockIdx.x < l_blocks) lse_rows(l, blockIdx.x);
+    else pack_rows<In, T, TWO>(h, blockIdx.x - l_blocks);
 }
 
 // ------------------------------------------------------- a few tokens
@@ -932,7 +999,7 @@ struct XentPlan {
     int terms;
     int64_t N, V, D, kp, np;
     int64_t piece;  // words of a piece of the vocabulary
-    size_t part, z_target, hp, wp, all, hs, h_scale, w_scale, w_max, up_max, prob, sum, slabs, bytes;
+    size_t part, z_target, hp, wp, all, hs, h_scale, w_scale, w_max, up_max, prob, sum, slabs_h, slabs_w, bytes;
 
     Cut cut_h(int64_t words) const { return Cut(N, D, terms * (up_to(words, kBK) / kBK), true); }
     Cut cut_w(int64_t words) const { return Cut(words, D, terms * (np / kBK), true); }
@@ -960,15 +1027,18 @@ struct XentPlan {
             const int64_t words = std::min(piece, up_to(V, kBK));
             all = c.take(two ? elem * V * kp : 0);
             w_max = c.take(sizeof(float) * kMaxParts);
-            up_max = c.take(sizeof(UpMax));
+            up_max = c.take(sizeof(UpParts));
             hs = c.take(elem * N * kp);
             prob = c.take(elem * np * words);
             sum = c.take(piece < V ? sizeof(float) * N * D : 0);
-            size_t s = 0;
+            size_t sh = 0, sw = 0;
             if (D)
-                for (int64_t w : {std::min(piece, V), V - (V - 1) / piece * piece})
-                    s = std::max({s, cut_h(w).slab_bytes(), cut_w(w).slab_bytes()});
-            slabs = c.take(s);
+                for (int64_t w : {std::min(piece, V), V - (V - 1) / piece * piece}) {
+                    sh = std::max(sh, cut_h(w).slab_bytes());
+                    sw = std::max(sw, cut_w(w).slab_bytes());
+                }
+            slabs_h = c.take(sh);
+            slabs_w = c.take(sw);
         }
         bytes = c.used;
     }
@@ -989,16 +1059,25 @@ template <class T, bool GRAD, bool TWO> int run_logits(LogitArgs a, int64_t toke
     return c.m_tiles;
 }
 
-template <class T, bool TA, class Out> void run_product(StoreArgs a, const Cut &c, hipStream_t s)
+// Both products of a piece, in one launch if their tiles have one shape.
+template <class T, class Out> void run_products(StoreArgs h, const Cut &ch, StoreArgs w, const Cut &cw, hipStream_t s)
 {
-    c.put(a.p);
-    auto go = [&](auto shape) {
+    ch.put(h.p);
+    cw.put(w.p);
+    auto go = [&](auto shape, int hb, int wb, int ht, int wt) {
         using S = decltype(shape);
-        k_product<T, S, TA, true, Out><<<(unsigned)c.blocks(), S::threads, 0, s>>>(a);
-        if (c.tail) k_slabs<S, Out><<<dim3((unsigned)c.tail, S::BM * S::BN / 1024), 256, 0, s>>>(a);
+        k_products<T, S, Out><<<(unsigned)(hb + wb), S::threads, 0, s>>>(h, w, hb);
+        if (ht + wt) k_slabs<S, Out><<<dim3((unsigned)(ht + wt), S::BM * S::BN / 1024), 256, 0, s>>>(h, w, ht);
     };
-    if (c.big) go(Big{});
-    else go(Small{});
+    auto by_shape = [&](bool big, int hb, int wb, int ht, int wt) {
+        if (big) go(Big{}, hb, wb, ht, wt);
+        else go(Small{}, hb, wb, ht, wt);
+    };
+    if (ch.big == cw.big) by_shape(ch.big, ch.blocks(), cw.blocks(), ch.tail, cw.tail);
+    else {
+        by_shape(ch.big, ch.blocks(), 0, ch.tail, 0);
+        by_shape(cw.big, 0, cw.blocks(), 0, cw.tail);
+    }
 }
 
 template <class Out> void run_finish(const StoreArgs &a, hipStream_t s)
@@ -1020,7 +1099,8 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
         if (a.N <= 16) k_few<In, 1><<<tiles, 64 * kFewWaves, 0, s>>>(f);
         else if (a.N <= 32) k_few<In, 2><<<tiles, 64 * kFewWaves, 0, s>>>(f);
         else k_few<In, 4><<<tiles, 64 * kFewWaves, 0, s>>>(f);
-        k_lse<<<token_blocks, 256, 0, s>>>(part, tiles, a.N, a.targets, a.V, z_target, a.loss, a.lse);
+        const LseArgs l{part, tiles, a.N, a.V, a.targets, z_target, a.loss, a.lse};
+        k_lse<In, T, TWO><<<token_blocks, 256, 0, s>>>(l, (int)token_blocks, PackArgs{});
         return hipGetLastError();
     }
     if (a.N == 0) {
@@ -1038,10 +1118,10 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     float *h_scale = (float *)(ws + p.h_scale), *w_scale = (float *)(ws + p.w_scale), *w_max = (float *)(ws + p.w_max);
     Operand h{ws + p.hp, p.kp, a.N * p.kp, a.N, 0}, w{ws + p.wp, p.kp, a.V * p.kp, a.V, 0};
     Operand w_all = w;  // for dhidden's product
-    if (TWO && grad) {
-        k_max<<<kMaxParts, 1024, 0, s>>>((const float *)a.weight, a.ld_weight, a.V, a.D, w_max);
-        w_all.p = ws + p.all;
-    }
+    const bool back = grad && a.D > 0;
+    UpParts *up_max = (UpParts *)(ws + p.up_max);
+    const UpArgs u{a.upstream, TWO ? h_scale : nullptr, a.targets, a.N, a.V, up_max};
+    if (TWO && back) w_all.p = ws + p.all;
     PackArgs k{};
     k.D = a.D;
     k.kp = p.kp;
@@ -1049,15 +1129,19 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     else {
         k.src = a.hidden, k.ld = a.ld_hidden, k.rows = a.N;
         k.dst = ws + p.hp, k.part = h.part, k.scale = h_scale;
-        k_pack<In, T, TWO><<<token_blocks, 256, 0, s>>>(k);
+        k_lay_hidden<In, T, TWO><<<token_blocks + (TWO && back ? kMaxParts : 0), 256, 0, s>>>(
+            k, (int)token_blocks, (const float *)a.weight, a.ld_weight, a.V, w_max);
     }
+    unsigned word_blocks = 0;
     if (!TWO && in_place(a.weight, a.ld_weight, a.D)) w.p = a.weight, w.ld = a.ld_weight;
     else {
+        word_blocks = (unsigned)ceil_div(a.V, 4);
         k.src = a.weight, k.ld = a.ld_weight, k.rows = a.V;
         k.dst = ws + p.wp, k.part = w.part, k.scale = w_scale;
-        if (TWO && grad) k.all = ws + p.all, k.w_max = w_max;
-        k_pack<In, T, TWO><<<(unsigned)ceil_div(a.V, 4), 256, 0, s>>>(k);
+        if (TWO && back) k.all = ws + p.all, k.w_max = w_max;
     }
+    if (word_blocks || back)
+        k_lay_weight<In, T, TWO><<<word_blocks + (back ? kUpParts : 0), 256, 0, s>>>(k, (int)word_blocks, u);
     if (!TWO) w_all = w;
     LogitArgs l{};
     l.p.a = w;
@@ -1072,20 +1156,18 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     l.part = part;
     l.z_target = z_target;
     const int tiles = run_logits<T, false, TWO>(l, a.N, s);
-    k_lse<<<token_blocks, 256, 0, s>>>(part, tiles, a.N, a.targets, a.V, z_target, a.loss, a.lse);
-    if (!grad || a.D == 0) return hipGetLastError();
-
-    UpMax *up_max = (UpMax *)(ws + p.up_max);
-    k_up_max<<<1, 1024, 0, s>>>(a.upstream, a.targets, TWO ? h_scale : nullptr, a.N, a.V, up_max);
+    const LseArgs sums{part, tiles, a.N, a.V, a.targets, z_target, a.loss, a.lse};
     const Operand hs{ws + p.hs, p.kp, a.N * p.kp, p.kp, a.N};
-    PackArgs u{};
-    u.src = a.hidden, u.ld = a.ld_hidden, u.rows = a.N, u.D = a.D;
-    u.dst = ws + p.hs, u.kp = p.kp, u.part = hs.part;
-    u.targets = a.targets, u.V = a.V, u.up = a.upstream, u.up_max = up_max;
-    k_pack<In, T, TWO><<<token_blocks, 256, 0, s>>>(u);
+    PackArgs v{};
+    v.src = a.hidden, v.ld = a.ld_hidden, v.rows = a.N, v.D = a.D;
+    v.dst = ws + p.hs, v.kp = p.kp, v.part = hs.part;
+    v.targets = a.targets, v.V = a.V, v.up = a.upstream, v.up_max = up_max;
+    k_lse<In, T, TWO><<<token_blocks * (back ? 2 : 1), 256, 0, s>>>(sums, (int)token_blocks, v);
+    if (!back) return hipGetLastError();
+
     StoreArgs d{};  // dhidden
     d.M = a.N, d.N = a.D;
-    d.slabs = (float *)(ws + p.slabs);
+    d.slabs = (float *)(ws + p.slabs_h);
     d.sum = p.piece < a.V ? (float *)(ws + p.sum) : nullptr;
     d.out = a.dhidden, d.ld_out = a.ld_dhidden;
     d.up = a.upstream, d.targets = a.targets, d.V = a.V;
@@ -1107,17 +1189,16 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
         d.p.terms = p.terms;
         d.p.k_tiles = (int)(kv / kBK);
         d.add = v0 > 0;
-        run_product<T, false, In>(d, p.cut_h(words), s);
         StoreArgs e{};  // dweight
         e.M = words, e.N = a.D;
-        e.slabs = d.slabs;
+        e.slabs = (float *)(ws + p.slabs_w);
         e.out = (In *)a.dweight + v0 * a.ld_dweight, e.ld_out = a.ld_dweight;
         e.up_max = up_max;
         e.p.a = Operand{ws + p.prob, kv, l.prob_part, kv, p.np};
         e.p.b = hs;
         e.p.terms = p.terms;
         e.p.k_tiles = (int)(p.np / kBK);
-        run_product<T, true, In>(e, p.cut_w(words), s);
+        run_products<T, In>(d, p.cut_h(words), e, p.cut_w(words), s);
     }
     if (d.sum) run_finish<In>(d, s);
     return hipGetLastError();

@@ -50,8 +50,9 @@ def test_embed_refusals():
 
 def test_embed_grad_refusals():
     f = seq.lib().tq_embed_grad
-    need = space(seq.lib().tq_embed_grad_workspace, 5, 8, 3)
-    ok = [P, 8, BF16, 5, 8, P, 3, 1.0, P, 8, P, need, None]
+    need = space(seq.lib().tq_embed_grad_workspace, 5, 8, 3000)
+    assert need > 0 and space(seq.lib().tq_embed_grad_workspace, 5, 8, 3) == 0
+    ok = [P, 8, BF16, 5, 8, P, 3000, 1.0, P, 8, P, need, None]
     for k, v in ((0, None), (1, 7), (2, 9), (3, -1), (5, None), (8, None), (9, 7), (10, None), (10, P + 16),
                  (11, need - 1), (0, P + 1)):
         refused(tq.TQ_E_INVALID, f, *changed(ok, k, v))
