@@ -69,7 +69,8 @@ tq_status tq_embed_grad(const void *grad_out, int64_t ld_grad_out, int32_t type,
  * tq_gated_scan_grad starts from: float [B, ceil(T / TQ_SCAN_PIECE), D], the
  * state before step j * TQ_SCAN_PIECE (steps past a record's length: not
  * written).
- * h0, h_last and states are contiguous. */
+ * h0, h_last and states are contiguous.  TQ_E_UNSUPPORTED for D > 2^20 or
+ * B ceil(D / 64) ceil(T / 64) >= 2^31. */
 #define TQ_SCAN_PIECE 64
 tq_status tq_gated_scan_workspace(int64_t B, int64_t T, int64_t D, size_t *bytes);
 tq_status tq_gated_scan(int32_t type, int64_t B, int64_t T, int64_t D, const void *x, int64_t x_batch, int64_t x_step,

@@ -77,6 +77,7 @@ void check_scan(const char *call, int type, int64_t B, int64_t T, int64_t D)
     check_size(call, "B", B);
     check_size(call, "T", T);
     check_size(call, "D", D);
+    if (D > kMaxWidth) fail(TQ_E_UNSUPPORTED, text(call, "D must be at most 2^20"));
     // rows x segments of 64 steps, in doubles: the product of three sizes
     if ((double)B * (double)((D + 63) / 64) * (double)((T + 63) / 64) > kMaxIndex ||
         scan_items(B, T, D) > kMaxIndex)

@@ -11,12 +11,13 @@
 //
 // The state a segment starts from comes from the pairs of the segments before
 // it, which their workgroups publish as soon as they have them, and replace by
-// (0, state at the segment's end) once they know that: looking back from the
-// nearest segment, the composition is complete as soon as A = 0.  A slot of all
-// ones is not published yet.  Workgroups take their segments in the order in which
-// they start (a ticket), earlier segments of all rows first, and wait for
-// segments with lower tickets only; the lowest ticket that is not done waits
-// for nobody, so every wait ends.
+// the state at the segment's end once they know that.  A workgroup looks back
+// until it meets a state and goes forwards from there, pair by pair: whichever
+// state it met, the result is that of one step after the other, to the bit.  A
+// slot of all ones is not published yet.  Workgroups take their segments in the
+// order in which they start (a ticket), earlier segments of all rows first, and
+// wait for segments with lower tickets only; the lowest ticket that is not done
+// waits for nobody, so every wait ends.
 //
 // The backward pass walks time the other way.  Pairs forwards give h_{t-1} from
 // the saved state before the piece of TQ_SCAN_PIECE steps, and
@@ -68,8 +69,12 @@ template <class T> __device__ __forceinline__ void gate(float g, float &a, float
 }
 
 // ------------------------------------------------------------ published pairs
+// A pair (A, B), A >= 0, or a state (-0, h): one 64-bit access, of which a reader
+// sees all or nothing.  Agent scope reaches the other XCDs; nothing else is
+// handed over, so no ordering is needed.
 using Slot = unsigned long long;
 constexpr Slot kEmpty = ~(Slot)0;
+constexpr uint32_t kState = 0x80000000u;
 
 struct Geom {
     uint32_t rows, slabs;  // rows: records x slabs
@@ -78,22 +83,25 @@ struct Geom {
     unsigned *ticket;
 };
 
-// One 64-bit access per pair: a reader sees all of it or none.  Agent scope
-// reaches the other XCDs; nothing else is handed over, so no ordering is needed.
-__device__ __forceinline__ void publish(Slot *p, float a, float b)
+__device__ __forceinline__ void publish(Slot *p, uint32_t hi, float b)
 {
-    const uint32_t hi = a == a ? __float_as_uint(a) : 0x7fc00000u;  // a NaN, but not kEmpty
     __hip_atomic_store(p, (Slot)hi << 32 | __float_as_uint(b), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void publish_pair(Slot *p, float a, float b)
+{
+    publish(p, a == a ? __float_as_uint(a) : 0x7fc00000u, b);  // a NaN, but not kEmpty
 }
 __device__ __forceinline__ Slot look(const Slot *p)
 {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// The pair at p, which was `v` when last looked at.  The count only keeps a
-// broken launch from running for good: it is a matter of seconds.
-__device__ __forceinline__ float2 await(const Slot *p, Slot v)
+__device__ __forceinline__ bool is_state(float a) { return __float_as_uint(a) == kState; }
+// What is at p, which was `v` when last looked at, once it is published, or
+// (`state`) once it is a state.  The count only keeps a broken launch from
+// running for good: it is a matter of seconds.
+__device__ __forceinline__ float2 await(const Slot *p, Slot v, bool state)
 {
-    for (int k = 0; v == kEmpty && k < 1 << 22; k++) {
+    for (int k = 0; (v == kEmpty || (state && (uint32_t)(v >> 32) != kState)) && k < 1 << 22; k++) {
         __builtin_amdgcn_s_sleep(1);
         v = look(p);
     }
@@ -218,49 +226,54 @@ __device__ __forceinline__ void put(typename K::T *p, int64_t step, int64_t T, c
     }
 }
 
-// The state the segment starts from: `first` if it is the first of its row,
-// else the composition of the segments before it.  Each wavefront looks at one
-// slot of a window; all wavefronts get the same result.
+// The state the segment starts from: `first` if it is the first of its row.
+// Each wavefront looks at one slot of a window of kWaves, the nearest window
+// first; the last of the kWindows windows waits for a state in its oldest slot.
+// All wavefronts get the same result.
+constexpr int kWindows = 4;
 template <class K>
 __device__ __forceinline__ void look_back(const Geom &g, const Place<K> &at, float2 (*win)[kWaves][K::slab],
                                           const float (&first)[K::CV], float (&h)[K::CV])
 {
     constexpr int CV = K::CV;
-    float P[CV];
-#pragma unroll
-    for (int j = 0; j < CV; j++) P[j] = 1.f, h[j] = 0.f;
-    int turn = 0;
-    for (int top = at.seg - 1; top >= at.seg0; top -= kWaves, turn ^= 1) {
-        const int s = top - at.wave;
+    const int before = at.seg - at.seg0;  // segments of the row before this one
+    int seen = 0;                         // of them, in `win`
+    bool found[CV] = {};
+    for (int k = 0; k < kWindows && seen < before; k++) {
+        const int back = k * kWaves + at.wave;
         float2 q[CV];
 #pragma unroll
         for (int j = 0; j < CV; j++) q[j] = make_float2(1.f, 0.f);
-        if (s >= at.seg0) {
-            const Slot *p = g.slots + ((int64_t)s * g.rows + at.row) * K::slab + at.lane * CV;
+        if (back < before) {
+            const Slot *p = g.slots + ((int64_t)(at.seg - 1 - back) * g.rows + at.row) * K::slab + at.lane * CV;
             Slot v[CV];
 #pragma unroll
             for (int j = 0; j < CV; j++) v[j] = look(p + j);
 #pragma unroll
-            for (int j = 0; j < CV; j++) q[j] = await(p + j, v[j]);
+            for (int j = 0; j < CV; j++) q[j] = await(p + j, v[j], back == kWindows * kWaves - 1);
         }
 #pragma unroll
-        for (int j = 0; j < CV; j++) win[turn][at.wave][at.lane * CV + j] = q[j];
+        for (int j = 0; j < CV; j++) win[k][at.wave][at.lane * CV + j] = q[j];
         __syncthreads();
-        bool more = false;
+        seen = min((k + 1) * kWaves, before);
+        bool all = true;
 #pragma unroll
-        for (int w = 0; w < kWaves; w++)
+        for (int j = 0; j < CV; j++) {
 #pragma unroll
-            for (int j = 0; j < CV; j++) {
-                const float2 r = win[turn][w][at.lane * CV + j];
-                h[j] = fmaf(P[j], r.y, h[j]);
-                P[j] *= r.x;
-            }
-#pragma unroll
-        for (int j = 0; j < CV; j++) more = more || P[j] != 0.f;
-        if (!__any(more)) return;  // the same in every wavefront
+            for (int w = 0; w < kWaves; w++) found[j] = found[j] || is_state(win[k][w][at.lane * CV + j].x);
+            all = all && found[j];
+        }
+        if (__all(all)) break;  // the same in every wavefront
     }
+    // from the oldest slot on: a state starts anew
 #pragma unroll
-    for (int j = 0; j < CV; j++) h[j] = fmaf(P[j], first[j], h[j]);
+    for (int j = 0; j < CV; j++) h[j] = first[j];
+    for (int back = seen - 1; back >= 0; back--)
+#pragma unroll
+        for (int j = 0; j < CV; j++) {
+            const float2 q = win[back / kWaves][back % kWaves][at.lane * CV + j];
+            h[j] = is_state(q.x) ? q.y : fmaf(q.x, h[j], q.y);
+        }
 }
 
 // ------------------------------------------------------------------ forward
@@ -268,7 +281,7 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArg
 {
     using T = typename K::T;
     constexpr int CV = K::CV, L = K::steps;
-    __shared__ float2 agg[kWaves][K::slab], win[2][kWaves][K::slab];
+    __shared__ float2 agg[kWaves][K::slab], win[kWindows][kWaves][K::slab];
     const Place<K> at(a, g, take_item(g), false);
     T *y = (T *)a.y + at.b * a.yb + at.t0 * a.ys;
     float ga[L][CV], gb[L][CV], A[CV], B[CV];
@@ -327,15 +340,14 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArg
             }
 #pragma unroll
         for (int j = 0; j < CV; j++) {
-            if (j >= at.n) wholeA[j] = wholeB[j] = 0.f;  // lanes past D ask for nothing more
-            if (at.seg > at.seg0) publish(slot + j, wholeA[j], wholeB[j]);
+            if (at.seg > at.seg0) publish_pair(slot + j, wholeA[j], wholeB[j]);
         }
     }
     float h[CV];
     look_back<K>(g, at, win, first, h);
     if (shared)
 #pragma unroll
-        for (int j = 0; j < CV; j++) publish(slot + j, 0.f, fmaf(wholeA[j], h[j], wholeB[j]));
+        for (int j = 0; j < CV; j++) publish(slot + j, kState, fmaf(wholeA[j], h[j], wholeB[j]));
     for (int w = 0; w < at.wave; w++)
 #pragma unroll
         for (int j = 0; j < CV; j++) {
@@ -367,7 +379,7 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(Sc
 {
     using T = typename K::T;
     constexpr int CV = K::CV, L = K::steps, kBefore = kPiece / L;  // wavefronts of a piece
-    __shared__ float2 agg[kWaves][K::slab], win[2][kWaves][K::slab];
+    __shared__ float2 agg[kWaves][K::slab], win[kWindows][kWaves][K::slab];
     __shared__ float rev[kWaves][K::slab];
     const Place<K> at(a, g, take_item(g), true);
     T *dx = (T *)a.dx + at.b * a.dxb + at.t0 * a.dxs, *dg = (T *)a.dg + at.b * a.dgb + at.t0 * a.dgs;
@@ -444,8 +456,7 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(Sc
             }
 #pragma unroll
         for (int j = 0; j < CV; j++) {
-            if (j >= at.n) wholeA[j] = wholeB[j] = 0.f;
-            if (shared && at.seg > at.seg0) publish(slot + j, wholeA[j], wholeB[j]);
+            if (shared && at.seg > at.seg0) publish_pair(slot + j, wholeA[j], wholeB[j]);
         }
     }
     float m[CV];
@@ -454,7 +465,7 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(Sc
 #pragma unroll
         for (int j = 0; j < CV; j++) {
             const float out = fmaf(wholeA[j], m[j], wholeB[j]);
-            if (shared) publish(slot + j, 0.f, out);
+            if (shared) publish(slot + j, kState, out);
             if (a.dh0 && at.seg == g.segs - 1 && j < at.n) a.dh0[at.b * a.D + at.c0 + j] = out;
         }
     for (int w = kWaves - 1; w > at.wave; w--)

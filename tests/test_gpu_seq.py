@@ -223,6 +223,22 @@ def test_gated_scan_saturated_gates(ty):
     assert torch.all(dg == 0) and torch.all(dh0 == 0)
 
 
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("B,T,D", [(1, 20011, 331), (13, 3000, 200)])
+def test_gated_scan_is_reproducible(ty, B, T, D):
+    """The same bits whatever the order in which segments finish."""
+    dtype = TYPES[ty][0]
+    x, g = torch.randn((2, B, T, D), device="cuda").to(dtype).unbind(0)
+    g = (g * 2 + 3).to(dtype)
+    dy, dh = torch.randn((B, T, D), device="cuda").to(dtype), torch.randn((B, D), device="cuda")
+    want = None
+    for _ in range(6):
+        y, h, states = seq.gated_scan(x, g, keep=True)
+        out = (y, h, states) + seq.gated_scan_grad(x, g, states, dy, dh_last=dh)
+        want = want or [o.clone() for o in out]
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
 def test_gated_scan_nothing_to_do():
     z = torch.zeros((2, 0, 5), device="cuda")
     h0 = torch.ones((2, 5), device="cuda")
