@@ -98,7 +98,9 @@ typedef const __attribute__((address_space(1))) void global_void;
 // from global memory, 16 bytes per lane.
 //
 // Along K: W rows of eight 16-byte pieces, the pieces of row r in the order
-// piece ^ (r % 8), so that 32 lanes reading one piece of 32 rows meet all banks.
+// piece ^ (r / 2 % 8): two rows fill the 64 banks once, so that the 16 lanes that
+// read one piece of 16 rows at a time meet all banks.  (With piece ^ (r % 8) rows
+// r and r + 8 met, and half of the LDS cycles were conflicts.)
 template <class T, int W, int WAVES>
 __device__ __forceinline__ void stage(T *lds, const T *src, const Operand &o, int64_t k0, int64_t at, int wave, int lane)
 {
@@ -106,20 +108,20 @@ __device__ __forceinline__ void stage(T *lds, const T *src, const Operand &o, in
     for (int i = 0; i < W / 8 / WAVES; i++) {
         const int r8 = (i * WAVES + wave) * 8;
         const int64_t row = min(at + r8 + (lane >> 3), o.extent - 1);
-        const T *g = src + row * o.ld + k0 + ((lane & 7) ^ (lane >> 3)) * 8;
+        const T *g = src + row * o.ld + k0 + ((lane & 7) ^ (((r8 >> 1) + (lane >> 4)) & 7)) * 8;
         __builtin_amdgcn_global_load_lds((global_void *)g, (lds_void *)(lds + r8 * kBK), 16, 0, 0);
     }
 }
 template <class T> __device__ __forceinline__ frag<T> read_frag(const T *lds, int at, int ks, int lane)
 {
     const int row = at + (lane & 31), piece = ks * 2 + (lane >> 5);
-    return *(const frag<T> *)(lds + row * kBK + ((piece ^ (row & 7)) * 8));
+    return *(const frag<T> *)(lds + row * kBK + ((piece ^ ((row >> 1) & 7)) * 8));
 }
 
 // Across K: kBK rows of W elements.  The transposing LDS read gives 16 lanes
 // four rows each of 16 columns, from 8 bytes at four rows by four pieces of four
-// elements; row k has its 16-byte pieces in the order piece ^ 2 (k % 4), so
-// that the four rows lie in different banks.
+// elements; row k has its 16-byte pieces in the order piece ^ 4 (k % 4), so
+// that four rows of 32 columns, which 32 lanes read at a time, meet all banks.
 template <class T, int W, int WAVES>
 __device__ __forceinline__ void stage_t(T *lds, const T *src, const Operand &o, int64_t k0, int64_t at, int wave,
                                         int lane)
@@ -130,7 +132,7 @@ __device__ __forceinline__ void stage_t(T *lds, const T *src, const Operand &o, 
     for (int i = 0; i < kBK / ROWS / WAVES; i++) {
         const int r0 = (i * WAVES + wave) * ROWS, r = r0 + lane / PIECES;
         const int64_t k = min(k0 + r, o.k_rows - 1);
-        int64_t col = at + ((lane % PIECES) ^ (2 * (r & 3))) * 8;
+        int64_t col = at + ((lane % PIECES) ^ (4 * (r & 3))) * 8;
         if (col >= o.extent) col = 0;
         __builtin_amdgcn_global_load_lds((global_void *)(src + k * o.ld + col), (lds_void *)(lds + r0 * W), 16, 0, 0);
     }
@@ -141,7 +143,7 @@ template <class T, int W> __device__ __forceinline__ frag<T> read_frag_t(const T
 {
     const int i = lane & 15, g = lane >> 4;
     const int k = ks * 16 + 8 * (g >> 1) + (i >> 2), col = at + 16 * (g & 1) + 4 * (i & 3);
-    const T *p = lds + k * W + (((col >> 3) ^ (2 * ((i >> 2) & 3))) * 8) + (col & 7);
+    const T *p = lds + k * W + (((col >> 3) ^ (4 * ((i >> 2) & 3))) * 8) + (col & 7);
     union {
         s16x4 half[2];
         frag<T> all;
