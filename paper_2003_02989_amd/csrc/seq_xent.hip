@@ -75,7 +75,7 @@ struct ProductArgs {
     int k_tiles;  // K / kBK
     int m_tiles, n_tiles;
     int full;     // tiles that one workgroup computes alone; the others are
-    int splits;   // cut along K into this many
+    int splits;   // cut into this many, along K or (logits) along N
 };
 
 // Tile of C, wavefronts WM x WN, each with FM x FN blocks of 32 x 32.
@@ -86,6 +86,9 @@ template <int WM_, int WN_, int FM_, int FN_> struct Shape {
 };
 using Big = Shape<2, 4, 4, 2>;    // 256 x 256
 using Small = Shape<2, 2, 2, 2>;  // 128 x 128
+// A half and a quarter of a large tile, for logits of a last, incomplete round.
+using Half = Shape<4, 2, 2, 2>;     // 256 x 128
+using Quarter = Shape<4, 2, 2, 1>;  // 256 x 64
 
 // Where an element of a wavefront's block lies: C row (within 32) of register i
 // of a lane; its column is lane % 32.
@@ -153,7 +156,7 @@ template <class T, int W> __device__ __forceinline__ frag<T> read_frag_t(const T
     return u.all;
 }
 
-template <class T, class S> struct Stages {
+template <class T> struct Stages {
     T *a0, *b0, *a1, *b1;
 };
 // The four arrays are separate objects: the compiler then knows that reads of
@@ -161,11 +164,11 @@ template <class T, class S> struct Stages {
 #define TQ_STAGES(T, S, name)                                                                                          \
     __shared__ alignas(1024) T name##_a0[S::BM * kBK], name##_b0[S::BN * kBK], name##_a1[S::BM * kBK],                 \
         name##_b1[S::BN * kBK];                                                                                        \
-    const Stages<T, S> name{name##_a0, name##_b0, name##_a1, name##_b1}
+    const Stages<T> name{name##_a0, name##_b0, name##_a1, name##_b1}
 
 // The sums of the tile at (m0, n0) over the K tiles [k0, k1) (of all terms).
 template <class T, class S, bool TA, bool TB>
-__device__ __forceinline__ void product(const ProductArgs &a, const Stages<T, S> &l, int64_t m0, int64_t n0, int k0,
+__device__ __forceinline__ void product(const ProductArgs &a, const Stages<T> &l, int64_t m0, int64_t n0, int k0,
                                         int k1, f32x16 (&acc)[S::FM][S::FN])
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -282,12 +285,12 @@ struct LogitArgs {
     int64_t ld_prob, prob_rows, prob_part;
 };
 
-template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S::threads) void k_logits(LogitArgs a)
+//
+// join: S::WM rows of S::BN, in LDS (GRAD: unused).
+template <class T, class S, bool GRAD, bool TWO>
+__device__ __forceinline__ void logits_tile(const LogitArgs &a, const Stages<T> &lds, float2 *join, int64_t m0, int64_t n0)
 {
-    TQ_STAGES(T, S, lds);
-    const Tile t = tile_of(a.p, blockIdx.x);
     f32x16 acc[S::FM][S::FN];
-    const int64_t m0 = t.m * S::BM, n0 = t.n * S::BN;
     product<T, S, false, false>(a.p, lds, m0, n0, 0, a.p.terms * a.p.k_tiles, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
@@ -312,7 +315,6 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
             }
     }
     if constexpr (!GRAD) {
-        __shared__ float2 join[S::WM][S::BN];
 #pragma unroll
         for (int j = 0; j < S::FN; j++) {
             const int64_t n = n0 + wn + j * 32 + (lane & 31);
@@ -353,17 +355,17 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
                 for (int e = 0; e < 16; e++) sum4[e & 3] += exp_less(acc[i][j][e], ref2);
             float sum = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
             sum += __shfl_xor(sum, 32, 64);
-            if (lane < 32) join[wave / S::WN][wn + j * 32 + lane] = make_float2(top, sum);
+            if (lane < 32) join[wave / S::WN * S::BN + wn + j * 32 + lane] = make_float2(top, sum);
         }
         __syncthreads();
         for (int c = threadIdx.x; c < S::BN; c += S::threads) {
             float top = -INFINITY, sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < S::WM; w++) top = fmaxf(top, join[w][c].x);
+            for (int w = 0; w < S::WM; w++) top = fmaxf(top, join[w * S::BN + c].x);
             const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int w = 0; w < S::WM; w++) sum += join[w][c].y * __expf(join[w][c].x - ref);
-            if (n0 + c < a.N) a.part[(n0 + c) * a.p.m_tiles + t.m] = make_float2(top, sum);
+            for (int w = 0; w < S::WM; w++) sum += join[w * S::BN + c].y * __expf(join[w * S::BN + c].x - ref);
+            if (n0 + c < a.N) a.part[(n0 + c) * a.p.m_tiles + m0 / S::BM] = make_float2(top, sum);
         }
     } else {
 #pragma unroll
@@ -409,7 +411,7 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
                         : wave / PER == 2 ? lds.a1
                                           : lds.b1) +
                        wave % PER * WORDS * TOKENS;
-#pragma unroll
+#pragma unroll 1  // unrolled, the addresses of both parts stay in registers and spill
         for (int part = 0; part < (TWO ? 2 : 1); part++) {
 #pragma unroll
             for (int j = 0; j < S::FN; j++) {
@@ -423,7 +425,7 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
                         for (int e = 0; e < 4; e++) {
                             const float p = acc[i][j][4 * q + e];
                             four[e] = (T)p;
-                            if (part == 0) acc[i][j][4 * q + e] = TWO ? p - (float)four[e] : p;
+                            if constexpr (TWO) acc[i][j][4 * q + e] = p - (float)four[e];
                         }
                         const int piece = i * 4 + q;
                         __builtin_memcpy(__builtin_assume_aligned(buf + row * WORDS + ((piece ^ (row & (PIECES - 1))) * 8) +
@@ -444,6 +446,25 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
             wave_fence();
         }
     }
+}
+
+// Large tiles of a last, incomplete round go in halves or quarters of their
+// tokens: an epilogue follows the whole sum, so that they are not cut along K.
+template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S::threads) void k_logits(LogitArgs a)
+{
+    TQ_STAGES(T, S, lds);
+    __shared__ float2 join[GRAD ? 1 : std::max(S::WM * S::BN, Half::WM * Half::BN)];
+    const Tile t = tile_of(a.p, blockIdx.x);
+    const int64_t m0 = t.m * S::BM, n0 = t.n * S::BN;
+    if constexpr (std::is_same_v<S, Big>)
+        if (t.split >= 0) {
+            const int64_t n = n0 + t.split * (S::BN / a.p.splits);
+            if (n >= (GRAD ? a.prob_rows : a.N)) return;
+            if (a.p.splits == 4) logits_tile<T, Quarter, GRAD, TWO>(a, lds, join, m0, n);
+            else logits_tile<T, Half, GRAD, TWO>(a, lds, join, m0, n);
+            return;
+        }
+    logits_tile<T, S, GRAD, TWO>(a, lds, join, m0, n0);
 }
 
 // ------------------------------------------------------------ the products
@@ -535,7 +556,7 @@ struct Factor {
 };
 
 template <class T, class S, bool TA, class Out>
-__device__ __forceinline__ void product_tile(const StoreArgs &a, const Stages<T, S> &lds, int blk)
+__device__ __forceinline__ void product_tile(const StoreArgs &a, const Stages<T> &lds, int blk)
 {
     const Tile t = tile_of(a.p, blk);
     f32x16 acc[S::FM][S::FN];
@@ -949,37 +970,56 @@ int64_t ceil_div(int64_t n, int64_t m) { return (n + m - 1) / m; }
 
 // How C [M, N] is cut into tiles.  Tiles go to the compute units in rounds (256
 // large ones or 512 small ones, two to a compute unit, at a time); the tiles of
-// a last, incomplete round are cut along K (where that is possible) so that
-// they fill it.  The shape with fewer rounds is taken, a round of small tiles
-// counting 5/8 of one of large ones: half the work, at four fifths of the rate.
+// a last, incomplete round are cut along K so that they fill it, those of logits,
+// if large, in two or four along the tokens.
+//
+// What a cut costs is estimated in steps, a large tile's kBK of K (2.2 us): a small
+// tile's count 5/8, half the work at four fifths of the rate; a tile begins and ends in
+// three; writing and adding up the slabs of a round takes twelve.
 struct Cut {
     bool big;
     int m_tiles, n_tiles, full, splits, tail;
-    double rounds;
-    template <class S> static Cut of(int64_t M, int64_t N, int64_t k_tiles, bool split)
+    double work, slabs;        // steps of all tiles over the slots, and of the slabs
+    double longest;            // of a tile of the last round
+    int slots() const { return big ? 256 : 512; }
+    // room: what the parts of the last round may take, up to slots
+    template <class S> static Cut of(int64_t M, int64_t N, int64_t k_tiles, int room)
     {
+        constexpr double kEnds = 3, kSlabs = 12;
         Cut c{};
         c.big = std::is_same_v<S, Big>;
-        const int slots = c.big ? 256 : 512;
+        const int slots = c.slots();
+        const double scale = c.big ? 1. : 0.625;
         c.m_tiles = (int)ceil_div(M, S::BM);
         c.n_tiles = (int)ceil_div(N, S::BN);
         const int tiles = c.m_tiles * c.n_tiles;
         c.tail = tiles % slots;
         c.splits = 1;
-        if (split && c.tail)
-            c.splits = (int)std::max<int64_t>(1, std::min({(int64_t)(slots / c.tail), k_tiles / 4, (int64_t)16}));
-        c.rounds = tiles / slots + (c.tail ? 1.0 / c.splits + (c.splits > 1 ? 0.1 : 0.0) : 0.0);
+        auto slabs = [&](int q) { return q > 1 ? kSlabs * c.tail * q / slots : 0.; };
+        auto last = [&](int q) { return (double)ceil_div(k_tiles, q) + kEnds + slabs(q); };
+        for (int q = 2; q <= 16 && (int64_t)c.tail * q <= room && k_tiles / q >= 4; q++)
+            if (last(q) < last(c.splits)) c.splits = q;
+        c.work = scale * tiles / slots * (k_tiles + kEnds);
+        c.slabs = scale * slabs(c.splits);
+        c.longest = scale * (ceil_div(k_tiles, c.tail ? c.splits : 1) + kEnds);
         if (c.splits == 1) c.tail = 0;
         c.full = tiles - c.tail;
-        if (!c.big) c.rounds *= 0.625;
         return c;
     }
-    Cut() = default;
-    Cut(int64_t M, int64_t N, int64_t k_tiles, bool split)
+    // of logits
+    template <class S> static Cut logits(int64_t M, int64_t N)
     {
-        const Cut b = of<Big>(M, N, k_tiles, split), s = of<Small>(M, N, k_tiles, split);
-        *this = b.rounds <= s.rounds ? b : s;
+        Cut c = of<S>(M, N, 1, 0);
+        c.tail = c.full % c.slots();
+        if (c.big && c.tail) c.splits = c.tail <= c.slots() / 4 ? 4 : c.tail <= c.slots() / 2 ? 2 : 1;
+        const double rounds = c.full / c.slots() + (c.tail ? 1. / c.splits + (c.splits > 1 ? 0.1 : 0.) : 0.);
+        c.work = rounds * (c.big ? 1. : 0.625);
+        if (c.splits == 1) c.tail = 0;
+        c.full -= c.tail;
+        return c;
     }
+    // steps of a launch of its own
+    double steps() const { return slabs + (blocks() <= slots() ? longest : work + 0.5 * longest); }
     int blocks() const { return full + tail * splits; }
     size_t slab_bytes() const
     {
@@ -995,6 +1035,50 @@ struct Cut {
     }
 };
 
+Cut cut_logits(int64_t M, int64_t N)
+{
+    const Cut b = Cut::logits<Big>(M, N), s = Cut::logits<Small>(M, N);
+    return b.work <= s.work ? b : s;
+}
+
+// dhidden's and dweight's products.  Of one shape they share a launch, dhidden's
+// tiles first, where one fills what the other leaves free of a round; else two more
+// launches take as long as eight steps.
+struct Cuts {
+    Cut h, w;
+    double steps() const
+    {
+        if (h.big != w.big) return h.steps() + w.steps() + 8;
+        const double longest = std::max(h.longest, w.longest);
+        if (h.blocks() + w.blocks() <= h.slots()) return h.slabs + w.slabs + longest;
+        return h.slabs + w.slabs + std::max(longest, h.work + w.work + 0.5 * w.longest);
+    }
+};
+Cuts cut_products(int64_t N, int64_t D, int64_t words, int64_t h_tiles, int64_t w_tiles)
+{
+    Cuts best{};
+    double least = INFINITY;
+    auto take = [&](const Cut &h, const Cut &w) {
+        const Cuts c{h, w};
+        if (c.steps() < least) least = c.steps(), best = c;
+    };
+    auto shape = [&](auto s) {
+        using S = decltype(s);
+        const int slots = std::is_same_v<S, Big> ? 256 : 512;
+        const Cut h = Cut::of<S>(N, D, h_tiles, slots), w = Cut::of<S>(words, D, w_tiles, slots);
+        take(h, w);
+        // both in one round: what either leaves of it is the other's
+        const Cut whole = Cut::of<S>(N, D, h_tiles, 0);
+        take(Cut::of<S>(N, D, h_tiles, slots - w.blocks()), w);
+        take(whole, Cut::of<S>(words, D, w_tiles, slots - whole.blocks()));
+        return Cuts{h, w};
+    };
+    const Cuts b = shape(Big{}), s = shape(Small{});
+    take(b.h, s.w);
+    take(s.h, b.w);
+    return best;
+}
+
 // Sizes and workspace of a call.
 struct XentPlan {
     bool two, few;
@@ -1003,8 +1087,10 @@ struct XentPlan {
     int64_t piece;  // words of a piece of the vocabulary
     size_t part, z_target, hp, wp, all, hs, h_scale, w_scale, w_max, up_max, prob, sum, slabs_h, slabs_w, bytes;
 
-    Cut cut_h(int64_t words) const { return Cut(N, D, terms * (up_to(words, kBK) / kBK), true); }
-    Cut cut_w(int64_t words) const { return Cut(words, D, terms * (np / kBK), true); }
+    Cuts cuts(int64_t words) const
+    {
+        return cut_products(N, D, words, terms * (up_to(words, kBK) / kBK), terms * (np / kBK));
+    }
 
     XentPlan(int32_t type, int64_t N_, int64_t V_, int64_t D_, bool grad)
         : two(type == TQ_F32), few(!grad && N_ <= kFewTokens), terms(two ? 3 : 1), N(N_), V(V_), D(D_)
@@ -1036,8 +1122,9 @@ struct XentPlan {
             size_t sh = 0, sw = 0;
             if (D)
                 for (int64_t w : {std::min(piece, V), V - (V - 1) / piece * piece}) {
-                    sh = std::max(sh, cut_h(w).slab_bytes());
-                    sw = std::max(sw, cut_w(w).slab_bytes());
+                    const Cuts c = cuts(w);
+                    sh = std::max(sh, c.h.slab_bytes());
+                    sw = std::max(sw, c.w.slab_bytes());
                 }
             slabs_h = c.take(sh);
             slabs_w = c.take(sw);
@@ -1054,7 +1141,7 @@ bool in_place(const void *p, int64_t ld, int64_t D)
 
 template <class T, bool GRAD, bool TWO> int run_logits(LogitArgs a, int64_t tokens, hipStream_t s)
 {
-    const Cut c(a.p.a.extent, tokens, a.p.terms * a.p.k_tiles, false);
+    const Cut c = cut_logits(a.p.a.extent, tokens);
     c.put(a.p);
     if (c.big) k_logits<T, Big, GRAD, TWO><<<(unsigned)c.blocks(), Big::threads, 0, s>>>(a);
     else k_logits<T, Small, GRAD, TWO><<<(unsigned)c.blocks(), Small::threads, 0, s>>>(a);
@@ -1062,8 +1149,9 @@ template <class T, bool GRAD, bool TWO> int run_logits(LogitArgs a, int64_t toke
 }
 
 // Both products of a piece, in one launch if their tiles have one shape.
-template <class T, class Out> void run_products(StoreArgs h, const Cut &ch, StoreArgs w, const Cut &cw, hipStream_t s)
+template <class T, class Out> void run_products(StoreArgs h, StoreArgs w, const Cuts &c, hipStream_t s)
 {
+    const Cut &ch = c.h, &cw = c.w;
     ch.put(h.p);
     cw.put(w.p);
     auto go = [&](auto shape, int hb, int wb, int ht, int wt) {
@@ -1200,7 +1288,7 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
         e.p.b = hs;
         e.p.terms = p.terms;
         e.p.k_tiles = (int)(p.np / kBK);
-        run_products<T, In>(d, p.cut_h(words), e, p.cut_w(words), s);
+        run_products<T, In>(d, e, p.cuts(words), s);
     }
     if (d.sum) run_finish<In>(d, s);
     return hipGetLastError();

@@ -365,6 +365,13 @@ def test_softmax_xent_and_gradients(ty, N, V, D):
 
 
 @pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("N,V,D", [(4200, 4100, 40), (4099, 1025, 300), (2500, 4097, 33), (600, 9001, 260)])
+def test_softmax_xent_many_tiles(ty, N, V, D):
+    """More tiles than compute units, and last rounds cut in two, in four and not at all."""
+    test_softmax_xent_and_gradients(ty, N, V, D)
+
+
+@pytest.mark.parametrize("ty", TYPES)
 @pytest.mark.parametrize("N", [5, 200])
 def test_softmax_xent_bad_rows_without_targets(ty, N):
     """Rows without a target may hold anything; so may their upstream."""
