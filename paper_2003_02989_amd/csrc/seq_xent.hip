@@ -1071,6 +1071,8 @@ Cuts cut_products(int64_t N, int64_t D, int64_t words, int64_t h_tiles, int64_t 
         const Cut whole = Cut::of<S>(N, D, h_tiles, 0);
         take(Cut::of<S>(N, D, h_tiles, slots - w.blocks()), w);
         take(whole, Cut::of<S>(words, D, w_tiles, slots - whole.blocks()));
+        const int share = (int)(slots * h.work / (h.work + w.work));
+        take(Cut::of<S>(N, D, h_tiles, share), Cut::of<S>(words, D, w_tiles, slots - share));
         return Cuts{h, w};
     };
     const Cuts b = shape(Big{}), s = shape(Small{});
@@ -1087,7 +1089,8 @@ struct XentPlan {
     int64_t piece;  // words of a piece of the vocabulary
     size_t part, z_target, hp, wp, all, hs, h_scale, w_scale, w_max, up_max, prob, sum, slabs_h, slabs_w, bytes;
 
-    Cuts cuts(int64_t words) const
+    Cuts cuts, last_cuts;  // of a piece's products, of the last one's
+    Cuts cuts_of(int64_t words) const
     {
         return cut_products(N, D, words, terms * (up_to(words, kBK) / kBK), terms * (np / kBK));
     }
@@ -1120,12 +1123,13 @@ struct XentPlan {
             prob = c.take(elem * np * words);
             sum = c.take(piece < V ? sizeof(float) * N * D : 0);
             size_t sh = 0, sw = 0;
-            if (D)
-                for (int64_t w : {std::min(piece, V), V - (V - 1) / piece * piece}) {
-                    const Cuts c = cuts(w);
-                    sh = std::max(sh, c.h.slab_bytes());
-                    sw = std::max(sw, c.w.slab_bytes());
-                }
+            if (D) {
+                const int64_t left = V - (V - 1) / piece * piece;
+                last_cuts = cuts_of(left);
+                cuts = left < V ? cuts_of(piece) : last_cuts;
+                sh = std::max(cuts.h.slab_bytes(), last_cuts.h.slab_bytes());
+                sw = std::max(cuts.w.slab_bytes(), last_cuts.w.slab_bytes());
+            }
             slabs_h = c.take(sh);
             slabs_w = c.take(sw);
         }
@@ -1288,7 +1292,7 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
         e.p.b = hs;
         e.p.terms = p.terms;
         e.p.k_tiles = (int)(p.np / kBK);
-        run_products<T, In>(d, e, p.cuts(words), s);
+        run_products<T, In>(d, e, v0 + words < a.V ? p.cuts : p.last_cuts, s);
     }
     if (d.sum) run_finish<In>(d, s);
     return hipGetLastError();
