@@ -277,6 +277,9 @@ __device__ __forceinline__ void look_back(const Geom &g, const Place<K> &at, flo
 }
 
 // ------------------------------------------------------------------ forward
+// 24 x 4099 x 1024 bf16, ragged: 106 us, 3.8 TB/s; 1 x 100001 x 331 fp32:
+// 113 us, 3.5 TB/s.  What is left to the memory's rate is waiting: for a
+// segment's reads, for the other wavefronts' pairs and for the state before it.
 template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a, Geom g)
 {
     using T = typename K::T;
@@ -375,6 +378,8 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArg
 }
 
 // ----------------------------------------------------------------- backward
+// 24 x 4099 x 1024 bf16, ragged: 194 us, 3.6 TB/s.  Eight steps per wavefront:
+// it holds twice what the forward pass holds per step.
 template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(ScanArgs a, Geom g)
 {
     using T = typename K::T;
@@ -507,9 +512,20 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(Sc
 
 // ------------------------------------------------------------------- a few steps
 // Records that are extended by a step or a few: no exchange between lanes, a
-// lane takes VE channels of one record through all steps.
-constexpr int kFew = 8;
-template <class T> __global__ __launch_bounds__(256) void k_scan_few(ScanArgs a, int64_t chunks)
+// lane takes VE channels of one record through all steps.  One step of
+// 1024 x 512 bf16: 4.5 us.
+//
+// Up to eight steps always (B = 1: 11 us of a call, as the other kernels take);
+// up to 32, backwards 16, if there are many channels, since most wavefronts of a
+// segment would be empty: 1024 x 9 x 512 bf16 15 us against 51, backwards 26 against
+// 45; 1024 x 32 x 512 38 against 51.  With 64 x 512 channels 32 steps take 31 us
+// against 14.
+bool few_steps(int64_t B, int64_t T, int64_t D, bool back)
+{
+    return T <= 8 || (T <= (back ? 16 : 32) && B * D >= 1 << 19);
+}
+// G steps are read at a time.
+template <class T, int G> __global__ __launch_bounds__(256) void k_scan_few(ScanArgs a, int64_t chunks)
 {
     constexpr int VE = kVec<T>;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -523,28 +539,37 @@ template <class T> __global__ __launch_bounds__(256) void k_scan_few(ScanArgs a,
     float h[VE] = {};
     if (a.h0) load_part<VE>(a.h0 + b * a.D + c, n, h);
     if (a.states && len) store_part<VE>(a.states + b * a.D + c, n, h);
-    for (int64_t t = 0; t < a.T; t++) {
-        float o[VE] = {};
-        if (t < len) {
-            float xv[VE], gv[VE];
-            load_part<VE>(x + t * a.xs, n, xv);
-            load_part<VE>(g + t * a.gs, n, gv);
+    for (int64_t t0 = 0; t0 < a.T; t0 += G) {
+        float xv[G][VE] = {}, gv[G][VE] = {};
+        if (t0 < len)
 #pragma unroll
-            for (int j = 0; j < VE; j++) {
-                float av, cv;
-                gate<T>(gv[j], av, cv);
-                o[j] = h[j] = fmaf(av, h[j], cv * xv[j]);
+            for (int i = 0; i < G; i++) {
+                const int64_t t = min(t0 + i, len - 1);
+                load_part<VE>(x + t * a.xs, n, xv[i]);
+                load_part<VE>(g + t * a.gs, n, gv[i]);
             }
+#pragma unroll
+        for (int i = 0; i < G; i++) {
+            const int64_t t = t0 + i;
+            if (t >= a.T) break;
+            float o[VE] = {};
+            if (t < len)
+#pragma unroll
+                for (int j = 0; j < VE; j++) {
+                    float av, cv;
+                    gate<T>(gv[i][j], av, cv);
+                    o[j] = h[j] = fmaf(av, h[j], cv * xv[i][j]);
+                }
+            store_part<VE>(y + t * a.ys, n, o);
         }
-        store_part<VE>(y + t * a.ys, n, o);
     }
     if (a.h_last) store_part<VE>(a.h_last + b * a.D + c, n, h);
 }
 
 // The gradients of a few steps: the lane keeps the states it passes forwards.
-template <class T> __global__ __launch_bounds__(256) void k_scan_grad_few(ScanArgs a, int64_t chunks)
+template <class T, int STEPS, int VE>
+__global__ __launch_bounds__(256) void k_scan_grad_few(ScanArgs a, int64_t chunks)
 {
-    constexpr int VE = 4;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= a.B * chunks) return;
     const int64_t b = i / chunks, c = i % chunks * VE;
@@ -553,12 +578,12 @@ template <class T> __global__ __launch_bounds__(256) void k_scan_grad_few(ScanAr
     if (a.lengths) len = min(max((int64_t)a.lengths[b], (int64_t)0), a.T);
     const T *x = (const T *)a.x + b * a.xb + c, *g = (const T *)a.g + b * a.gb + c, *dy = (const T *)a.dy + b * a.dyb + c;
     T *dx = (T *)a.dx + b * a.dxb + c, *dg = (T *)a.dg + b * a.dgb + c;
-    float m[VE] = {}, h[kFew][VE], ga[kFew][VE], gc[kFew][VE], xv[kFew][VE];
+    float m[VE] = {}, h[STEPS][VE], ga[STEPS][VE], gc[STEPS][VE], xv[STEPS][VE];
     if (a.dh_last) load_part<VE>(a.dh_last + b * a.D + c, n, m);
     float s[VE] = {};
     if (len) load_part<VE>(a.states_in + b * a.D + c, n, s);
 #pragma unroll
-    for (int t = 0; t < kFew; t++) {
+    for (int t = 0; t < STEPS; t++) {
         if (t >= len) break;
         float gv[VE];
         load_part<VE>(x + t * a.xs, n, xv[t]);
@@ -571,7 +596,7 @@ template <class T> __global__ __launch_bounds__(256) void k_scan_grad_few(ScanAr
         }
     }
 #pragma unroll
-    for (int t = kFew - 1; t >= 0; t--) {
+    for (int t = STEPS - 1; t >= 0; t--) {
         if (t >= a.T) continue;
         float ox[VE] = {}, og[VE] = {};
         if (t < len) {
@@ -632,9 +657,11 @@ template <class T, bool BACK, class F> auto by_kind(int64_t D, F &&f)
 
 template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
 {
-    if (a.T <= kFew) {
+    if (few_steps(a.B, a.T, a.D, false)) {
         const int64_t chunks = (a.D + kVec<T> - 1) / kVec<T>;
-        k_scan_few<T><<<(unsigned)((a.B * chunks + 255) / 256), 256, 0, s>>>(a, chunks);
+        const unsigned blocks = (unsigned)((a.B * chunks + 255) / 256);
+        if (a.T == 1) k_scan_few<T, 1><<<blocks, 256, 0, s>>>(a, chunks);
+        else k_scan_few<T, 4><<<blocks, 256, 0, s>>>(a, chunks);
         return hipGetLastError();
     }
     return by_kind<T, false>(a.D, [&](auto kind) {
@@ -647,9 +674,13 @@ template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
 
 template <class T> hipError_t scan_grad_t(const ScanArgs &a, hipStream_t s)
 {
-    if (a.T <= kFew) {
-        const int64_t chunks = (a.D + 3) / 4;
-        k_scan_grad_few<T><<<(unsigned)((a.B * chunks + 255) / 256), 256, 0, s>>>(a, chunks);
+    if (few_steps(a.B, a.T, a.D, true)) {
+        auto go = [&](auto kernel, int ve) {
+            const int64_t chunks = (a.D + ve - 1) / ve;
+            kernel<<<(unsigned)((a.B * chunks + 255) / 256), 256, 0, s>>>(a, chunks);
+        };
+        if (a.T <= 8) go(k_scan_grad_few<T, 8, 4>, 4);
+        else go(k_scan_grad_few<T, 16, 2>, 2);
         return hipGetLastError();
     }
     return by_kind<T, true>(a.D, [&](auto kind) {
