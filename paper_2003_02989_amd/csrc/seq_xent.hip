@@ -272,6 +272,8 @@ __device__ __forceinline__ float exp_less(float z, float r2) { return __builtin_
 // ------------------------------------------------------------ the logits
 // A = weight (rows: words), B = hidden (rows: tokens): a lane's registers hold
 // words of one token, so that sums over words stay within a lane until the end.
+// 8192 x 65537 x 1024 bf16: 1130 us, 970 TFLOP/s; with p stored, in two
+// pieces, 610 us each.
 struct LogitArgs {
     ProductArgs p;
     const float *word_scale, *token_scale;  // of fp32 operands
@@ -602,7 +604,8 @@ __device__ __forceinline__ void product_tile(const StoreArgs &a, const Stages<T>
 }
 
 // dhidden's product in the first h_blocks workgroups and dweight's, whose tiles
-// fill what the former's last round leaves free, in the others.
+// fill what the former's last round leaves free, in the others.  8192 x 65537 x 1024
+// bf16, in two pieces: 1040 us each, 1060 TFLOP/s, the matrix units busy half of the time.
 template <class T, class S, class Out>
 __global__ __launch_bounds__(S::threads) void k_products(StoreArgs h, StoreArgs w, int h_blocks)
 {
@@ -835,9 +838,14 @@ __global__ __launch_bounds__(256) void k_lse(LseArgs l, int l_blocks, PackArgs h
 }
 
 // ------------------------------------------------------- a few tokens
-// With up to kFewTokens tokens the weights are what there is to read: wavefronts
+// With few tokens the weights are what there is to read: wavefronts
 // stream kFewRows x 16 words each from memory into 16 x 16 matrix instructions,
-// no LDS, no packing; the few hidden rows come from the caches.
+// no LDS, no packing; the few hidden rows come from the caches.  Bound by reading
+// the weights: 4 x 65537 x 512 bf16 15 to 20 us, 3.3 to 4.5 TB/s (67 MB, partly from the
+// last-level cache).  Up to 16 tokens of rows that the tiles can read where they
+// are (23 us for 16, 41 us for 64; tiles 27 us for 65), else up to kFewTokens, since
+// the tiles need the weights laid out first (fp32 of that size: 73 us for 64 tokens,
+// tiles 111 us for 65).
 constexpr int kFewTokens = 64, kFewRows = 2, kFewWaves = 4;
 constexpr int kFewWords = 16 * kFewRows * kFewWaves;  // of a workgroup
 
@@ -1096,7 +1104,7 @@ struct XentPlan {
     }
 
     XentPlan(int32_t type, int64_t N_, int64_t V_, int64_t D_, bool grad)
-        : two(type == TQ_F32), few(!grad && N_ <= kFewTokens), terms(two ? 3 : 1), N(N_), V(V_), D(D_)
+        : two(type == TQ_F32), few(!grad && N_ <= (two || D_ % kBK ? kFewTokens : 16)), terms(two ? 3 : 1), N(N_), V(V_), D(D_)
     {
         const size_t elem = 2 * (two ? 2 : 1);
         kp = std::max<int64_t>(up_to(D, kBK), kBK);

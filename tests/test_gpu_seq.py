@@ -188,6 +188,12 @@ def test_gated_scan_without_optional_arguments():
 
 
 @pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("T", [9, 16, 31])
+def test_gated_scan_few_steps_of_many_channels(ty, T):
+    test_gated_scan_and_gradients(ty, True, 1100, T, 480)
+
+
+@pytest.mark.parametrize("ty", TYPES)
 def test_gated_scan_step_by_step_in_place(ty):
     """Records extended step by step reach the states of one scan."""
     dtype, u, tiny = TYPES[ty]
@@ -369,6 +375,12 @@ def test_softmax_xent_and_gradients(ty, N, V, D):
 def test_softmax_xent_many_tiles(ty, N, V, D):
     """More tiles than compute units, and last rounds cut in two, in four and not at all."""
     test_softmax_xent_and_gradients(ty, N, V, D)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("N", [16, 17, 33])
+def test_softmax_xent_few_tokens_of_whole_pieces(ty, N):
+    test_softmax_xent_and_gradients(ty, N, 300, 128)
 
 
 @pytest.mark.parametrize("ty", TYPES)
