@@ -569,10 +569,11 @@ template <class T> hipError_t embed_grad_t(const EmbedGradArgs &a, hipStream_t s
         u.chunk_blocks = (int)((p.chunks + per - 1) / per);
         k_embed_sums<T, decltype(w)::value, L><<<(unsigned)(u.chunk_blocks + zeros), kThreads, 0, s>>>(u);
     });
-    // a long run has more than kOver places
-    const int64_t most = a.N / kOver;
-    k_embed_join<T><<<dim3((unsigned)std::min<int64_t>(most, 128), (unsigned)((a.D + 63) / 64)), kJoinWaves * 64, 0,
-                     s>>>(u);
+    // a long run has more than kOver places: with fewer ids there is none to join
+    const int64_t most = a.N / (kOver + 1);
+    if (most)
+        k_embed_join<T><<<dim3((unsigned)std::min<int64_t>(most, 128), (unsigned)((a.D + 63) / 64)), kJoinWaves * 64, 0,
+                         s>>>(u);
     return hipGetLastError();
 }
 

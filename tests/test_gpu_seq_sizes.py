@@ -1,0 +1,17 @@
+"""Sequence operators on the GPU at sizes where another variant takes over,
+against the oracle's 64-bit forms, with the tolerances of test_gpu_seq."""
+import pytest
+
+import test_gpu_seq as base
+from test_gpu_seq import TYPES
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("kind", ["uniform", "one"])
+@pytest.mark.parametrize("N,V,D", [(48, 17, 4096), (63, 3, 2049), (57, 5, 2100), (33, 9, 4099), (16, 17, 8193),
+                                   (64, 3, 2100), (65, 3, 2100), (66, 3, 2100)])
+def test_table_gradient_of_few_wide_rows(ty, kind, N, V, D):
+    """Too wide for the kernel of few ids, too few ids for a long run."""
+    base.test_embed_grad(ty, N, V, D, kind)
