@@ -61,6 +61,8 @@ int hipGetLastError(void)
     error = 0;
     return e;
 }
+int kernel_count(void) { return n_kernels; }
+const char *kernel_name(int i) { return kernels[i].name; }
 int launch_count(void) { return n_launches; }
 void launch_clear(void) { n_launches = 0; }
 const char *launch_name(int i) { return launches[i].name; }
@@ -76,6 +78,7 @@ import ctypes, json, sys
 rec = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
 rec.launch_name.restype = ctypes.c_char_p
 rec.launch_size.restype = ctypes.c_uint32
+rec.kernel_name.restype = ctypes.c_char_p
 lib = ctypes.CDLL(sys.argv[2])
 lib.tq_last_error.restype = ctypes.c_char_p
 kinds = {"p": ctypes.c_void_p, "i": ctypes.c_int32, "n": ctypes.c_int64, "s": ctypes.c_size_t, "f": ctypes.c_float}
@@ -88,7 +91,7 @@ for name, spec, args in json.load(sys.stdin):
     out.append({"rc": rc, "error": lib.tq_last_error().decode(), "need": need.value,
                 "kernels": [[rec.launch_name(i).decode()] + [rec.launch_size(i, k) for k in range(6)]
                             for i in range(rec.launch_count())]})
-json.dump(out, sys.stdout)
+json.dump({"kernels": [rec.kernel_name(i).decode() for i in range(rec.kernel_count())], "calls": out}, sys.stdout)
 """
 
 P = 1 << 20  # stands for a device pointer, 256-byte aligned
@@ -114,7 +117,8 @@ ALL = (1 << 63) - 1  # a workspace of any size
 
 def recorded(calls, tmp_path):
     """[(name, *arguments)] run in a child process: for each {"rc", "error",
-    "need", "kernels"}, the last [[name, grid x, y, z, workgroup x, y, z]]."""
+    "need", "kernels"}, the last [[name, grid x, y, z, workgroup x, y, z]]; and
+    the names of all kernels there are."""
     so = str(tmp_path / "recorder.so")
     subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-w", "-x", "c", "-", "-o", so], input=_RECORDER, text=True, check=True)
     asked = [(c[0], SPECS[c[0]], list(c[1:]) + [None] * (len(SPECS[c[0]]) - len(c) + 1)) for c in calls]
@@ -122,7 +126,8 @@ def recorded(calls, tmp_path):
     r = subprocess.run([sys.executable, "-c", _CHILD, so, lib], input=json.dumps(asked), capture_output=True, text=True,
                        timeout=120)
     assert r.returncode == 0, f"ended with {r.returncode}: {r.stderr[-2000:]}"
-    return json.loads(r.stdout)
+    got = json.loads(r.stdout)
+    return got["calls"], got["kernels"]
 
 
 # the calls of the operators on dense arrays; types 0: fp32, 1: bf16, 2: f16

@@ -15,3 +15,10 @@ pytestmark = pytest.mark.gpu
 def test_table_gradient_of_few_wide_rows(ty, kind, N, V, D):
     """Too wide for the kernel of few ids, too few ids for a long run."""
     base.test_embed_grad(ty, N, V, D, kind)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("N,D,pad", [(3, 4097, 0), (5, 5001, 2), (2, 8191, 1), (7, 8192, 0), (3, 8193, 0), (4, 12001, 3),
+                                     (2, 16383, 1), (5, 16384, 0), (4100, 8200, 0)])
+def test_layer_norm_of_rows_that_a_whole_workgroup_holds(ty, N, D, pad):
+    base.test_layer_norm_and_gradients(ty, True, N, D, pad)

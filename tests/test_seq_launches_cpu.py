@@ -10,7 +10,7 @@ ROOT = la.ROOT
 
 
 def run(calls, tmp_path):
-    got = la.recorded(calls, tmp_path)
+    got, _ = la.recorded(calls, tmp_path)
     for c, g in zip(calls, got):
         assert g["rc"] == 0, (c[0], c[1:8], g["error"], g["kernels"][-3:])
     return got
@@ -29,3 +29,20 @@ def test_table_gradient_of_any_number_of_ids(ty, tmp_path):
     for c, g in zip(calls, run(calls, tmp_path)):
         joins = [n for n in names(g) if "k_embed_join" in n]
         assert not joins or c[7] > 64, c[:8]
+
+
+def test_every_variant_of_layer_norm_is_reached(tmp_path):
+    """Rows of every width go to the variant that their width is meant for, and
+    no variant is left that no width reaches."""
+    widths = sorted({max(1, w + d) for w in (1, 4, 8, 32, 64, 128, 256, 512, 1024, 2048, 4096, 8192, 16384) for d in (-1, 0, 1)})
+    widths += [768, 769, 1536, 1537, 100003]
+    calls = [f(ty, 5, D) for f in (la.norm, la.norm_grad) for ty in range(3) for D in widths]
+    got, kernels = la.recorded(calls, tmp_path)
+    assert all(g["rc"] == 0 for g in got)
+    reached = {n for g in got for n in names(g)}
+    assert {k for k in kernels if "k_norm" in k} == reached
+    for c, g in zip(calls, got):
+        if c[0] == "tq_layer_norm":
+            one = 4096 if c[3] == 0 else 8192  # of 16 pieces to a lane of 256, in registers
+            want = "Li256ELi4E" if one // 2 < c[5] <= one else "Li1024ELi2E" if one < c[5] <= 2 * one else "k_norm_wide" if c[5] > 2 * one else ""
+            assert want in names(g)[0], (c[3], c[5], names(g))
