@@ -323,7 +323,7 @@ tq_status tq_softmax_xent_grad_workspace(int32_t type, int64_t N, int64_t V, int
 {
     return guarded([&] {
         check_xent("softmax_xent_grad_workspace", type, N, V, D);
-        give(bytes, xent_workspace(type, N, V, D, true));
+        give(bytes, V ? xent_workspace(type, N, V, D, true) : 0);
     });
 }
 

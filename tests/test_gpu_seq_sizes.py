@@ -1,8 +1,10 @@
 """Sequence operators on the GPU at sizes where another variant takes over,
 against the oracle's 64-bit forms, with the tolerances of test_gpu_seq."""
 import pytest
+import torch
 
 import test_gpu_seq as base
+from paper_2003_02989_amd import seq
 from test_gpu_seq import TYPES
 
 pytestmark = pytest.mark.gpu
@@ -22,3 +24,14 @@ def test_table_gradient_of_few_wide_rows(ty, kind, N, V, D):
                                      (2, 16383, 1), (5, 16384, 0), (4100, 8200, 0)])
 def test_layer_norm_of_rows_that_a_whole_workgroup_holds(ty, N, D, pad):
     base.test_layer_norm_and_gradients(ty, True, N, D, pad)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+def test_cross_entropy_of_nothing(ty):
+    """No tokens and no vocabulary: empty results."""
+    dtype = TYPES[ty][0]
+    e = torch.zeros((0, 5), dtype=dtype, device="cuda")
+    t, up = torch.zeros(0, dtype=torch.int64, device="cuda"), torch.zeros(0, device="cuda")
+    dh, dW, loss, lse = seq.softmax_xent_grad(e, e, t, up)
+    assert dh.shape == dW.shape == (0, 5) and loss.shape == lse.shape == (0,)
+    assert seq.softmax_xent(e, e, t)[0].shape == (0,)

@@ -46,3 +46,21 @@ def test_every_variant_of_layer_norm_is_reached(tmp_path):
             one = 4096 if c[3] == 0 else 8192  # of 16 pieces to a lane of 256, in registers
             want = "Li256ELi4E" if one // 2 < c[5] <= one else "Li1024ELi2E" if one < c[5] <= 2 * one else "k_norm_wide" if c[5] > 2 * one else ""
             assert want in names(g)[0], (c[3], c[5], names(g))
+
+
+def test_sizes_of_nothing(tmp_path):
+    """Every size that may be zero, alone and together: the workspace is asked
+    for and the call made; none ends the process, none has an empty grid."""
+    calls = []
+    for ty in range(3):
+        for N in (0, 1, 70):
+            for V in (0, 1, 300):
+                for D in (0, 1, 64):
+                    if not (N and not V):
+                        calls += [("tq_softmax_xent_workspace", ty, N, V, D), la.xent(ty, N, V, D),
+                                  ("tq_softmax_xent_grad_workspace", ty, N, V, D), la.xent_grad(ty, N, V, D)]
+                    calls += [("tq_embed_grad_workspace", V, D, N), la.embed(ty, N, V, D), la.embed_grad(ty, N, V, D)]
+                calls += [("tq_layer_norm_grad_workspace", N, V), la.norm(ty, N, V), la.norm_grad(ty, N, V)]
+                for B in (0, 2):
+                    calls += [("tq_gated_scan_workspace", B, N, V), la.scan(ty, B, N, V), la.scan_grad(ty, B, N, V)]
+    run(calls, tmp_path)
