@@ -28,6 +28,7 @@
 
 #include "seq.h"
 #include "seq_device.h"
+#include "seq_slots.h"
 
 namespace tq {
 namespace {
@@ -69,13 +70,9 @@ template <class T> __device__ __forceinline__ void gate(float g, float &a, float
 }
 
 // ------------------------------------------------------------ published pairs
-// A pair (A, B), A >= 0, or a state (-0, h): one 64-bit access, of which a reader
-// sees all or nothing.  Agent scope reaches the other XCDs; nothing else is
-// handed over, so no ordering is needed.
-using Slot = unsigned long long;
-constexpr Slot kEmpty = ~(Slot)0;
-constexpr uint32_t kState = 0x80000000u;
-
+// One 64-bit access each (seq_slots.h), of which a reader sees all or nothing.
+// Agent scope reaches the other XCDs; nothing else is handed over, so no ordering
+// is needed.
 struct Geom {
     uint32_t rows, slabs;  // rows: records x slabs
     int segs;
@@ -83,29 +80,24 @@ struct Geom {
     unsigned *ticket;
 };
 
-__device__ __forceinline__ void publish(Slot *p, uint32_t hi, float b)
+__device__ __forceinline__ void publish(Slot *p, Slot v)
 {
-    __hip_atomic_store(p, (Slot)hi << 32 | __float_as_uint(b), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ void publish_pair(Slot *p, float a, float b)
-{
-    publish(p, a == a ? __float_as_uint(a) : 0x7fc00000u, b);  // a NaN, but not kEmpty
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ Slot look(const Slot *p)
 {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ bool is_state(float a) { return __float_as_uint(a) == kState; }
 // What is at p, which was `v` when last looked at, once it is published, or
 // (`state`) once it is a state.  The count only keeps a broken launch from
-// running for good: it is a matter of seconds.
-__device__ __forceinline__ float2 await(const Slot *p, Slot v, bool state)
+// running for good: it is a matter of seconds, and its outputs are NaN.
+__device__ __forceinline__ SlotPair await(const Slot *p, Slot v, bool state)
 {
-    for (int k = 0; (v == kEmpty || (state && (uint32_t)(v >> 32) != kState)) && k < 1 << 22; k++) {
+    for (int k = 0; !slot_ready(v, state) && k < 1 << 22; k++) {
         __builtin_amdgcn_s_sleep(1);
         v = look(p);
     }
-    return make_float2(__uint_as_float((uint32_t)(v >> 32)), __uint_as_float((uint32_t)v));
+    return slot_value(v, state);
 }
 
 __global__ __launch_bounds__(256) void k_scan_clear(Slot *slots, int64_t n, unsigned *ticket)
@@ -232,7 +224,7 @@ __device__ __forceinline__ void put(typename K::T *p, int64_t step, int64_t T, c
 // All wavefronts get the same result.
 constexpr int kWindows = 4;
 template <class K>
-__device__ __forceinline__ void look_back(const Geom &g, const Place<K> &at, float2 (*win)[kWaves][K::slab],
+__device__ __forceinline__ void look_back(const Geom &g, const Place<K> &at, SlotPair (*win)[kWaves][K::slab],
                                           const float (&first)[K::CV], float (&h)[K::CV])
 {
     constexpr int CV = K::CV;
@@ -241,9 +233,9 @@ __device__ __forceinline__ void look_back(const Geom &g, const Place<K> &at, flo
     bool found[CV] = {};
     for (int k = 0; k < kWindows && seen < before; k++) {
         const int back = k * kWaves + at.wave;
-        float2 q[CV];
+        SlotPair q[CV];
 #pragma unroll
-        for (int j = 0; j < CV; j++) q[j] = make_float2(1.f, 0.f);
+        for (int j = 0; j < CV; j++) q[j] = SlotPair{slot_bits(1.f), 0.f};
         if (back < before) {
             const Slot *p = g.slots + ((int64_t)(at.seg - 1 - back) * g.rows + at.row) * K::slab + at.lane * CV;
             Slot v[CV];
@@ -260,7 +252,7 @@ __device__ __forceinline__ void look_back(const Geom &g, const Place<K> &at, flo
 #pragma unroll
         for (int j = 0; j < CV; j++) {
 #pragma unroll
-            for (int w = 0; w < kWaves; w++) found[j] = found[j] || is_state(win[k][w][at.lane * CV + j].x);
+            for (int w = 0; w < kWaves; w++) found[j] = found[j] || win[k][w][at.lane * CV + j].a == kState;
             all = all && found[j];
         }
         if (__all(all)) break;  // the same in every wavefront
@@ -270,10 +262,7 @@ __device__ __forceinline__ void look_back(const Geom &g, const Place<K> &at, flo
     for (int j = 0; j < CV; j++) h[j] = first[j];
     for (int back = seen - 1; back >= 0; back--)
 #pragma unroll
-        for (int j = 0; j < CV; j++) {
-            const float2 q = win[back / kWaves][back % kWaves][at.lane * CV + j];
-            h[j] = is_state(q.x) ? q.y : fmaf(q.x, h[j], q.y);
-        }
+        for (int j = 0; j < CV; j++) h[j] = slot_step(win[back / kWaves][back % kWaves][at.lane * CV + j], h[j]);
 }
 
 // ------------------------------------------------------------------ forward
@@ -284,7 +273,8 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArg
 {
     using T = typename K::T;
     constexpr int CV = K::CV, L = K::steps;
-    __shared__ float2 agg[kWaves][K::slab], win[kWindows][kWaves][K::slab];
+    __shared__ float2 agg[kWaves][K::slab];
+    __shared__ SlotPair win[kWindows][kWaves][K::slab];
     const Place<K> at(a, g, take_item(g), false);
     T *y = (T *)a.y + at.b * a.yb + at.t0 * a.ys;
     float ga[L][CV], gb[L][CV], A[CV], B[CV];
@@ -343,14 +333,14 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArg
             }
 #pragma unroll
         for (int j = 0; j < CV; j++) {
-            if (at.seg > at.seg0) publish_pair(slot + j, wholeA[j], wholeB[j]);
+            if (at.seg > at.seg0) publish(slot + j, pair_slot(wholeA[j], wholeB[j]));
         }
     }
     float h[CV];
     look_back<K>(g, at, win, first, h);
     if (shared)
 #pragma unroll
-        for (int j = 0; j < CV; j++) publish(slot + j, kState, fmaf(wholeA[j], h[j], wholeB[j]));
+        for (int j = 0; j < CV; j++) publish(slot + j, state_slot(fmaf(wholeA[j], h[j], wholeB[j])));
     for (int w = 0; w < at.wave; w++)
 #pragma unroll
         for (int j = 0; j < CV; j++) {
@@ -384,7 +374,8 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(Sc
 {
     using T = typename K::T;
     constexpr int CV = K::CV, L = K::steps, kBefore = kPiece / L;  // wavefronts of a piece
-    __shared__ float2 agg[kWaves][K::slab], win[kWindows][kWaves][K::slab];
+    __shared__ float2 agg[kWaves][K::slab];
+    __shared__ SlotPair win[kWindows][kWaves][K::slab];
     __shared__ float rev[kWaves][K::slab];
     const Place<K> at(a, g, take_item(g), true);
     T *dx = (T *)a.dx + at.b * a.dxb + at.t0 * a.dxs, *dg = (T *)a.dg + at.b * a.dgb + at.t0 * a.dgs;
@@ -461,7 +452,7 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(Sc
             }
 #pragma unroll
         for (int j = 0; j < CV; j++) {
-            if (shared && at.seg > at.seg0) publish_pair(slot + j, wholeA[j], wholeB[j]);
+            if (shared && at.seg > at.seg0) publish(slot + j, pair_slot(wholeA[j], wholeB[j]));
         }
     }
     float m[CV];
@@ -470,7 +461,7 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(Sc
 #pragma unroll
         for (int j = 0; j < CV; j++) {
             const float out = fmaf(wholeA[j], m[j], wholeB[j]);
-            if (shared) publish(slot + j, kState, out);
+            if (shared) publish(slot + j, state_slot(out));
             if (a.dh0 && at.seg == g.segs - 1 && j < at.n) a.dh0[at.b * a.D + at.c0 + j] = out;
         }
     for (int w = kWaves - 1; w > at.wave; w--)
