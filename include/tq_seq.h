@@ -118,7 +118,9 @@ tq_status tq_layer_norm_grad(const void *x, int64_t ld_x, int32_t type, int64_t 
  * loss[i] = 0 where targets[i] >= V.  loss and lse are float [N].  Products of
  * 16-bit inputs are exact and summed in fp32; fp32 inputs are split into
  * pairs of 16-bit numbers that hold 22 of their 24 bits, products summed in
- * fp32.  A row of infinities or NaN gives NaN for that row. */
+ * fp32.  A row of infinities or NaN gives NaN for that row.  TQ_E_UNSUPPORTED
+ * for D > 2^20, and where ceil(N / 128) ceil(V / 128), or either times
+ * ceil(D / 128), reaches 2^27. */
 tq_status tq_softmax_xent_workspace(int32_t type, int64_t N, int64_t V, int64_t D, size_t *bytes);
 tq_status tq_softmax_xent(const void *hidden, int64_t ld_hidden, int32_t type, int64_t N, int64_t V, int64_t D,
                           const void *weight, int64_t ld_weight, const uint64_t *targets, float *loss, float *lse,

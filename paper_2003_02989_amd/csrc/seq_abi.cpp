@@ -1,5 +1,6 @@
 // seq_abi.cpp -- the extern "C" entry points of tq_seq.h: every argument is
 // checked here, on the host, before anything is enqueued.
+#include <algorithm>
 #include <climits>
 
 #include "abi_util.h"
@@ -307,8 +308,10 @@ static void check_xent(const char *call, int type, int64_t N, int64_t V, int64_t
     check_size(call, "D", D);
     if (N && V == 0) fail(TQ_E_INVALID, text(call, "a vocabulary needs one row at least"));
     if (D > kMaxWidth) fail(TQ_E_UNSUPPORTED, text(call, "D must be at most 2^20"));
-    if (((N + 127) / 128) * ((V + 127) / 128) > kMaxIndex / 16)
-        fail(TQ_E_UNSUPPORTED, text(call, "too many tokens and words"));
+    // tiles of 128 x 128 of the logits and of the gradients
+    const auto tiles = [](int64_t n) { return (n + 127) / 128; };
+    if (tiles(N) * tiles(V) > kMaxIndex / 16 || std::max(tiles(N), tiles(V)) * tiles(D) > kMaxIndex / 16)
+        fail(TQ_E_UNSUPPORTED, text(call, "ceil(N / 128) * ceil(V / 128), and either times ceil(D / 128), must be below 2^27"));
 }
 
 tq_status tq_softmax_xent_workspace(int32_t type, int64_t N, int64_t V, int64_t D, size_t *bytes)

@@ -6,6 +6,18 @@
 
 namespace tq {
 
+// A launch has fewer than 2^32 threads along x: from kGridX workgroups on (of at
+// most 1024 threads) they go on along y.  The last row's may be past the end: every
+// kernel launched so returns in them before it reads or writes anything.
+constexpr unsigned kGridX = 1 << 21;
+inline dim3 grid_of(int64_t blocks)
+{
+    if (blocks <= kGridX) return dim3((unsigned)blocks);
+    return dim3(kGridX, (unsigned)((blocks + kGridX - 1) / kGridX));
+}
+// The number of a workgroup of such a launch, below 2^32.
+__device__ __forceinline__ uint32_t block_of() { return blockIdx.y * kGridX + blockIdx.x; }
+
 // Elements per 16-byte access.
 template <class T> constexpr int kVec = 16 / (int)sizeof(T);
 

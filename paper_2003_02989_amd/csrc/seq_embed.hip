@@ -37,7 +37,7 @@ constexpr int kRows = 4;
 template <class T, int W, int L> __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a)
 {
     const int lane = threadIdx.x % L;
-    const int64_t group = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+    const int64_t group = (int64_t)block_of() * (kThreads / L) + threadIdx.x / L;
     const int64_t i0 = group * kRows;
     if (i0 >= a.N) return;
     uint64_t t[kRows];
@@ -87,7 +87,7 @@ template <class T> hipError_t embed_t(const EmbedArgs &a, hipStream_t s)
     by_width<T>(a.D, [&](auto w, auto l) {
         constexpr int L = decltype(l)::value;
         const int64_t groups = (a.N + kRows - 1) / kRows, per = kThreads / L;
-        k_embed<T, decltype(w)::value, L><<<(unsigned)((groups + per - 1) / per), kThreads, 0, s>>>(a);
+        k_embed<T, decltype(w)::value, L><<<grid_of((groups + per - 1) / per), kThreads, 0, s>>>(a);
     });
     return hipGetLastError();
 }

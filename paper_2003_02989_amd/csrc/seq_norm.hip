@@ -134,7 +134,8 @@ template <class T> __global__ __launch_bounds__(kWide) void k_norm_wide(NormArgs
     constexpr int VE = kVec<T>;
     __shared__ float red[2][16];
     int turn = 0;
-    const int64_t row = blockIdx.x;
+    const int64_t row = block_of();
+    if (row >= a.N) return;
     const T *x = (const T *)a.x + row * a.ld_x;
     float s = 0.f, q = 0.f;
     for (int64_t at = (int64_t)threadIdx.x * VE; at < a.D; at += kWide * VE) {
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_norm_join(NormArgs a, const
 {
     __shared__ float red[kJoinWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    const int64_t c = (int64_t)block_of() * 64 + lane;
     float s = 0.f;
     if (c < 2 * a.D)
 #pragma unroll 8
@@ -382,7 +383,7 @@ template <class T> hipError_t norm_t(const NormArgs &a, hipStream_t s)
 {
     return by_width<T, false>(a.D, [&](auto l, auto c, auto w) {
         constexpr int L = decltype(l)::value, C = decltype(c)::value, W = decltype(w)::value;
-        if constexpr (L == 0) k_norm_wide<T><<<(unsigned)a.N, kWide, 0, s>>>(a);
+        if constexpr (L == 0) k_norm_wide<T><<<grid_of(a.N), kWide, 0, s>>>(a);
         else {
             constexpr int R = kThreadsOf<L> / L;
             k_norm<T, L, C, W><<<(unsigned)std::min((a.N + R - 1) / R, kBlocks), kThreadsOf<L>, 0, s>>>(a);
@@ -405,7 +406,7 @@ template <class T> hipError_t norm_grad_t(const NormArgs &a, hipStream_t s)
             blocks = std::min((a.N + R - 1) / R, L > 256 ? kGradBlocks / 4 : L > 64 ? kGradBlocks / 2 : kGradBlocks);
             if (blocks) k_norm_grad<T, L, C, W><<<(unsigned)blocks, kThreadsOf<L>, 0, s>>>(a, part);
         }
-        k_norm_join<T><<<(unsigned)((2 * a.D + 63) / 64), kJoinWaves * 64, 0, s>>>(a, part, (int)blocks);
+        k_norm_join<T><<<grid_of((2 * a.D + 63) / 64), kJoinWaves * 64, 0, s>>>(a, part, (int)blocks);
         return hipGetLastError();
     });
 }

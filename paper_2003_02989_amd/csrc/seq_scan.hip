@@ -74,7 +74,7 @@ template <class T> __device__ __forceinline__ void gate(float g, float &a, float
 // Agent scope reaches the other XCDs; nothing else is handed over, so no ordering
 // is needed.
 struct Geom {
-    uint32_t rows, slabs;  // rows: records x slabs
+    uint32_t rows, slabs, items;  // rows: records x slabs; items: rows x segs
     int segs;
     Slot *slots;   // [segs][rows][kSlab]
     unsigned *ticket;
@@ -102,7 +102,7 @@ __device__ __forceinline__ SlotPair await(const Slot *p, Slot v, bool state)
 
 __global__ __launch_bounds__(256) void k_scan_clear(Slot *slots, int64_t n, unsigned *ticket)
 {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2;
+    const int64_t i = ((int64_t)block_of() * 256 + threadIdx.x) * 2;
     if (i == 0) *ticket = 0;
     if (i < n) *(ulonglong2 *)(slots + i) = make_ulonglong2(kEmpty, kEmpty);  // n is even
 }
@@ -143,7 +143,7 @@ template <class K> struct Place {
 
 __device__ __forceinline__ uint32_t take_item(const Geom &g)
 {
-    if (g.segs == 1) return blockIdx.x;
+    if (g.segs == 1) return block_of();
     __shared__ uint32_t item;
     if (threadIdx.x == 0) item = atomicAdd(g.ticket, 1u);
     __syncthreads();
@@ -275,7 +275,9 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArg
     constexpr int CV = K::CV, L = K::steps;
     __shared__ float2 agg[kWaves][K::slab];
     __shared__ SlotPair win[kWindows][kWaves][K::slab];
-    const Place<K> at(a, g, take_item(g), false);
+    const uint32_t item = take_item(g);
+    if (item >= g.items) return;
+    const Place<K> at(a, g, item, false);
     T *y = (T *)a.y + at.b * a.yb + at.t0 * a.ys;
     float ga[L][CV], gb[L][CV], A[CV], B[CV];
     if (at.idle()) {
@@ -377,7 +379,9 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(Sc
     __shared__ float2 agg[kWaves][K::slab];
     __shared__ SlotPair win[kWindows][kWaves][K::slab];
     __shared__ float rev[kWaves][K::slab];
-    const Place<K> at(a, g, take_item(g), true);
+    const uint32_t item = take_item(g);
+    if (item >= g.items) return;
+    const Place<K> at(a, g, item, true);
     T *dx = (T *)a.dx + at.b * a.dxb + at.t0 * a.dxs, *dg = (T *)a.dg + at.b * a.dgb + at.t0 * a.dgs;
     float ga[L][CV], gc[L][CV], A[CV], Bf[CV], Br[CV];
     if (at.idle()) {
@@ -519,7 +523,7 @@ bool few_steps(int64_t B, int64_t T, int64_t D, bool back)
 template <class T, int G> __global__ __launch_bounds__(256) void k_scan_few(ScanArgs a, int64_t chunks)
 {
     constexpr int VE = kVec<T>;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t i = (int64_t)block_of() * 256 + threadIdx.x;
     if (i >= a.B * chunks) return;
     const int64_t b = i / chunks, c = i % chunks * VE;
     const int n = (int)min((int64_t)VE, a.D - c);
@@ -561,7 +565,7 @@ template <class T, int G> __global__ __launch_bounds__(256) void k_scan_few(Scan
 template <class T, int STEPS, int VE>
 __global__ __launch_bounds__(256) void k_scan_grad_few(ScanArgs a, int64_t chunks)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t i = (int64_t)block_of() * 256 + threadIdx.x;
     if (i >= a.B * chunks) return;
     const int64_t b = i / chunks, c = i % chunks * VE;
     const int n = (int)min((int64_t)VE, a.D - c);
@@ -628,12 +632,12 @@ template <class K> struct Layout {
     Geom start(void *ws, hipStream_t s) const
     {
         Geom g{};
-        g.rows = (uint32_t)rows, g.slabs = (uint32_t)slabs, g.segs = segs;
+        g.rows = (uint32_t)rows, g.slabs = (uint32_t)slabs, g.items = (uint32_t)items, g.segs = segs;
         if (segs == 1) return g;
         g.slots = (Slot *)((char *)ws + slots);
         g.ticket = (unsigned *)((char *)ws + ticket);
         const int64_t n = items * K::slab;
-        k_scan_clear<<<(unsigned)((n + 511) / 512), 256, 0, s>>>(g.slots, n, g.ticket);
+        k_scan_clear<<<grid_of((n + 511) / 512), 256, 0, s>>>(g.slots, n, g.ticket);
         return g;
     }
 };
@@ -650,7 +654,7 @@ template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
 {
     if (few_steps(a.B, a.T, a.D, false)) {
         const int64_t chunks = (a.D + kVec<T> - 1) / kVec<T>;
-        const unsigned blocks = (unsigned)((a.B * chunks + 255) / 256);
+        const dim3 blocks = grid_of((a.B * chunks + 255) / 256);
         if (a.T == 1) k_scan_few<T, 1><<<blocks, 256, 0, s>>>(a, chunks);
         else k_scan_few<T, 4><<<blocks, 256, 0, s>>>(a, chunks);
         return hipGetLastError();
@@ -658,7 +662,7 @@ template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
     return by_kind<T, false>(a.D, [&](auto kind) {
         using K = decltype(kind);
         const Layout<K> l(a.B, a.T, a.D);
-        k_scan<K><<<(unsigned)l.items, kThreads, 0, s>>>(a, l.start(a.ws, s));
+        k_scan<K><<<grid_of(l.items), kThreads, 0, s>>>(a, l.start(a.ws, s));
         return hipGetLastError();
     });
 }
@@ -668,7 +672,7 @@ template <class T> hipError_t scan_grad_t(const ScanArgs &a, hipStream_t s)
     if (few_steps(a.B, a.T, a.D, true)) {
         auto go = [&](auto kernel, int ve) {
             const int64_t chunks = (a.D + ve - 1) / ve;
-            kernel<<<(unsigned)((a.B * chunks + 255) / 256), 256, 0, s>>>(a, chunks);
+            kernel<<<grid_of((a.B * chunks + 255) / 256), 256, 0, s>>>(a, chunks);
         };
         if (a.T <= 8) go(k_scan_grad_few<T, 8, 4>, 4);
         else go(k_scan_grad_few<T, 16, 2>, 2);
@@ -677,7 +681,7 @@ template <class T> hipError_t scan_grad_t(const ScanArgs &a, hipStream_t s)
     return by_kind<T, true>(a.D, [&](auto kind) {
         using K = decltype(kind);
         const Layout<K> l(a.B, a.T, a.D);
-        k_scan_grad<K><<<(unsigned)l.items, kThreads, 0, s>>>(a, l.start(a.ws, s));
+        k_scan_grad<K><<<grid_of(l.items), kThreads, 0, s>>>(a, l.start(a.ws, s));
         return hipGetLastError();
     });
 }

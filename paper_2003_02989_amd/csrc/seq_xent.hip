@@ -76,6 +76,7 @@ struct ProductArgs {
     int m_tiles, n_tiles;
     int full;     // tiles that one workgroup computes alone; the others are
     int splits;   // cut into this many, along K or (logits) along N
+    int blocks;   // workgroups of all tiles
 };
 
 // Tile of C, wavefronts WM x WN, each with FM x FN blocks of 32 x 32.
@@ -456,7 +457,9 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
 {
     TQ_STAGES(T, S, lds);
     __shared__ float2 join[GRAD ? 1 : std::max(S::WM * S::BN, Half::WM * Half::BN)];
-    const Tile t = tile_of(a.p, blockIdx.x);
+    const int blk = (int)block_of();
+    if (blk >= a.p.blocks) return;
+    const Tile t = tile_of(a.p, blk);
     const int64_t m0 = t.m * S::BM, n0 = t.n * S::BN;
     if constexpr (std::is_same_v<S, Big>)
         if (t.split >= 0) {
@@ -610,8 +613,9 @@ template <class T, class S, class Out>
 __global__ __launch_bounds__(S::threads) void k_products(StoreArgs h, StoreArgs w, int h_blocks)
 {
     TQ_STAGES(T, S, lds);
-    if ((int)blockIdx.x < h_blocks) product_tile<T, S, false, Out>(h, lds, blockIdx.x);
-    else product_tile<T, S, true, Out>(w, lds, blockIdx.x - h_blocks);
+    const int blk = (int)block_of();
+    if (blk < h_blocks) product_tile<T, S, false, Out>(h, lds, blk);
+    else if (blk - h_blocks < w.p.blocks) product_tile<T, S, true, Out>(w, lds, blk - h_blocks);
 }
 
 // The tiles that were cut along K: their slabs, added up in order.
@@ -647,10 +651,11 @@ template <class S, class Out> __global__ __launch_bounds__(256) void k_slabs(Sto
 // out = factor(row) sum; zeros without a sum.
 template <class Out> __global__ __launch_bounds__(256) void k_finish(StoreArgs a)
 {
-    const int64_t n = (int64_t)blockIdx.y * 256 + threadIdx.x, m = blockIdx.x;
+    const int64_t n = (int64_t)blockIdx.y * 256 + threadIdx.x;
     const Factor factor(a);
     if (n >= a.N) return;
-    ((Out *)a.out)[m * a.ld_out + n] = (Out)(a.sum ? factor.of(a.sum[m * a.N + n], m) : 0.f);
+    for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x)
+        ((Out *)a.out)[m * a.ld_out + n] = (Out)(a.sum ? factor.of(a.sum[m * a.N + n], m) : 0.f);
 }
 
 // ------------------------------------------------------------ laying out
@@ -817,24 +822,27 @@ __device__ __forceinline__ void lse_rows(const LseArgs &a, int blk)
 // (their partial maxima).
 template <class In, class T, bool TWO>
 __global__ __launch_bounds__(256) void k_lay_hidden(PackArgs h, int h_blocks, const float *w, int64_t ld_w, int64_t V,
-                                                   float *w_max)
+                                                   float *w_max, int max_blocks)
 {
-    if ((int)blockIdx.x < h_blocks) pack_rows<In, T, TWO>(h, blockIdx.x);
-    else max_part(w, ld_w, V, h.D, w_max, blockIdx.x - h_blocks);
+    const int blk = (int)block_of();
+    if (blk < h_blocks) pack_rows<In, T, TWO>(h, blk);
+    else if (blk - h_blocks < max_blocks) max_part(w, ld_w, V, h.D, w_max, blk - h_blocks);
 }
 // The weights' rows laid out, and the largest upstream.
 template <class In, class T, bool TWO>
-__global__ __launch_bounds__(256) void k_lay_weight(PackArgs w, int w_blocks, UpArgs u)
+__global__ __launch_bounds__(256) void k_lay_weight(PackArgs w, int w_blocks, UpArgs u, int up_blocks)
 {
-    if ((int)blockIdx.x < w_blocks) pack_rows<In, T, TWO>(w, blockIdx.x);
-    else up_max(u, blockIdx.x - w_blocks);
+    const int blk = (int)block_of();
+    if (blk < w_blocks) pack_rows<In, T, TWO>(w, blk);
+    else if (blk - w_blocks < up_blocks) up_max(u, blk - w_blocks);
 }
 // After the logits: lse and loss, and hidden's rows laid out for dweight.
 template <class In, class T, bool TWO>
-__global__ __launch_bounds__(256) void k_lse(LseArgs l, int l_blocks, PackArgs h)
+__global__ __launch_bounds__(256) void k_lse(LseArgs l, int l_blocks, PackArgs h, int h_blocks)
 {
-    if ((int)blockIdx.x < l_blocks) lse_rows(l, blockIdx.x);
-    else pack_rows<In, T, TWO>(h, blockIdx.x - l_blocks);
+    const int blk = (int)block_of();
+    if (blk < l_blocks) lse_rows(l, blk);
+    else if (blk - l_blocks < h_blocks) pack_rows<In, T, TWO>(h, blk - l_blocks);
 }
 
 // ------------------------------------------------------- a few tokens
@@ -883,8 +891,9 @@ struct FewArgs {
     const void *hidden, *weight;
     int64_t ld_hidden, ld_weight, N, V, D;
     const uint64_t *targets;
-    float2 *part;
+    float2 *part;  // [N, tiles]
     float *z_target;
+    int tiles;
 };
 
 template <class T, int NT> __global__ __launch_bounds__(64 * kFewWaves) void k_few(FewArgs a)
@@ -892,7 +901,9 @@ template <class T, int NT> __global__ __launch_bounds__(64 * kFewWaves) void k_f
     constexpr int VE = kVec<T>, STEP = 4 * VE;
     __shared__ float2 join[kFewWaves][NT * 16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t v0 = ((int64_t)blockIdx.x * kFewWaves + wave) * 16 * kFewRows;
+    const int tile = (int)block_of();
+    if (tile >= a.tiles) return;
+    const int64_t v0 = ((int64_t)tile * kFewWaves + wave) * 16 * kFewRows;
     const T *w[kFewRows], *h[NT];
     const int64_t k_lane = (lane >> 4) * VE;
 #pragma unroll
@@ -968,7 +979,7 @@ template <class T, int NT> __global__ __launch_bounds__(64 * kFewWaves) void k_f
         const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
         for (int k = 0; k < kFewWaves; k++) sum += join[k][n].y * __expf(join[k][n].x - ref);
-        a.part[(int64_t)n * gridDim.x + blockIdx.x] = make_float2(top, sum);
+        a.part[(int64_t)n * a.tiles + tile] = make_float2(top, sum);
     }
 }
 
@@ -1040,6 +1051,7 @@ struct Cut {
         p.n_tiles = n_tiles;
         p.full = full;
         p.splits = splits;
+        p.blocks = blocks();
     }
 };
 
@@ -1155,8 +1167,8 @@ template <class T, bool GRAD, bool TWO> int run_logits(LogitArgs a, int64_t toke
 {
     const Cut c = cut_logits(a.p.a.extent, tokens);
     c.put(a.p);
-    if (c.big) k_logits<T, Big, GRAD, TWO><<<(unsigned)c.blocks(), Big::threads, 0, s>>>(a);
-    else k_logits<T, Small, GRAD, TWO><<<(unsigned)c.blocks(), Small::threads, 0, s>>>(a);
+    if (c.big) k_logits<T, Big, GRAD, TWO><<<grid_of(c.blocks()), Big::threads, 0, s>>>(a);
+    else k_logits<T, Small, GRAD, TWO><<<grid_of(c.blocks()), Small::threads, 0, s>>>(a);
     return c.m_tiles;
 }
 
@@ -1168,7 +1180,8 @@ template <class T, class Out> void run_products(StoreArgs h, StoreArgs w, const 
     cw.put(w.p);
     auto go = [&](auto shape, int hb, int wb, int ht, int wt) {
         using S = decltype(shape);
-        k_products<T, S, Out><<<(unsigned)(hb + wb), S::threads, 0, s>>>(h, w, hb);
+        w.p.blocks = wb;
+        k_products<T, S, Out><<<grid_of((int64_t)hb + wb), S::threads, 0, s>>>(h, w, hb);
         if (ht + wt) k_slabs<S, Out><<<dim3((unsigned)(ht + wt), S::BM * S::BN / 1024), 256, 0, s>>>(h, w, ht);
     };
     auto by_shape = [&](bool big, int hb, int wb, int ht, int wt) {
@@ -1184,7 +1197,7 @@ template <class T, class Out> void run_products(StoreArgs h, StoreArgs w, const 
 
 template <class Out> void run_finish(const StoreArgs &a, hipStream_t s)
 {
-    k_finish<Out><<<dim3((unsigned)a.M, (unsigned)ceil_div(a.N, 256)), 256, 0, s>>>(a);
+    k_finish<Out><<<dim3((unsigned)std::min<int64_t>(a.M, kGridX), (unsigned)ceil_div(a.N, 256)), 256, 0, s>>>(a);
 }
 
 // In: type of the arrays; T: of the products' operands; TWO: in two parts.
@@ -1196,25 +1209,23 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     float *z_target = (float *)(ws + p.z_target);
     const unsigned token_blocks = (unsigned)ceil_div(a.N, 4);
     if (p.few) {
-        const FewArgs f{a.hidden, a.weight, a.ld_hidden, a.ld_weight, a.N, a.V, a.D, a.targets, part, z_target};
         const int tiles = (int)ceil_div(a.V, kFewWords);
-        if (a.N <= 16) k_few<In, 1><<<tiles, 64 * kFewWaves, 0, s>>>(f);
-        else if (a.N <= 32) k_few<In, 2><<<tiles, 64 * kFewWaves, 0, s>>>(f);
-        else k_few<In, 4><<<tiles, 64 * kFewWaves, 0, s>>>(f);
+        const FewArgs f{a.hidden, a.weight, a.ld_hidden, a.ld_weight, a.N, a.V, a.D, a.targets, part, z_target, tiles};
+        if (a.N <= 16) k_few<In, 1><<<grid_of(tiles), 64 * kFewWaves, 0, s>>>(f);
+        else if (a.N <= 32) k_few<In, 2><<<grid_of(tiles), 64 * kFewWaves, 0, s>>>(f);
+        else k_few<In, 4><<<grid_of(tiles), 64 * kFewWaves, 0, s>>>(f);
         const LseArgs l{part, tiles, a.N, a.V, a.targets, z_target, a.loss, a.lse};
-        k_lse<In, T, TWO><<<token_blocks, 256, 0, s>>>(l, (int)token_blocks, PackArgs{});
+        k_lse<In, T, TWO><<<grid_of(token_blocks), 256, 0, s>>>(l, (int)token_blocks, PackArgs{}, 0);
         return hipGetLastError();
     }
     if (a.N == 0) {
         // no tokens: no gradient
-        for (int64_t v = 0; a.D && v < a.V; v += 1 << 20) {
-            StoreArgs e{};
-            e.M = std::min<int64_t>(a.V - v, 1 << 20);
-            e.N = a.D;
-            e.out = (In *)a.dweight + v * a.ld_dweight;
-            e.ld_out = a.ld_dweight;
-            run_finish<In>(e, s);
-        }
+        StoreArgs e{};
+        e.M = a.V;
+        e.N = a.D;
+        e.out = a.dweight;
+        e.ld_out = a.ld_dweight;
+        if (a.D) run_finish<In>(e, s);
         return hipGetLastError();
     }
     float *h_scale = (float *)(ws + p.h_scale), *w_scale = (float *)(ws + p.w_scale), *w_max = (float *)(ws + p.w_max);
@@ -1231,8 +1242,9 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     else {
         k.src = a.hidden, k.ld = a.ld_hidden, k.rows = a.N;
         k.dst = ws + p.hp, k.part = h.part, k.scale = h_scale;
-        k_lay_hidden<In, T, TWO><<<token_blocks + (TWO && back ? kMaxParts : 0), 256, 0, s>>>(
-            k, (int)token_blocks, (const float *)a.weight, a.ld_weight, a.V, w_max);
+        const int parts = TWO && back ? kMaxParts : 0;
+        k_lay_hidden<In, T, TWO><<<grid_of((int64_t)token_blocks + parts), 256, 0, s>>>(
+            k, (int)token_blocks, (const float *)a.weight, a.ld_weight, a.V, w_max, parts);
     }
     unsigned word_blocks = 0;
     if (!TWO && in_place(a.weight, a.ld_weight, a.D)) w.p = a.weight, w.ld = a.ld_weight;
@@ -1242,8 +1254,9 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
         k.dst = ws + p.wp, k.part = w.part, k.scale = w_scale;
         if (TWO && back) k.all = ws + p.all, k.w_max = w_max;
     }
-    if (word_blocks || back)
-        k_lay_weight<In, T, TWO><<<word_blocks + (back ? kUpParts : 0), 256, 0, s>>>(k, (int)word_blocks, u);
+    const int up_parts = back ? kUpParts : 0;
+    if (word_blocks + up_parts)
+        k_lay_weight<In, T, TWO><<<grid_of((int64_t)word_blocks + up_parts), 256, 0, s>>>(k, (int)word_blocks, u, up_parts);
     if (!TWO) w_all = w;
     LogitArgs l{};
     l.p.a = w;
@@ -1264,7 +1277,8 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     v.src = a.hidden, v.ld = a.ld_hidden, v.rows = a.N, v.D = a.D;
     v.dst = ws + p.hs, v.kp = p.kp, v.part = hs.part;
     v.targets = a.targets, v.V = a.V, v.up = a.upstream, v.up_max = up_max;
-    k_lse<In, T, TWO><<<token_blocks * (back ? 2 : 1), 256, 0, s>>>(sums, (int)token_blocks, v);
+    const int hs_blocks = back ? (int)token_blocks : 0;
+    k_lse<In, T, TWO><<<grid_of((int64_t)token_blocks + hs_blocks), 256, 0, s>>>(sums, (int)token_blocks, v, hs_blocks);
     if (!back) return hipGetLastError();
 
     StoreArgs d{};  // dhidden

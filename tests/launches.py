@@ -21,9 +21,9 @@ enum { kKernels = 1 << 14, kLaunches = 1 << 12, kInvalidConfiguration = 9 };
 static struct { const void *f; const char *name; } kernels[kKernels];
 static int n_kernels, n_launches, error;
 static struct { const char *name; dim3 grid, block; } launches[kLaunches];
-static dim3 grid_, block_;
-static size_t shared_;
-static void *stream_;
+/* launches nest: a kernel's arguments may launch another */
+static struct { dim3 grid, block; size_t shared; void *stream; } stack[8];
+static int depth;
 void **__hipRegisterFatBinary(const void *d) { static void *h; (void)d; return &h; }
 void __hipUnregisterFatBinary(void **m) { (void)m; }
 void __hipRegisterVar(void **m, void *v, char *h, char *n, int e, size_t s, int c, int g) {}
@@ -34,12 +34,13 @@ void __hipRegisterFunction(void **m, const void *f, char *d, const char *name, u
 }
 int __hipPushCallConfiguration(dim3 g, dim3 b, size_t s, void *q)
 {
-    grid_ = g, block_ = b, shared_ = s, stream_ = q;
+    stack[depth].grid = g, stack[depth].block = b, stack[depth].shared = s, stack[depth++].stream = q;
     return 0;
 }
 int __hipPopCallConfiguration(dim3 *g, dim3 *b, size_t *s, void **q)
 {
-    *g = grid_, *b = block_, *s = shared_, *q = stream_;
+    depth--;
+    *g = stack[depth].grid, *b = stack[depth].block, *s = stack[depth].shared, *q = stack[depth].stream;
     return 0;
 }
 int hipLaunchKernel(const void *f, dim3 g, dim3 b, void **a, size_t s, void *q)
@@ -47,8 +48,8 @@ int hipLaunchKernel(const void *f, dim3 g, dim3 b, void **a, size_t s, void *q)
     const char *name = "";
     for (int i = 0; i < n_kernels; i++)
         if (kernels[i].f == f) name = kernels[i].name;
-    if (n_launches < kLaunches) launches[n_launches].name = name, launches[n_launches].grid = g, launches[n_launches].block = b;
-    n_launches++;
+    if (n_launches < kLaunches)
+        launches[n_launches].name = name, launches[n_launches].grid = g, launches[n_launches++].block = b;
     /* fewer than 2^32 threads along each axis, at most 65535 workgroups along y and z, none empty */
     if (!g.x || !g.y || !g.z || (uint64_t)g.x * b.x >> 32 || (uint64_t)g.y * b.y >> 32 || g.y > 65535 || g.z > 65535 ||
         (uint64_t)b.x * b.y * b.z > 1024)
@@ -117,8 +118,8 @@ ALL = (1 << 63) - 1  # a workspace of any size
 
 def recorded(calls, tmp_path):
     """[(name, *arguments)] run in a child process: for each {"rc", "error",
-    "need", "kernels"}, the last [[name, grid x, y, z, workgroup x, y, z]]; and
-    the names of all kernels there are."""
+    "need", "kernels"}, the last the first 4096 [name, grid x, y, z, workgroup
+    x, y, z]; and the names of all kernels there are."""
     so = str(tmp_path / "recorder.so")
     subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-w", "-x", "c", "-", "-o", so], input=_RECORDER, text=True, check=True)
     asked = [(c[0], SPECS[c[0]], list(c[1:]) + [None] * (len(SPECS[c[0]]) - len(c) + 1)) for c in calls]

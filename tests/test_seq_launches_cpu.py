@@ -64,3 +64,30 @@ def test_sizes_of_nothing(tmp_path):
                 for B in (0, 2):
                     calls += [("tq_gated_scan_workspace", B, N, V), la.scan(ty, B, N, V), la.scan_grad(ty, B, N, V)]
     run(calls, tmp_path)
+
+
+M31 = (1 << 31) - 1
+
+
+def test_largest_sizes(tmp_path):
+    """Sizes up to the limits that the header names are launched, or refused
+    before anything is: as unsupported, by the checks of the arguments."""
+    calls = []
+    for ty in range(3):
+        calls += [la.embed(ty, M31, V, D) for V in (5, M31) for D in (1, 64, 65, 2048)]
+        calls += [la.embed_grad(ty, N, V, D) for N in (100, 600, M31) for V in (5, M31) for D in (1, 300, 1 << 20)]
+        for B, T, D in ((M31, 1, 1), (M31, 64, 1), (1 << 23, 33, 1), (1 << 23, 64, 130), (1, M31, 1), (1, M31, 4000),
+                        (1 << 16, 1, 1 << 20), (1 << 16, 8, 1 << 20), (1 << 14, 16, 1 << 20), (1 << 26, 1000, 3)):
+            calls += [la.scan(ty, B, T, D), la.scan_grad(ty, B, T, D)]
+        calls += [f(ty, N, D) for f in (la.norm, la.norm_grad)
+                  for N, D in ((M31, 1), (M31, 64), (M31, 100003), (1, M31), (5000, M31), (1 << 22, 16385))]
+        for N, V, D in ((M31, 16, 1), (M31, 16, 64), (4, M31, 64), (60, M31, 64), (100, M31, 33), (100, M31, 64),
+                        (1 << 20, 1 << 20, 64), (1 << 24, 300, 8), (1 << 24, 300, 64), (100, 1 << 26, 32), (1 << 14, 5, 1 << 20)):
+            calls += [la.xent(ty, N, V, D), la.xent_grad(ty, N, V, D)]
+        calls += [la.xent_grad(ty, 0, M31, 64)]
+    run(calls, tmp_path)
+    # too many tiles for one launch
+    for c in (la.xent(0, M31, M31, 8), la.xent_grad(1, M31, 5, 1 << 20), la.xent_grad(1, 5, M31, 1 << 20),
+              la.scan(1, M31, 65, 1), la.scan_grad(0, M31, 64, 65)):
+        got = la.recorded([c], tmp_path)[0][0]
+        assert got["rc"] == 2 and not got["kernels"], (c[0], c[1:8], got["rc"], got["error"])
