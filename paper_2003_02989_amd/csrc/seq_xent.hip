@@ -850,10 +850,12 @@ __global__ __launch_bounds__(256) void k_lse(LseArgs l, int l_blocks, PackArgs h
 // stream kFewRows x 16 words each from memory into 16 x 16 matrix instructions,
 // no LDS, no packing; the few hidden rows come from the caches.  Bound by reading
 // the weights: 4 x 65537 x 512 bf16 15 to 20 us, 3.3 to 4.5 TB/s (67 MB, partly from the
-// last-level cache).  Up to 16 tokens of rows that the tiles can read where they
+// last-level cache).  Up to 16 tokens of weights that the tiles can read where they
 // are (23 us for 16, 41 us for 64; tiles 27 us for 65), else up to kFewTokens, since
 // the tiles need the weights laid out first (fp32 of that size: 73 us for 64 tokens,
-// tiles 111 us for 65).
+// tiles 111 us for 65; 65537 x 500 bf16 28 us for 33 tokens and 32 for 64, laid out
+// 53; rows of 512 that lie 513 apart 41 us for 17 tokens, 45 for 32 and 56 for 64,
+// laid out 50).
 constexpr int kFewTokens = 64, kFewRows = 2, kFewWaves = 4;
 constexpr int kFewWords = 16 * kFewRows * kFewWaves;  // of a workgroup
 
@@ -1115,8 +1117,9 @@ struct XentPlan {
         return cut_products(N, D, words, terms * (up_to(words, kBK) / kBK), terms * (np / kBK));
     }
 
-    XentPlan(int32_t type, int64_t N_, int64_t V_, int64_t D_, bool grad)
-        : two(type == TQ_F32), few(!grad && N_ <= (two || D_ % kBK ? kFewTokens : 16)), terms(two ? 3 : 1), N(N_), V(V_), D(D_)
+    // in_place: the products can read the weights where they are
+    XentPlan(int32_t type, int64_t N_, int64_t V_, int64_t D_, bool grad, bool in_place)
+        : two(type == TQ_F32), few(!grad && N_ <= (in_place ? 16 : kFewTokens)), terms(two ? 3 : 1), N(N_), V(V_), D(D_)
     {
         const size_t elem = 2 * (two ? 2 : 1);
         kp = std::max<int64_t>(up_to(D, kBK), kBK);
@@ -1157,10 +1160,12 @@ struct XentPlan {
     }
 };
 
-// Whether the products can read rows of D 16-bit elements where they are.
-bool in_place(const void *p, int64_t ld, int64_t D)
+// Whether the products can read rows of D elements where they are: whole, aligned
+// ones of 16 bits.
+bool whole_rows(int32_t type, int64_t D) { return type != TQ_F32 && D > 0 && D % kBK == 0; }
+bool in_place(int32_t type, const void *p, int64_t ld, int64_t D)
 {
-    return D % kBK == 0 && D > 0 && ld % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+    return whole_rows(type, D) && ld % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
 }
 
 template <class T, bool GRAD, bool TWO> int run_logits(LogitArgs a, int64_t tokens, hipStream_t s)
@@ -1203,7 +1208,9 @@ template <class Out> void run_finish(const StoreArgs &a, hipStream_t s)
 // In: type of the arrays; T: of the products' operands; TWO: in two parts.
 template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const XentArgs &a, bool grad, hipStream_t s)
 {
-    const XentPlan p(type, a.N, a.V, a.D, grad);
+    const bool h_in_place = in_place(type, a.hidden, a.ld_hidden, a.D);
+    const bool w_in_place = in_place(type, a.weight, a.ld_weight, a.D);
+    const XentPlan p(type, a.N, a.V, a.D, grad, w_in_place);
     char *ws = (char *)a.ws;
     float2 *part = (float2 *)(ws + p.part);
     float *z_target = (float *)(ws + p.z_target);
@@ -1238,7 +1245,7 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     PackArgs k{};
     k.D = a.D;
     k.kp = p.kp;
-    if (!TWO && in_place(a.hidden, a.ld_hidden, a.D)) h.p = a.hidden, h.ld = a.ld_hidden;
+    if (h_in_place) h.p = a.hidden, h.ld = a.ld_hidden;
     else {
         k.src = a.hidden, k.ld = a.ld_hidden, k.rows = a.N;
         k.dst = ws + p.hp, k.part = h.part, k.scale = h_scale;
@@ -1247,7 +1254,7 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
             k, (int)token_blocks, (const float *)a.weight, a.ld_weight, a.V, w_max, parts);
     }
     unsigned word_blocks = 0;
-    if (!TWO && in_place(a.weight, a.ld_weight, a.D)) w.p = a.weight, w.ld = a.ld_weight;
+    if (w_in_place) w.p = a.weight, w.ld = a.ld_weight;
     else {
         word_blocks = (unsigned)ceil_div(a.V, 4);
         k.src = a.weight, k.ld = a.ld_weight, k.rows = a.V;
@@ -1324,7 +1331,9 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
 
 size_t xent_workspace(int32_t type, int64_t N, int64_t V, int64_t D, bool grad)
 {
-    return XentPlan(type, N, V, D, grad).bytes;
+    // where the weights lie is not known here: what either way of a call with few tokens takes
+    const size_t laid_out = XentPlan(type, N, V, D, grad, false).bytes;
+    return whole_rows(type, D) ? std::max(laid_out, XentPlan(type, N, V, D, grad, true).bytes) : laid_out;
 }
 
 hipError_t launch_xent(int32_t type, const XentArgs &a, bool grad, hipStream_t s)

@@ -1,9 +1,11 @@
 """Sequence operators on the GPU at sizes where another variant takes over,
 against the oracle's 64-bit forms, with the tolerances of test_gpu_seq."""
+import numpy as np
 import pytest
 import torch
 
 import test_gpu_seq as base
+from oracle import seq as ref
 from paper_2003_02989_amd import seq
 from test_gpu_seq import TYPES
 
@@ -35,3 +37,23 @@ def test_cross_entropy_of_nothing(ty):
     dh, dW, loss, lse = seq.softmax_xent_grad(e, e, t, up)
     assert dh.shape == dW.shape == (0, 5) and loss.shape == lse.shape == (0,)
     assert seq.softmax_xent(e, e, t)[0].shape == (0,)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("N", [16, 17, 40, 64, 65])
+@pytest.mark.parametrize("ld,shift", [(129, 0), (136, 0), (136, 1), (128, 0)])
+def test_cross_entropy_of_weights_that_lie_anywhere(ty, N, ld, shift):
+    """Whole pieces of D = 128 elements in rows that are aligned or not."""
+    dtype = TYPES[ty][0]
+    rng = np.random.default_rng(N)
+    V, D = 300, 128
+    h, hv = base.put(rng.standard_normal((N, D)), dtype)
+    W, Wv = base.put(0.2 * rng.standard_normal((V, ld)), dtype)
+    room = torch.empty(V * ld + 8, dtype=dtype, device="cuda")[shift:shift + V * ld].view(V, ld)
+    room.copy_(W)
+    t = rng.integers(-1, V + 1, N)
+    loss, lse = seq.softmax_xent(h, room[:, :D], torch.as_tensor(t).cuda())
+    wl, ws, z = ref.xent(hv, Wv[:, :D], t)
+    es = base.logit_error(ty, hv, Wv[:, :D]).max(1) + (V + 32) * base.U + 4 * base.U * np.abs(z).max(1)
+    base.check("lse", lse, ws, es)
+    base.check("loss", loss, wl, np.where((t >= 0) & (t < V), 2 * es, 0))

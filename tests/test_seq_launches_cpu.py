@@ -91,3 +91,13 @@ def test_largest_sizes(tmp_path):
               la.scan(1, M31, 65, 1), la.scan_grad(0, M31, 64, 65)):
         got = la.recorded([c], tmp_path)[0][0]
         assert got["rc"] == 2 and not got["kernels"], (c[0], c[1:8], got["rc"], got["error"])
+
+
+def test_few_tokens_do_not_copy_the_weights(tmp_path):
+    """Losses of up to 64 tokens read the weights where they are, however these lie."""
+    calls = [la.xent(ty, N, 65537, D, ld) for ty in range(3) for N in (1, 16, 17, 40, 64)
+             for D, ld in ((512, 512), (512, 513), (512, 516), (500, 500), (64, 65))]
+    # weights that begin inside a 16-byte piece
+    calls += [c[:7] + (la.P + 2,) + c[8:] for c in calls if c[3] != 0]
+    for c, g in zip(calls, run(calls, tmp_path)):
+        assert not any("k_lay_weight" in n for n in names(g)), (c[3:6], c[2], c[7], names(g))
