@@ -57,6 +57,8 @@ def lib():
 # The smallest calls are all latency: what runs on every call is kept short.
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_device = torch._C._cuda_getDevice
+_many = torch.cuda.device_count() > 1  # else there is no other device to be on
 
 
 def _call(f, *args):
@@ -69,6 +71,8 @@ def _tensor(t, name, dtype=None, shape=None):
     """t, checked to be on the current device, of `dtype` and `shape`."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
+    if _many and t.get_device() != _device():
+        raise ValueError(f"{name} is on device {t.get_device()}, the current device is {_device()}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if shape is not None and t.shape != shape:
@@ -83,10 +87,7 @@ def _typed(t, name):
     code = _TYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-    dev = t.get_device()
-    if dev != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is on device {dev}, the current device is {torch.cuda.current_device()}")
-    return code, dev
+    return code, t.get_device()
 
 
 def _dense(t, name, dtype, shape=None):

@@ -32,3 +32,28 @@ def test_rows_of_strided_tensors():
 
 def test_records_module_imports():
     assert records.RecordModel and records.ising_records
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    class On(torch.Tensor):  # stands for a tensor of device `at`
+        is_cuda = True
+        at = 0
+
+        def get_device(self):
+            return self.at
+
+    def on(t, at):
+        t = t.as_subclass(On)
+        t.at = at
+        return t
+    monkeypatch.setattr(seq, "_many", True, raising=False)
+    monkeypatch.setattr(seq, "_device", lambda: 0, raising=False)
+    x = torch.zeros((2, 3, 4))
+    for take in (lambda t: seq._dense(t, "x", torch.float32), lambda t: seq._rows(t, "x"),
+                 lambda t: seq._steps(t, "x", None, (2, 3, 4))):
+        take(on(x, 0))
+        with pytest.raises(ValueError, match="device 1"):
+            take(on(x, 1))
+    assert seq._typed(on(x, 0), "x") == (0, 0)
+    with pytest.raises(ValueError, match="device 1"):
+        seq._typed(on(x, 1), "x")
