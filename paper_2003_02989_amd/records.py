@@ -45,7 +45,11 @@ def ising_records(n, steps, records, seed, dt=0.25, field=0.9):
 
 class RecordModel:
     """Parameters and one training step; ``dtype`` is that of the parameters'
-    working copies and of the activations, the parameters themselves are fp32."""
+    working copies and of the activations, the parameters themselves are fp32.
+
+    float16 has no numbers below 2^-24, where the terms of a mean over many shots
+    lie: its loss is scaled before the gradients are formed, and they are given
+    back in fp32, without the scale."""
 
     def __init__(self, n, width, dtype=torch.bfloat16, seed=0):
         self.start, self.width, self.dtype = 1 << n, width, dtype
@@ -73,9 +77,16 @@ class RecordModel:
         first = torch.full_like(records[:, :1], self.start)
         return torch.cat((first, records[:, :-1]), 1)
 
+    def loss_scale(self, shots):
+        """A power of two near the root of the number of shots: a shot's part of the
+        gradients is that much above their mean, their sum that much below what it
+        would be without a mean."""
+        return 2.0 ** (shots.bit_length() // 2) if self.dtype == torch.float16 else 1.0
+
     def loss_and_grads(self, records, lengths=None):
-        """(mean loss of the shots there are, gradients in ``dtype``); records
-        [B, T], -1 where there is no shot, lengths int32 [B] or None."""
+        """(mean loss of the shots there are, gradients in ``dtype``, of float16 in
+        fp32); records [B, T], -1 where there is no shot, lengths int32 [B] or
+        None."""
         p, W = self.working(), self.width
         ids = self.inputs(records)
         e = seq.embed(ids, p["table"])
@@ -86,12 +97,17 @@ class RecordModel:
             there &= torch.arange(records.shape[1], device=records.device) < lengths[:, None]
         targets = torch.where(there, records, torch.full_like(records, -1))
         count = there.sum().clamp(min=1).float()
-        dy, dreadout, loss, _ = seq.softmax_xent_grad(y, p["readout"], targets, there.float() / count)
+        scale = self.loss_scale(records.numel())
+        upstream = there.float() / count * scale
+        dy, dreadout, loss, _ = seq.softmax_xent_grad(y, p["readout"], targets, upstream)
         dh, dweight, dbias = seq.layer_norm_grad(h, p["weight"], mean, rstd, dy)
         de = torch.empty_like(e)
         seq.gated_scan_grad(e[..., :W], e[..., W:], kept, dh, lengths=lengths, dx=de[..., :W], dg=de[..., W:])
         dtable = seq.embed_grad(ids, de, self.vocab)
-        return loss.sum() / count, {"table": dtable, "weight": dweight, "bias": dbias, "readout": dreadout}
+        grads = {"table": dtable, "weight": dweight, "bias": dbias, "readout": dreadout}
+        if self.dtype == torch.float16:
+            grads = {k: g.float() / scale for k, g in grads.items()}
+        return loss.sum() / count, grads
 
     def step(self, records, lengths=None, lr=1e-2):
         """One Adam step; returns the loss before it (a device scalar)."""
