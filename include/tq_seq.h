@@ -131,7 +131,10 @@ tq_status tq_softmax_xent(const void *hidden, int64_t ld_hidden, int32_t type, i
  * and dweight = (upstream p)^T hidden, both in the inputs' type; rows without
  * a target (>= V) have zero dhidden and add nothing to dweight, whatever they
  * hold.  loss and lse, the outputs of tq_softmax_xent, come from the same
- * call. */
+ * call.  For 16-bit types p is formed in 32 bits and enters both products
+ * rounded to 16; hidden times upstream enters dweight's product as two 16-bit
+ * numbers, which hold what a single one would lose, unless all upstreams that
+ * are not zero are the same up to powers of two. */
 tq_status tq_softmax_xent_grad_workspace(int32_t type, int64_t N, int64_t V, int64_t D, size_t *bytes);
 tq_status tq_softmax_xent_grad(const void *hidden, int64_t ld_hidden, int32_t type, int64_t N, int64_t V, int64_t D,
                                const void *weight, int64_t ld_weight, const uint64_t *targets, const float *upstream,

@@ -22,11 +22,16 @@
 // The stored p is p itself, up to a power of two: its largest entries are near -1,
 // and a factor common to all tokens would put the same rounding error into each.
 // upstream multiplies dhidden's rows at the end, in fp32, and enters dweight
-// through the hidden rows, relative to the largest, so that the mean's equal
-// weights change nothing there.  fp32 rows are scaled to magnitudes of 2^13 ..
-// 2^14 on their own where the product leaves the row's axis standing; the
-// operands that a product sums over the rows of have one scale for all.
+// through the hidden rows, relative to the largest.  16-bit rows times that have
+// twice the digits, and where any are lost (ups that differ by more than a power of
+// two; the mean's equal weights lose none) they enter as two numbers, too, in two
+// products: rounded to one, dweight is off by 1.4 to 1.5 times what its own rounding
+// costs.  fp32 rows are scaled to magnitudes of 2^13 .. 2^14 on their own where the
+// product leaves the row's axis standing; the operands that a product sums over the
+// rows of have one scale for all, and their digits count from the largest row's.
 #include <algorithm>
+#include <cfloat>
+#include <climits>
 #include <type_traits>
 
 #include "seq.h"
@@ -71,7 +76,7 @@ struct Operand {
 
 struct ProductArgs {
     Operand a, b;
-    int terms;    // 1, or 3 for operands in two parts
+    int terms;    // 1, 2 if the second operand is in two parts, 3 if both are
     int k_tiles;  // K / kBK
     int m_tiles, n_tiles;
     int full;     // tiles that one workgroup computes alone; the others are
@@ -181,11 +186,11 @@ __device__ __forceinline__ void product(const ProductArgs &a, const Stages<T> &l
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
     auto fetch = [&](int kt, T *la, T *lb) {
-        // the small terms first: l_a h_b, h_a l_b, h_a h_b
+        // the small terms first: l_a h_b, h_a l_b, h_a h_b, or the last ones of these
         const int term = kt / a.k_tiles;
         const int64_t k = (int64_t)(kt - term * a.k_tiles) * kBK;
-        const T *ga = (const T *)a.a.p + (a.terms == 3 && term == 0 ? a.a.part : 0);
-        const T *gb = (const T *)a.b.p + (a.terms == 3 && term == 1 ? a.b.part : 0);
+        const T *ga = (const T *)a.a.p + (term == a.terms - 3 ? a.a.part : 0);
+        const T *gb = (const T *)a.b.p + (term == a.terms - 2 ? a.b.part : 0);
         if constexpr (TA) stage_t<T, S::BM, S::waves>(la, ga, a.a, k, m0, wave, lane);
         else stage<T, S::BM, S::waves>(la, ga, a.a, k, m0, wave, lane);
         if constexpr (TB) stage_t<T, S::BN, S::waves>(lb, gb, a.b, k, n0, wave, lane);
@@ -473,12 +478,15 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
 }
 
 // ------------------------------------------------------------ the products
-// Partial maxima, by kUpParts workgroups, over the rows with a target and a finite
-// up that is not zero: of |up|, and of the exponents of up times the row's scale.
+// By kUpParts workgroups, over the rows with a target and a finite up that is not
+// zero: the largest |up| and exponent of up times the row's scale; the least and
+// the largest digits of up past its exponent.
 constexpr int kUpParts = 64;
 struct UpParts {
     float up[kUpParts];
     int bits[kUpParts];
+    int least[kUpParts], most[kUpParts];
+    int terms;  // of dweight's product of 16-bit rows, written with its hidden rows
 };
 // The largest |up| (1 if there is none), and the power of two that dweight's
 // hidden rows are scaled by, 0 for 16-bit rows: it brings the largest of up
@@ -501,6 +509,20 @@ __device__ __forceinline__ UpMax up_max_of(const UpParts *p)
     return UpMax{u, e > -1000 ? e - exponent(u) : 0};
 }
 
+// Whether two ups differ by more than a power of two: hidden rows times up over the
+// largest up do not fit 16 bits then.
+__device__ __forceinline__ bool up_varies(const UpParts *p)
+{
+    const int lane = threadIdx.x & 63;
+    int least = p->least[lane], most = p->most[lane];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        least = min(least, __shfl_xor(least, d, 64));
+        most = max(most, __shfl_xor(most, d, 64));
+    }
+    return least < most;
+}
+
 // What becomes of C: out = factor(row) C, or C is added up in fp32 over the
 // pieces of the vocabulary (`sum`), or a part of a tile goes to its slab.
 struct StoreArgs {
@@ -518,6 +540,7 @@ struct StoreArgs {
     int64_t V;
     const UpParts *up_max;
     const float *w_max;
+    const int *terms;  // NULL: p.terms
 };
 
 // The power of two that brings numbers of magnitude up to m into [2^13, 2^14).
@@ -563,16 +586,18 @@ struct Factor {
 template <class T, class S, bool TA, class Out>
 __device__ __forceinline__ void product_tile(const StoreArgs &a, const Stages<T> &lds, int blk)
 {
-    const Tile t = tile_of(a.p, blk);
+    ProductArgs p = a.p;
+    if (a.terms) p.terms = *a.terms;
+    const Tile t = tile_of(p, blk);
     f32x16 acc[S::FM][S::FN];
     const int64_t m0 = t.m * S::BM, n0 = t.n * S::BN;
-    const int all = a.p.terms * a.p.k_tiles;
+    const int all = p.terms * p.k_tiles;
     int k0 = 0, k1 = all;
     if (t.split >= 0) {
-        k0 = (int)((int64_t)all * t.split / a.p.splits);
-        k1 = (int)((int64_t)all * (t.split + 1) / a.p.splits);
+        k0 = (int)((int64_t)all * t.split / p.splits);
+        k1 = (int)((int64_t)all * (t.split + 1) / p.splits);
     }
-    product<T, S, TA, true>(a.p, lds, m0, n0, k0, k1, acc);
+    product<T, S, TA, true>(p, lds, m0, n0, k0, k1, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
     if (t.split >= 0) {
@@ -689,11 +714,12 @@ struct PackArgs {
     void *all;          // fp32: a second copy with the scale of the maximum in w_max
     const float *w_max;
     // dst for dweight's product: zeros for rows without a target, other rows
-    // times up, relative to the largest, and 2^-bits
+    // times up, relative to the largest, and 2^-bits; of 16-bit rows a second part
+    // with what the first one's rounding lost, unless it lost nothing
     const uint64_t *targets;
     int64_t V;
     const float *up;
-    const UpParts *up_max;
+    UpParts *up_max;
 };
 
 // One wavefront per row, four rows per workgroup.
@@ -724,7 +750,12 @@ template <class In, class T, bool TWO> __device__ __forceinline__ void pack_rows
         if (a.scale && lane == 0) a.scale[r] = two_to(-bits);
     }
     float share = 1.f;
+    bool second = false;
     if (a.up) {
+        if constexpr (!TWO) {
+            second = up_varies(a.up_max);
+            if (r == 0 && lane == 0) a.up_max->terms = second ? 2 : 1;
+        }
         on = a.targets[r] < (uint64_t)a.V;
         share = on ? a.up[r] / largest.up : 0.f;
         bits = -largest.bits;
@@ -737,9 +768,10 @@ template <class In, class T, bool TWO> __device__ __forceinline__ void pack_rows
 #pragma unroll
         for (int j = 0; j < VE; j++) {
             g[j] = TWO ? ldexpf(f[j] * share, bits) : f[j] * share;
-            if (TWO) lo[j] = g[j] - (float)(T)g[j];
+            lo[j] = g[j] - (float)(T)g[j];
         }
         store_vec<VE>(dst, g);
+        if (second) store_vec<VE>(dst + a.part, lo);
         if constexpr (TWO) {
             store_vec<VE>(dst + a.part, lo);
             if (a.all) {
@@ -765,26 +797,38 @@ struct UpArgs {
 __device__ __forceinline__ void up_max(const UpArgs &a, int blk)
 {
     __shared__ float reds[4];
-    __shared__ int rede[4];
+    __shared__ int rede[4], redl[4], redm[4];
     float top = 0.f;
-    int e = -1000;
+    int e = -1000, least = INT_MAX, most = 0;
     for (int64_t i = (int64_t)blk * 256 + threadIdx.x; i < a.N; i += 256 * kUpParts) {
         const float u = fabsf(a.up[i]);
         const bool on = a.targets[i] < (uint64_t)a.V && u > 0.f && u < INFINITY;
+        const int digits = __float_as_int(u) & 0x7fffff;
         top = on ? fmaxf(top, u) : top;
+        // numbers below the normal ones have their digits elsewhere
+        least = on ? min(least, u < FLT_MIN ? -1 : digits) : least;
+        most = on ? max(most, digits) : most;
         if (a.scale) e = on ? max(e, exponent(u) + exponent(a.scale[i])) : e;
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
         top = fmaxf(top, __shfl_xor(top, d, 64));
         e = max(e, __shfl_xor(e, d, 64));
+        least = min(least, __shfl_xor(least, d, 64));
+        most = max(most, __shfl_xor(most, d, 64));
     }
-    if ((threadIdx.x & 63) == 0) reds[threadIdx.x >> 6] = top, rede[threadIdx.x >> 6] = e;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) reds[wave] = top, rede[wave] = e, redl[wave] = least, redm[wave] = most;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 0; w < 4; w++) top = fmaxf(top, reds[w]), e = max(e, rede[w]);
+        for (int w = 0; w < 4; w++) {
+            top = fmaxf(top, reds[w]), e = max(e, rede[w]);
+            least = min(least, redl[w]), most = max(most, redm[w]);
+        }
         a.out->up[blk] = top;
         a.out->bits[blk] = e;
+        a.out->least[blk] = least;
+        a.out->most[blk] = most;
     }
 }
 
@@ -1142,7 +1186,7 @@ struct XentPlan {
             all = c.take(two ? elem * V * kp : 0);
             w_max = c.take(sizeof(float) * kMaxParts);
             up_max = c.take(sizeof(UpParts));
-            hs = c.take(elem * N * kp);
+            hs = c.take(sizeof(uint16_t) * 2 * N * kp);  // in two parts, 16-bit rows too
             prob = c.take(elem * np * words);
             sum = c.take(piece < V ? sizeof(float) * N * D : 0);
             size_t sh = 0, sw = 0;
@@ -1320,6 +1364,7 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
         e.p.a = Operand{ws + p.prob, kv, l.prob_part, kv, p.np};
         e.p.b = hs;
         e.p.terms = p.terms;
+        e.terms = TWO ? nullptr : &up_max->terms;
         e.p.k_tiles = (int)(p.np / kBK);
         run_products<T, In>(d, e, v0 + words < a.V ? p.cuts : p.last_cuts, s);
     }

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import test_gpu_seq as base
+from gpu_util import say
 from oracle import seq as ref
 from paper_2003_02989_amd import seq
 from test_gpu_seq import TYPES
@@ -57,3 +58,30 @@ def test_cross_entropy_of_weights_that_lie_anywhere(ty, N, ld, shift):
     es = base.logit_error(ty, hv, Wv[:, :D]).max(1) + (V + 32) * base.U + 4 * base.U * np.abs(z).max(1)
     base.check("lse", lse, ws, es)
     base.check("loss", loss, wl, np.where((t >= 0) & (t < V), 2 * es, 0))
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f16"])
+@pytest.mark.parametrize("kind", ["equal", "powers of two", "any", "signs and zeros", "two classes"])
+@pytest.mark.parametrize("N,V,D", [(600, 4097, 64), (1000, 4097, 130)])
+def test_cross_entropy_gradient_of_unequal_tokens(ty, kind, N, V, D):
+    """dweight loses nothing to upstream: its error is that of its own rounding and
+    of p's.  With u half a unit of 1, rounding numbers of any digits costs 0.42 u in
+    the mean square, and p just below 1 is off by u / 2 / sqrt(3) = 0.29 u: together
+    1.21 times the former at most.  A further rounding of any digits makes it 1.41
+    at least."""
+    dtype = TYPES[ty][0]
+    rng = np.random.default_rng(N)
+    h, hv = base.put(rng.standard_normal((N, D)), dtype)
+    W, Wv = base.put(1.5 / np.sqrt(D) * rng.standard_normal((V, D)), dtype)
+    t = rng.integers(0, V, N)
+    up = {"equal": np.full(N, 0.7), "powers of two": 0.7 * 2.0 ** -rng.integers(0, 9, N), "any": rng.random(N) + 0.02,
+          "signs and zeros": rng.standard_normal(N) * (rng.random(N) < 0.8),
+          "two classes": np.where(rng.random(N) < 0.5, 1.0, 0.37)}[kind]
+    up, upv = base.put(up, torch.float32)
+    dh, dW, _, _ = seq.softmax_xent_grad(h, W, torch.as_tensor(t).cuda(), up)
+    wdh, wdW, _, _, _ = ref.xent_grad(hv, Wv, t, upv)
+    for name, got, want in (("dhidden", dh, wdh), ("dweight", dW, wdW)):
+        least = np.linalg.norm(torch.as_tensor(want).to(dtype).double().numpy() - want)
+        err = np.linalg.norm(got.double().cpu().numpy() - want)
+        say(ty, kind, name, err / least)
+        assert err <= 1.25 * least, name
