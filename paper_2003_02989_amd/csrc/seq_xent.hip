@@ -892,9 +892,11 @@ __global__ __launch_bounds__(256) void k_lse(LseArgs l, int l_blocks, PackArgs h
 // ------------------------------------------------------- a few tokens
 // With few tokens the weights are what there is to read: wavefronts
 // stream kFewRows x 16 words each from memory into 16 x 16 matrix instructions,
-// no LDS, no packing; the few hidden rows come from the caches.  Bound by reading
-// the weights: 4 x 65537 x 512 bf16 15 to 20 us, 3.3 to 4.5 TB/s (67 MB, partly from the
-// last-level cache).  Up to 16 tokens of weights that the tiles can read where they
+// no LDS, no packing; the few hidden rows come from the caches.  4 x 65537 x 512
+// bf16 15 to 20 us, 3.3 to 4.5 TB/s (67 MB, partly from the last-level cache): the
+// weights are all there is to read, but a wavefront waits for each step's reads
+// before it asks for the next one's (the compiler does not unroll loops around
+// matrix instructions whose trip count it does not know).  Up to 16 tokens of weights that the tiles can read where they
 // are (23 us for 16, 41 us for 64; tiles 27 us for 65), else up to kFewTokens, since
 // the tiles need the weights laid out first (fp32 of that size: 73 us for 64 tokens,
 // tiles 111 us for 65; 65537 x 500 bf16 28 us for 33 tokens and 32 for 64, laid out
@@ -964,7 +966,6 @@ template <class T, int NT> __global__ __launch_bounds__(64 * kFewWaves) void k_f
 #pragma unroll
         for (int t = 0; t < NT; t++) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int64_t whole = a.D / STEP * STEP;
-#pragma unroll 4
     for (int64_t k = k_lane; k < whole; k += STEP) {
         T x[kFewRows][VE], y[NT][VE];
 #pragma unroll
