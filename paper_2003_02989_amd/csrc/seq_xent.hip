@@ -479,13 +479,13 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
 
 // ------------------------------------------------------------ the products
 // By kUpParts workgroups, over the rows with a target and a finite up that is not
-// zero: the largest |up| and exponent of up times the row's scale; the least and
-// the largest digits of up past its exponent.
+// zero: the largest |up|; of fp32 rows the largest exponent of up times the row's
+// scale (else -1000); of 16-bit rows the least and the largest digits of up.
 constexpr int kUpParts = 64;
 struct UpParts {
     float up[kUpParts];
     int bits[kUpParts];
-    int least[kUpParts], most[kUpParts];
+    int least[kUpParts], most[kUpParts];  // of 16-bit rows
     int terms;  // of dweight's product of 16-bit rows, written with its hidden rows
 };
 // The largest |up| (1 if there is none), and the power of two that dweight's
@@ -794,41 +794,39 @@ struct UpArgs {
     int64_t N, V;
     UpParts *out;
 };
-__device__ __forceinline__ void up_max(const UpArgs &a, int blk)
+template <bool TWO> __device__ __forceinline__ void up_max(const UpArgs &a, int blk)
 {
     __shared__ float reds[4];
-    __shared__ int rede[4], redl[4], redm[4];
+    __shared__ int low[4], high[4];
     float top = 0.f;
-    int e = -1000, least = INT_MAX, most = 0;
+    // fp32: the largest exponent, in `most`; 16 bits: the least and largest digits
+    int least = INT_MAX, most = TWO ? -1000 : 0;
     for (int64_t i = (int64_t)blk * 256 + threadIdx.x; i < a.N; i += 256 * kUpParts) {
         const float u = fabsf(a.up[i]);
         const bool on = a.targets[i] < (uint64_t)a.V && u > 0.f && u < INFINITY;
-        const int digits = __float_as_int(u) & 0x7fffff;
         top = on ? fmaxf(top, u) : top;
-        // numbers below the normal ones have their digits elsewhere
-        least = on ? min(least, u < FLT_MIN ? -1 : digits) : least;
-        most = on ? max(most, digits) : most;
-        if (a.scale) e = on ? max(e, exponent(u) + exponent(a.scale[i])) : e;
+        if constexpr (TWO) most = on ? max(most, exponent(u) + exponent(a.scale[i])) : most;
+        else {
+            const int digits = __float_as_int(u) & 0x7fffff;
+            // numbers below the normal ones have their digits elsewhere
+            least = on ? min(least, u < FLT_MIN ? -1 : digits) : least;
+            most = on ? max(most, digits) : most;
+        }
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
         top = fmaxf(top, __shfl_xor(top, d, 64));
-        e = max(e, __shfl_xor(e, d, 64));
-        least = min(least, __shfl_xor(least, d, 64));
         most = max(most, __shfl_xor(most, d, 64));
+        if constexpr (!TWO) least = min(least, __shfl_xor(least, d, 64));
     }
     const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) reds[wave] = top, rede[wave] = e, redl[wave] = least, redm[wave] = most;
+    if ((threadIdx.x & 63) == 0) reds[wave] = top, low[wave] = least, high[wave] = most;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 0; w < 4; w++) {
-            top = fmaxf(top, reds[w]), e = max(e, rede[w]);
-            least = min(least, redl[w]), most = max(most, redm[w]);
-        }
+        for (int w = 0; w < 4; w++) top = fmaxf(top, reds[w]), least = min(least, low[w]), most = max(most, high[w]);
         a.out->up[blk] = top;
-        a.out->bits[blk] = e;
-        a.out->least[blk] = least;
-        a.out->most[blk] = most;
+        a.out->bits[blk] = TWO ? most : -1000;
+        if constexpr (!TWO) a.out->least[blk] = least, a.out->most[blk] = most;
     }
 }
 
@@ -878,7 +876,7 @@ __global__ __launch_bounds__(256) void k_lay_weight(PackArgs w, int w_blocks, Up
 {
     const int blk = (int)block_of();
     if (blk < w_blocks) pack_rows<In, T, TWO>(w, blk);
-    else if (blk - w_blocks < up_blocks) up_max(u, blk - w_blocks);
+    else if (blk - w_blocks < up_blocks) up_max<TWO>(u, blk - w_blocks);
 }
 // After the logits: lse and loss, and hidden's rows laid out for dweight.
 template <class In, class T, bool TWO>
