@@ -7,15 +7,27 @@
 namespace tq {
 
 // A launch has fewer than 2^32 threads along x: from kGridX workgroups on (of at
-// most 1024 threads) they go on along y.  The last row's may be past the end: every
-// kernel launched so returns in them before it reads or writes anything.
+// most 1024 threads) they go on along y.
 constexpr unsigned kGridX = 1 << 21;
+
+// In one launch, the last row of which may be past the end: the kernel returns in
+// those workgroups before it reads or writes anything.
 inline dim3 grid_of(int64_t blocks)
 {
     if (blocks <= kGridX) return dim3((unsigned)blocks);
     return dim3(kGridX, (unsigned)((blocks + kGridX - 1) / kGridX));
 }
-// The number of a workgroup of such a launch, below 2^32.
+// In whole rows and a rest, each calling go(grid, number of its first workgroup):
+// no workgroup is past the end, which small kernels would wait for their arguments
+// to find out (0.3 us).
+template <class F> void launch_exactly(int64_t blocks, F &&go)
+{
+    const int64_t rows = blocks / kGridX, rest = blocks % kGridX;
+    if (rows) go(dim3(kGridX, (unsigned)rows), (uint32_t)0);
+    if (rest) go(dim3((unsigned)rest), (uint32_t)(rows * kGridX));
+}
+
+// The number of a workgroup within a launch of either kind, below 2^32.
 __device__ __forceinline__ uint32_t block_of() { return blockIdx.y * kGridX + blockIdx.x; }
 
 // Elements per 16-byte access.

@@ -74,7 +74,8 @@ template <class T> __device__ __forceinline__ void gate(float g, float &a, float
 // Agent scope reaches the other XCDs; nothing else is handed over, so no ordering
 // is needed.
 struct Geom {
-    uint32_t rows, slabs, items;  // rows: records x slabs; items: rows x segs
+    uint32_t rows, slabs;  // rows: records x slabs
+    uint32_t first;        // of the launch
     int segs;
     Slot *slots;   // [segs][rows][kSlab]
     unsigned *ticket;
@@ -143,7 +144,7 @@ template <class K> struct Place {
 
 __device__ __forceinline__ uint32_t take_item(const Geom &g)
 {
-    if (g.segs == 1) return block_of();
+    if (g.segs == 1) return g.first + block_of();
     __shared__ uint32_t item;
     if (threadIdx.x == 0) item = atomicAdd(g.ticket, 1u);
     __syncthreads();
@@ -275,9 +276,7 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArg
     constexpr int CV = K::CV, L = K::steps;
     __shared__ float2 agg[kWaves][K::slab];
     __shared__ SlotPair win[kWindows][kWaves][K::slab];
-    const uint32_t item = take_item(g);
-    if (item >= g.items) return;
-    const Place<K> at(a, g, item, false);
+    const Place<K> at(a, g, take_item(g), false);
     T *y = (T *)a.y + at.b * a.yb + at.t0 * a.ys;
     float ga[L][CV], gb[L][CV], A[CV], B[CV];
     if (at.idle()) {
@@ -379,9 +378,7 @@ template <class K> __global__ __launch_bounds__(kThreads, 4) void k_scan_grad(Sc
     __shared__ float2 agg[kWaves][K::slab];
     __shared__ SlotPair win[kWindows][kWaves][K::slab];
     __shared__ float rev[kWaves][K::slab];
-    const uint32_t item = take_item(g);
-    if (item >= g.items) return;
-    const Place<K> at(a, g, item, true);
+    const Place<K> at(a, g, take_item(g), true);
     T *dx = (T *)a.dx + at.b * a.dxb + at.t0 * a.dxs, *dg = (T *)a.dg + at.b * a.dgb + at.t0 * a.dgs;
     float ga[L][CV], gc[L][CV], A[CV], Bf[CV], Br[CV];
     if (at.idle()) {
@@ -632,7 +629,7 @@ template <class K> struct Layout {
     Geom start(void *ws, hipStream_t s) const
     {
         Geom g{};
-        g.rows = (uint32_t)rows, g.slabs = (uint32_t)slabs, g.items = (uint32_t)items, g.segs = segs;
+        g.rows = (uint32_t)rows, g.slabs = (uint32_t)slabs, g.segs = segs;
         if (segs == 1) return g;
         g.slots = (Slot *)((char *)ws + slots);
         g.ticket = (unsigned *)((char *)ws + ticket);
@@ -662,7 +659,11 @@ template <class T> hipError_t scan_t(const ScanArgs &a, hipStream_t s)
     return by_kind<T, false>(a.D, [&](auto kind) {
         using K = decltype(kind);
         const Layout<K> l(a.B, a.T, a.D);
-        k_scan<K><<<grid_of(l.items), kThreads, 0, s>>>(a, l.start(a.ws, s));
+        Geom g = l.start(a.ws, s);
+        launch_exactly(l.items, [&](dim3 grid, uint32_t first) {
+            g.first = first;
+            k_scan<K><<<grid, kThreads, 0, s>>>(a, g);
+        });
         return hipGetLastError();
     });
 }
@@ -681,7 +682,11 @@ template <class T> hipError_t scan_grad_t(const ScanArgs &a, hipStream_t s)
     return by_kind<T, true>(a.D, [&](auto kind) {
         using K = decltype(kind);
         const Layout<K> l(a.B, a.T, a.D);
-        k_scan_grad<K><<<grid_of(l.items), kThreads, 0, s>>>(a, l.start(a.ws, s));
+        Geom g = l.start(a.ws, s);
+        launch_exactly(l.items, [&](dim3 grid, uint32_t first) {
+            g.first = first;
+            k_scan_grad<K><<<grid, kThreads, 0, s>>>(a, g);
+        });
         return hipGetLastError();
     });
 }

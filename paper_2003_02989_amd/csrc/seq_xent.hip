@@ -81,7 +81,6 @@ struct ProductArgs {
     int m_tiles, n_tiles;
     int full;     // tiles that one workgroup computes alone; the others are
     int splits;   // cut into this many, along K or (logits) along N
-    int blocks;   // workgroups of all tiles
 };
 
 // Tile of C, wavefronts WM x WN, each with FM x FN blocks of 32 x 32.
@@ -291,6 +290,7 @@ struct LogitArgs {
     const float *lse;
     void *prob;        // [tokens, words] of the piece, both up to a multiple of kBK
     int64_t ld_prob, prob_rows, prob_part;
+    uint32_t first;    // of the launch
 };
 
 //
@@ -462,9 +462,7 @@ template <class T, class S, bool GRAD, bool TWO> __global__ __launch_bounds__(S:
 {
     TQ_STAGES(T, S, lds);
     __shared__ float2 join[GRAD ? 1 : std::max(S::WM * S::BN, Half::WM * Half::BN)];
-    const int blk = (int)block_of();
-    if (blk >= a.p.blocks) return;
-    const Tile t = tile_of(a.p, blk);
+    const Tile t = tile_of(a.p, (int)(a.first + block_of()));
     const int64_t m0 = t.m * S::BM, n0 = t.n * S::BN;
     if constexpr (std::is_same_v<S, Big>)
         if (t.split >= 0) {
@@ -635,12 +633,12 @@ __device__ __forceinline__ void product_tile(const StoreArgs &a, const Stages<T>
 // fill what the former's last round leaves free, in the others.  8192 x 65537 x 1024
 // bf16, in two pieces: 1040 us each, 1060 TFLOP/s, the matrix units busy half of the time.
 template <class T, class S, class Out>
-__global__ __launch_bounds__(S::threads) void k_products(StoreArgs h, StoreArgs w, int h_blocks)
+__global__ __launch_bounds__(S::threads) void k_products(StoreArgs h, StoreArgs w, int h_blocks, uint32_t first)
 {
     TQ_STAGES(T, S, lds);
-    const int blk = (int)block_of();
+    const int blk = (int)(first + block_of());
     if (blk < h_blocks) product_tile<T, S, false, Out>(h, lds, blk);
-    else if (blk - h_blocks < w.p.blocks) product_tile<T, S, true, Out>(w, lds, blk - h_blocks);
+    else product_tile<T, S, true, Out>(w, lds, blk - h_blocks);
 }
 
 // The tiles that were cut along K: their slabs, added up in order.
@@ -940,6 +938,7 @@ struct FewArgs {
     float2 *part;  // [N, tiles]
     float *z_target;
     int tiles;
+    uint32_t first;  // of the launch
 };
 
 template <class T, int NT> __global__ __launch_bounds__(64 * kFewWaves) void k_few(FewArgs a)
@@ -947,8 +946,7 @@ template <class T, int NT> __global__ __launch_bounds__(64 * kFewWaves) void k_f
     constexpr int VE = kVec<T>, STEP = 4 * VE;
     __shared__ float2 join[kFewWaves][NT * 16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int tile = (int)block_of();
-    if (tile >= a.tiles) return;
+    const int tile = (int)(a.first + block_of());
     const int64_t v0 = ((int64_t)tile * kFewWaves + wave) * 16 * kFewRows;
     const T *w[kFewRows], *h[NT];
     const int64_t k_lane = (lane >> 4) * VE;
@@ -1096,7 +1094,6 @@ struct Cut {
         p.n_tiles = n_tiles;
         p.full = full;
         p.splits = splits;
-        p.blocks = blocks();
     }
 };
 
@@ -1215,8 +1212,11 @@ template <class T, bool GRAD, bool TWO> int run_logits(LogitArgs a, int64_t toke
 {
     const Cut c = cut_logits(a.p.a.extent, tokens);
     c.put(a.p);
-    if (c.big) k_logits<T, Big, GRAD, TWO><<<grid_of(c.blocks()), Big::threads, 0, s>>>(a);
-    else k_logits<T, Small, GRAD, TWO><<<grid_of(c.blocks()), Small::threads, 0, s>>>(a);
+    launch_exactly(c.blocks(), [&](dim3 grid, uint32_t first) {
+        a.first = first;
+        if (c.big) k_logits<T, Big, GRAD, TWO><<<grid, Big::threads, 0, s>>>(a);
+        else k_logits<T, Small, GRAD, TWO><<<grid, Small::threads, 0, s>>>(a);
+    });
     return c.m_tiles;
 }
 
@@ -1228,8 +1228,9 @@ template <class T, class Out> void run_products(StoreArgs h, StoreArgs w, const 
     cw.put(w.p);
     auto go = [&](auto shape, int hb, int wb, int ht, int wt) {
         using S = decltype(shape);
-        w.p.blocks = wb;
-        k_products<T, S, Out><<<grid_of((int64_t)hb + wb), S::threads, 0, s>>>(h, w, hb);
+        launch_exactly((int64_t)hb + wb, [&](dim3 grid, uint32_t first) {
+            k_products<T, S, Out><<<grid, S::threads, 0, s>>>(h, w, hb, first);
+        });
         if (ht + wt) k_slabs<S, Out><<<dim3((unsigned)(ht + wt), S::BM * S::BN / 1024), 256, 0, s>>>(h, w, ht);
     };
     auto by_shape = [&](bool big, int hb, int wb, int ht, int wt) {
@@ -1260,10 +1261,13 @@ template <class In, class T, bool TWO> hipError_t xent_t(int32_t type, const Xen
     const unsigned token_blocks = (unsigned)ceil_div(a.N, 4);
     if (p.few) {
         const int tiles = (int)ceil_div(a.V, kFewWords);
-        const FewArgs f{a.hidden, a.weight, a.ld_hidden, a.ld_weight, a.N, a.V, a.D, a.targets, part, z_target, tiles};
-        if (a.N <= 16) k_few<In, 1><<<grid_of(tiles), 64 * kFewWaves, 0, s>>>(f);
-        else if (a.N <= 32) k_few<In, 2><<<grid_of(tiles), 64 * kFewWaves, 0, s>>>(f);
-        else k_few<In, 4><<<grid_of(tiles), 64 * kFewWaves, 0, s>>>(f);
+        FewArgs f{a.hidden, a.weight, a.ld_hidden, a.ld_weight, a.N, a.V, a.D, a.targets, part, z_target, tiles, 0};
+        launch_exactly(tiles, [&](dim3 grid, uint32_t first) {
+            f.first = first;
+            if (a.N <= 16) k_few<In, 1><<<grid, 64 * kFewWaves, 0, s>>>(f);
+            else if (a.N <= 32) k_few<In, 2><<<grid, 64 * kFewWaves, 0, s>>>(f);
+            else k_few<In, 4><<<grid, 64 * kFewWaves, 0, s>>>(f);
+        });
         const LseArgs l{part, tiles, a.N, a.V, a.targets, z_target, a.loss, a.lse};
         k_lse<In, T, TWO><<<grid_of(token_blocks), 256, 0, s>>>(l, (int)token_blocks, PackArgs{}, 0);
         return hipGetLastError();
