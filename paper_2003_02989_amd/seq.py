@@ -290,6 +290,8 @@ def layer_norm(x, weight, bias=None, eps=1e-5, keep=False, y=None):
     mean = rstd = None
     if keep:
         mean, rstd = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
+        if not D:  # of no values
+            mean.fill_(float("nan")), rstd.fill_(float("nan"))
     _call((_lib or lib()).tq_layer_norm, xp, ld, code, x.numel() // D if D else 0, D, wp, bp, eps, yp, ldy, _ptr(mean),
           _ptr(rstd), _raw_stream(dev))
     return (y, mean, rstd) if keep else y

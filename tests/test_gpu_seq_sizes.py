@@ -85,3 +85,12 @@ def test_cross_entropy_gradient_of_unequal_tokens(ty, kind, N, V, D):
         err = np.linalg.norm(got.double().cpu().numpy() - want)
         say(ty, kind, name, err / least)
         assert err <= 1.25 * least, name
+
+
+def test_layer_norm_of_no_values():
+    """Rows without columns: their mean is not a number, whatever the memory held."""
+    torch.full((2, 64), 3.0, device="cuda")  # what the allocator hands out next
+    y, mean, rstd = seq.layer_norm(torch.zeros((64, 0), device="cuda"), torch.zeros(0, device="cuda"), keep=True)
+    assert y.shape == (64, 0) and torch.isnan(mean).all() and torch.isnan(rstd).all()
+    dx, dw, db = seq.layer_norm_grad(y, torch.zeros(0, device="cuda"), mean, rstd, y)
+    assert dx.shape == (64, 0) and dw.shape == db.shape == (0,)
