@@ -23,8 +23,9 @@
  *    axis; a leading dimension or stride counts elements.  Arrays need the
  *    alignment of their element only.
  *  - Sums, recurrent states and softmax statistics are kept in 32 bits; an
- *    output of a 16-bit type is rounded to it once.  No sum is formed with
- *    floating-point atomics: every output is bitwise reproducible.
+ *    output of a 16-bit type is rounded to it once, after that.  What is rounded
+ *    on the way stands at the call (tq_softmax_xent_grad).  No sum is formed
+ *    with floating-point atomics: every output is bitwise reproducible.
  *  - Ids are uint64 as tq_sample writes them.  An id >= V, such as the marker
  *    2^64 - 1 of a missing shot, is no error: it has an embedding of zeros and
  *    no loss, and no gradient comes from it.
@@ -69,8 +70,10 @@ tq_status tq_embed_grad(const void *grad_out, int64_t ld_grad_out, int32_t type,
  * tq_gated_scan_grad starts from: float [B, ceil(T / TQ_SCAN_PIECE), D], the
  * state before step j * TQ_SCAN_PIECE (steps past a record's length: not
  * written).
- * h0, h_last and states are contiguous.  TQ_E_UNSUPPORTED for D > 2^20 or
- * B ceil(D / 64) ceil(T / 64) >= 2^31. */
+ * h0, h_last and states are contiguous.  Once a channel's state is infinite or
+ * NaN its later ones are infinite or NaN too; which of the two is not fixed
+ * (gates multiplied together may be zero where none of them is).
+ * TQ_E_UNSUPPORTED for D > 2^20 or B ceil(D / 64) ceil(T / 64) >= 2^31. */
 #define TQ_SCAN_PIECE 64
 tq_status tq_gated_scan_workspace(int64_t B, int64_t T, int64_t D, size_t *bytes);
 tq_status tq_gated_scan(int32_t type, int64_t B, int64_t T, int64_t D, const void *x, int64_t x_batch, int64_t x_step,
@@ -134,7 +137,11 @@ tq_status tq_softmax_xent(const void *hidden, int64_t ld_hidden, int32_t type, i
  * call.  For 16-bit types p is formed in 32 bits and enters both products
  * rounded to 16; hidden times upstream enters dweight's product as two 16-bit
  * numbers, which hold what a single one would lose, unless all upstreams that
- * are not zero are the same up to powers of two. */
+ * are not zero are the same up to powers of two.  In f16 a token's part of
+ * dweight is resolved to 2^-25 of the largest upstream times one.  For fp32 the
+ * numbers that a sum over rows is formed of have their 22 bits at the largest row
+ * and less below it: dhidden's terms are resolved to 2^-38 of the largest weight
+ * times one, dweight's to 2^-38 of the largest hidden times upstream. */
 tq_status tq_softmax_xent_grad_workspace(int32_t type, int64_t N, int64_t V, int64_t D, size_t *bytes);
 tq_status tq_softmax_xent_grad(const void *hidden, int64_t ld_hidden, int32_t type, int64_t N, int64_t V, int64_t D,
                                const void *weight, int64_t ld_weight, const uint64_t *targets, const float *upstream,
