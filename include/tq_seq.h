@@ -141,7 +141,8 @@ tq_status tq_softmax_xent(const void *hidden, int64_t ld_hidden, int32_t type, i
  * dweight is resolved to 2^-25 of the largest upstream times one.  For fp32 the
  * numbers that a sum over rows is formed of have their 22 bits at the largest row
  * and less below it: dhidden's terms are resolved to 2^-38 of the largest weight
- * times one, dweight's to 2^-38 of the largest hidden times upstream. */
+ * times one, dweight's to 2^-38 of the largest hidden times upstream.  For f16 and
+ * fp32 p is resolved to 2^-40 at least. */
 tq_status tq_softmax_xent_grad_workspace(int32_t type, int64_t N, int64_t V, int64_t D, size_t *bytes);
 tq_status tq_softmax_xent_grad(const void *hidden, int64_t ld_hidden, int32_t type, int64_t N, int64_t V, int64_t D,
                                const void *weight, int64_t ld_weight, const uint64_t *targets, const float *upstream,
