@@ -1,0 +1,74 @@
+/*
+ * tq_model.h -- C ABI of the operators of selective models of measurement
+ * records, part of libtq: beside the operators of tq_seq.h, whose conventions
+ * hold here too.
+ *
+ * A selective model of records mixes a few neighbouring steps of a record
+ * (tq_causal_conv) and carries a state along it whose decay and whose input
+ * depend on each step (tq_selective_scan); both advance by single steps where
+ * records are extended.
+ */
+#ifndef TQ_MODEL_H
+#define TQ_MODEL_H
+
+#include "tq_seq.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* The selective state space scan over time of B records of T steps, D channels
+ * and S states (1 <= S <= 64) per channel: with
+ *     d_t = softplus(dt_t + dt_bias)                                  [D]
+ *     h_t = exp(d_t A) h_{t-1} + d_t x_t B_t   (h_{-1} = h0[b])       [D, S]
+ *     y_t = (sum_s C_t[s] h_t[:, s] + skip x_t) silu(z_t)             [D]
+ * for t < lengths[b] (clamped to [0, T]; NULL: all T).  Past its length a record
+ * keeps its state, y is zero and x, dt, B, C and z are not looked at.  x, dt, z
+ * and y are [B, T, D], Bm and Cm (the B_t and C_t) [B, T, S], each with a batch
+ * and a step stride of its own; A is float [D, S], skip and dt_bias float [D].
+ * NULL stands for zeros in h0, skip and dt_bias; a NULL z leaves the factor
+ * silu(z) out.  h_last float [B, D, S], the last state, may be h0 itself and may
+ * be NULL: a call with T = 1 then advances the records' states in place.
+ * states, when not NULL, receives what tq_selective_scan_grad starts from: float
+ * [B, ceil(T / TQ_STATES_PIECE), S, D], the state before every step that is a
+ * multiple of TQ_STATES_PIECE (past a record's length: not written).
+ * TQ_E_UNSUPPORTED for S > 64, D > 2^20 or B ceil(D / 64) ceil(T / 64) >= 2^31. */
+#define TQ_STATES_PIECE 16
+tq_status tq_selective_scan_workspace(int64_t B, int64_t T, int64_t D, int64_t S, size_t *bytes);
+tq_status tq_selective_scan(int32_t type, int64_t B, int64_t T, int64_t D, int64_t S, const void *x, int64_t x_batch,
+                            int64_t x_step, const void *dt, int64_t dt_batch, int64_t dt_step, const float *A,
+                            const void *Bm, int64_t B_batch, int64_t B_step, const void *Cm, int64_t C_batch,
+                            int64_t C_step, const float *skip, const void *z, int64_t z_batch, int64_t z_step,
+                            const float *dt_bias, const float *h0, const int32_t *lengths, void *y, int64_t y_batch,
+                            int64_t y_step, float *h_last, float *states, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/* Gradients of tq_selective_scan from dy, the gradient of y, and dh_last (NULL:
+ * zeros), that of h_last.  With q_t = dy_t silu(z_t), a_t = exp(d_t A) and
+ * l_t = C_t q_t + a_{t+1} l_{t+1} (dh_last in place of a l at the record's last step),
+ *     dx_t = d_t sum_s B_t l_t + skip q_t,       dskip = sum_bt q_t x_t,
+ *     dC_t = sum_d q_t h_t,                      dB_t = sum_d d_t x_t l_t,
+ *     dd_t = sum_s (A a_t h_{t-1} + B_t x_t) l_t,  ddt_t = dd_t sigmoid(dt_t + dt_bias),
+ *     dA = sum_bt d_t a_t h_{t-1} l_t,           ddt_bias = sum_bt ddt_t,
+ *     dz_t = dy_t (sum_s C_t h_t + skip x_t) silu'(z_t),  dh0 = a_0 l_0;
+ * dx, ddt, dz, dB and dC are zero past the record's length.  dx, ddt, dz [B, T, D]
+ * and dB, dC [B, T, S] have the inputs' type and strides of their own; dA, dskip,
+ * ddt_bias and dh0 are float as the tensors that they belong to.  dz goes with z;
+ * dskip, ddt_bias and dh0 may be NULL: not wanted.  `states` are the ones that
+ * tq_selective_scan wrote for the same inputs. */
+tq_status tq_selective_scan_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t S, size_t *bytes);
+tq_status tq_selective_scan_grad(int32_t type, int64_t B, int64_t T, int64_t D, int64_t S, const void *x,
+                                 int64_t x_batch, int64_t x_step, const void *dt, int64_t dt_batch, int64_t dt_step,
+                                 const float *A, const void *Bm, int64_t B_batch, int64_t B_step, const void *Cm,
+                                 int64_t C_batch, int64_t C_step, const float *skip, const void *z, int64_t z_batch,
+                                 int64_t z_step, const float *dt_bias, const float *states, const int32_t *lengths,
+                                 const void *dy, int64_t dy_batch, int64_t dy_step, const float *dh_last, void *dx,
+                                 int64_t dx_batch, int64_t dx_step, void *ddt, int64_t ddt_batch, int64_t ddt_step,
+                                 void *dz, int64_t dz_batch, int64_t dz_step, void *dB, int64_t dB_batch,
+                                 int64_t dB_step, void *dC, int64_t dC_batch, int64_t dC_step, float *dA, float *dskip,
+                                 float *ddt_bias, float *dh0, void *workspace, size_t workspace_bytes, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* TQ_MODEL_H */

@@ -1,0 +1,102 @@
+"""Plain 64-bit forms of the operators of selective models (test infrastructure
+only), written from the definitions, step by step, in float64 numpy.
+
+Functions whose results the tests compare with rounded ones also return
+magnitudes: the same sums with the absolute values of their terms, which rounding
+errors scale with.
+"""
+import numpy as np
+
+
+def sigmoid(v):
+    e = np.exp(-np.abs(v))
+    return np.where(v >= 0, 1 / (1 + e), e / (1 + e))
+
+
+def softplus(v):
+    return np.maximum(v, 0) + np.log1p(np.exp(-np.abs(v)))
+
+
+def _count(lengths, B, T):
+    return np.full(B, T) if lengths is None else np.clip(lengths, 0, T)
+
+
+def selective_scan(x, dt, A, Bm, Cm, skip, z, bias, h0, lengths):
+    """y, h_last, p (y before its gate), all states [B, T + 1, D, S] (first: h0;
+    past the length: kept), and (pm, pe, m, e): the magnitudes of p and of the
+    states, and bounds of their errors in units of one rounding in 32 bits.
+
+    With v = dt + bias rounded once, d = softplus(v) is off by |v| + 16 units (the
+    exponential, two reciprocals, the series), the exponent d A by 4 more; the decay
+    is off by |d A| times that and by 2 units of its own, a step's sum by one."""
+    B, T, D = x.shape
+    S = A.shape[1]
+    n = _count(lengths, B, T)
+    zero = np.zeros(D)
+    skip = zero if skip is None else skip
+    bias = zero if bias is None else bias
+    h = np.zeros((B, T + 1, D, S))
+    m, e = np.zeros_like(h), np.zeros_like(h)
+    if h0 is not None:
+        h[:, 0], m[:, 0] = h0, np.abs(h0)
+    y, p, pm, pe = (np.zeros((B, T, D)) for _ in range(4))
+    for b in range(B):
+        for t in range(T):
+            if t >= n[b]:
+                h[b, t + 1], m[b, t + 1], e[b, t + 1] = h[b, t], m[b, t], e[b, t]
+                continue
+            v = dt[b, t] + bias
+            d, off = softplus(v), np.abs(v) + 20
+            a = np.exp(d[:, None] * A)
+            u = (d * x[b, t])[:, None] * Bm[b, t]
+            h[b, t + 1] = a * h[b, t] + u
+            m[b, t + 1] = a * m[b, t] + np.abs(u)
+            e[b, t + 1] = a * (e[b, t] + (3 + (off * d)[:, None] * np.abs(A)) * m[b, t]) + (3 + off)[:, None] * np.abs(u)
+            p[b, t] = (Cm[b, t] * h[b, t + 1]).sum(-1) + skip * x[b, t]
+            pm[b, t] = (np.abs(Cm[b, t]) * m[b, t + 1]).sum(-1) + np.abs(skip * x[b, t])
+            pe[b, t] = (np.abs(Cm[b, t]) * e[b, t + 1]).sum(-1) + (S + 2) * pm[b, t]
+            y[b, t] = p[b, t] * (1 if z is None else z[b, t] * sigmoid(z[b, t]))
+    return y, h[:, T], p, h, (pm, pe, m, e)
+
+
+def selective_scan_grad(x, dt, A, Bm, Cm, skip, z, bias, h0, lengths, dy, dh_last, absolute=False):
+    """dx, ddt, dA, dB, dC, dskip, dz, ddt_bias, dh0.  With `absolute` every term
+    counts with its magnitude instead: what the errors of the sums scale with."""
+    f = np.abs if absolute else lambda v: v
+    B, T, D = x.shape
+    S = A.shape[1]
+    n = _count(lengths, B, T)
+    zero = np.zeros(D)
+    skip_, bias_ = zero if skip is None else skip, zero if bias is None else bias
+    _, _, p, h, (pm, _, m, _) = selective_scan(x, dt, A, Bm, Cm, skip, z, bias, h0, lengths)
+    if absolute:
+        h, p = m, pm
+    dx, ddt, dz = (np.zeros((B, T, D)) for _ in range(3))
+    dB, dC = np.zeros((B, T, S)), np.zeros((B, T, S))
+    dA, dskip, dbias, dh0 = np.zeros((D, S)), np.zeros(D), np.zeros(D), np.zeros((B, D, S))
+    for b in range(B):
+        r = np.zeros((D, S)) if dh_last is None else f(dh_last[b])
+        for t in range(n[b] - 1, -1, -1):
+            v = dt[b, t] + bias_
+            d, sg = softplus(v), sigmoid(v)
+            a = np.exp(d[:, None] * A)
+            xt, Bt, Ct = f(x[b, t]), f(Bm[b, t]), f(Cm[b, t])
+            q = f(dy[b, t])
+            if z is not None:
+                s = sigmoid(z[b, t])
+                # silu' is a sum of two terms, which cancel near z = -1.28
+                dz[b, t] = f(dy[b, t]) * p[b, t] * (s + f(z[b, t]) * s * (1 - s))
+                q = q * f(z[b, t] * s)
+            l = q[:, None] * Ct + r
+            dC[b, t] = (q[:, None] * h[b, t + 1]).sum(0)
+            dB[b, t] = ((d * xt)[:, None] * l).sum(0)
+            bl = (Bt * l).sum(-1)
+            dx[b, t] = d * bl + f(skip_) * q
+            w = a * h[b, t] * l
+            ddt[b, t] = ((f(A) * w).sum(-1) + xt * bl) * sg
+            dA += d[:, None] * w
+            dskip += q * xt
+            dbias += ddt[b, t]
+            r = a * l
+        dh0[b] = r
+    return dx, ddt, dA, dB, dC, dskip, dz, dbias, dh0

@@ -1,0 +1,38 @@
+// model.h -- launchers of the kernels of selective models; arguments are checked
+// by the callers (model_abi.cpp).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "../../include/tq_model.h"
+
+namespace tq {
+
+// An array of steps: element c of step t of record b at p + b batch + t step + c.
+struct Steps {
+    const void *p;
+    int64_t batch, step;
+};
+struct StepsOut {
+    void *p;
+    int64_t batch, step;
+};
+
+struct SelectArgs {
+    int64_t B, T, D;
+    int S;
+    Steps x, dt, Bm, Cm, z, dy;
+    const float *A, *skip, *dt_bias, *h0, *dh_last, *states_in;
+    const int32_t *lengths;
+    StepsOut y, dx, ddt, dz, dB, dC;
+    float *h_last, *states, *dA, *dskip, *ddt_bias, *dh0;
+    void *ws;
+};
+size_t select_workspace(int64_t B, int64_t T, int64_t D, int64_t S);
+size_t select_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t S);
+hipError_t launch_select(int32_t type, const SelectArgs &a, hipStream_t s);
+hipError_t launch_select_grad(int32_t type, const SelectArgs &a, hipStream_t s);
+
+} // namespace tq

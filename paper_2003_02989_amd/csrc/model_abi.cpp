@@ -1,0 +1,152 @@
+// model_abi.cpp -- the extern "C" entry points of tq_model.h: every argument is
+// checked here, on the host, before anything is enqueued.
+#include <algorithm>
+
+#include "abi_checks.h"
+#include "model.h"
+
+using namespace tq;
+
+namespace {
+
+constexpr int64_t kMaxStates = 64;
+
+void check_select(const char *call, int type, int64_t B, int64_t T, int64_t D, int64_t S)
+{
+    check_type(call, type);
+    check_size(call, "B", B);
+    check_size(call, "T", T);
+    check_size(call, "D", D);
+    if (S < 1) fail(TQ_E_INVALID, text(call, "a channel needs one state at least"));
+    if (S > kMaxStates) fail(TQ_E_UNSUPPORTED, text(call, "S must be at most 64"));
+    if (D > kMaxWidth) fail(TQ_E_UNSUPPORTED, text(call, "D must be at most 2^20"));
+    // in doubles: the product of three sizes
+    if ((double)B * (double)((D + 63) / 64) * (double)((T + 63) / 64) > kMaxIndex)
+        fail(TQ_E_UNSUPPORTED, text(call, "B * ceil(D / 64) * ceil(T / 64) must be below 2^31"));
+}
+
+void check_steps(const char *call, const char *name, int64_t B, int64_t T, int64_t D, const Steps &s, size_t align)
+{
+    check_strides(call, name, B, T, D, s.batch, s.step, false);
+    check_array(call, name, s.p, align);
+}
+
+void check_steps(const char *call, const char *name, int64_t B, int64_t T, int64_t D, const StepsOut &s, size_t align)
+{
+    check_strides(call, name, B, T, D, s.batch, s.step, true);
+    check_array(call, name, s.p, align);
+}
+
+} // namespace
+
+extern "C" {
+
+tq_status tq_selective_scan_workspace(int64_t B, int64_t T, int64_t D, int64_t S, size_t *bytes)
+{
+    return guarded([&] {
+        check_select("selective_scan_workspace", TQ_F32, B, T, D, S);
+        give(bytes, B && D ? select_workspace(B, T, D, S) : 0);
+    });
+}
+
+tq_status tq_selective_scan_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t S, size_t *bytes)
+{
+    return guarded([&] {
+        check_select("selective_scan_grad_workspace", TQ_F32, B, T, D, S);
+        give(bytes, D ? select_grad_workspace(B, T, D, S) : 0);
+    });
+}
+
+tq_status tq_selective_scan(int32_t type, int64_t B, int64_t T, int64_t D, int64_t S, const void *x, int64_t x_batch,
+                            int64_t x_step, const void *dt, int64_t dt_batch, int64_t dt_step, const float *A,
+                            const void *Bm, int64_t B_batch, int64_t B_step, const void *Cm, int64_t C_batch,
+                            int64_t C_step, const float *skip, const void *z, int64_t z_batch, int64_t z_step,
+                            const float *dt_bias, const float *h0, const int32_t *lengths, void *y, int64_t y_batch,
+                            int64_t y_step, float *h_last, float *states, void *workspace, size_t workspace_bytes,
+                            void *stream)
+{
+    return guarded([&] {
+        const char *call = "selective_scan";
+        check_select(call, type, B, T, D, S);
+        if (B == 0 || D == 0) return;
+        const size_t e = size_of(type);
+        SelectArgs a{};
+        a.B = B, a.T = T, a.D = D, a.S = (int)S;
+        a.x = {x, x_batch, x_step}, a.dt = {dt, dt_batch, dt_step}, a.z = {z, z_batch, z_step};
+        a.Bm = {Bm, B_batch, B_step}, a.Cm = {Cm, C_batch, C_step}, a.y = {y, y_batch, y_step};
+        if (T) {
+            check_steps(call, "x", B, T, D, a.x, e);
+            check_steps(call, "dt", B, T, D, a.dt, e);
+            check_steps(call, "B", B, T, S, a.Bm, e);
+            check_steps(call, "C", B, T, S, a.Cm, e);
+            if (z) check_steps(call, "z", B, T, D, a.z, e);
+            check_steps(call, "y", B, T, D, a.y, e);
+            check_array(call, "A", A, 4);
+        }
+        check_maybe("skip", skip, 4);
+        check_maybe("dt_bias", dt_bias, 4);
+        check_maybe("h0", h0, 4);
+        check_maybe("lengths", lengths, 4);
+        check_maybe("h_last", h_last, 4);
+        check_maybe("states", states, 4);
+        check_space(call, workspace, workspace_bytes, select_workspace(B, T, D, S));
+        a.A = A, a.skip = skip, a.dt_bias = dt_bias, a.h0 = h0, a.lengths = lengths;
+        a.h_last = h_last, a.states = states, a.ws = workspace;
+        hip_check(launch_select(type, a, as_stream(stream)), "selective scan launch");
+    });
+}
+
+tq_status tq_selective_scan_grad(int32_t type, int64_t B, int64_t T, int64_t D, int64_t S, const void *x,
+                                 int64_t x_batch, int64_t x_step, const void *dt, int64_t dt_batch, int64_t dt_step,
+                                 const float *A, const void *Bm, int64_t B_batch, int64_t B_step, const void *Cm,
+                                 int64_t C_batch, int64_t C_step, const float *skip, const void *z, int64_t z_batch,
+                                 int64_t z_step, const float *dt_bias, const float *states, const int32_t *lengths,
+                                 const void *dy, int64_t dy_batch, int64_t dy_step, const float *dh_last, void *dx,
+                                 int64_t dx_batch, int64_t dx_step, void *ddt, int64_t ddt_batch, int64_t ddt_step,
+                                 void *dz, int64_t dz_batch, int64_t dz_step, void *dB, int64_t dB_batch,
+                                 int64_t dB_step, void *dC, int64_t dC_batch, int64_t dC_step, float *dA, float *dskip,
+                                 float *ddt_bias, float *dh0, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return guarded([&] {
+        const char *call = "selective_scan_grad";
+        check_select(call, type, B, T, D, S);
+        if (D == 0) return;
+        const size_t e = size_of(type);
+        SelectArgs a{};
+        a.B = B, a.T = T, a.D = D, a.S = (int)S;
+        a.x = {x, x_batch, x_step}, a.dt = {dt, dt_batch, dt_step}, a.z = {z, z_batch, z_step};
+        a.Bm = {Bm, B_batch, B_step}, a.Cm = {Cm, C_batch, C_step}, a.dy = {dy, dy_batch, dy_step};
+        a.dx = {dx, dx_batch, dx_step}, a.ddt = {ddt, ddt_batch, ddt_step}, a.dz = {dz, dz_batch, dz_step};
+        a.dB = {dB, dB_batch, dB_step}, a.dC = {dC, dC_batch, dC_step};
+        if (B && T) {
+            check_steps(call, "x", B, T, D, a.x, e);
+            check_steps(call, "dt", B, T, D, a.dt, e);
+            check_steps(call, "B", B, T, S, a.Bm, e);
+            check_steps(call, "C", B, T, S, a.Cm, e);
+            if (!z != !dz) fail(TQ_E_INVALID, text(call, "dz goes with z"));
+            if (z) check_steps(call, "z", B, T, D, a.z, e);
+            if (z) check_steps(call, "dz", B, T, D, a.dz, e);
+            check_steps(call, "dy", B, T, D, a.dy, e);
+            check_steps(call, "dx", B, T, D, a.dx, e);
+            check_steps(call, "ddt", B, T, D, a.ddt, e);
+            check_steps(call, "dB", B, T, S, a.dB, e);
+            check_steps(call, "dC", B, T, S, a.dC, e);
+            check_array(call, "A", A, 4);
+            check_array(call, "states", states, 4);
+        }
+        check_array(call, "dA", dA, 4);
+        check_maybe("skip", skip, 4);
+        check_maybe("dt_bias", dt_bias, 4);
+        check_maybe("lengths", lengths, 4);
+        check_maybe("dh_last", dh_last, 4);
+        check_maybe("dskip", dskip, 4);
+        check_maybe("ddt_bias", ddt_bias, 4);
+        check_maybe("dh0", dh0, 4);
+        check_space(call, workspace, workspace_bytes, select_grad_workspace(B, T, D, S));
+        a.A = A, a.skip = skip, a.dt_bias = dt_bias, a.states_in = states, a.lengths = lengths, a.dh_last = dh_last;
+        a.dA = dA, a.dskip = dskip, a.ddt_bias = ddt_bias, a.dh0 = dh0, a.ws = workspace;
+        hip_check(launch_select_grad(type, a, as_stream(stream)), "selective scan gradient launch");
+    });
+}
+
+} // extern "C"

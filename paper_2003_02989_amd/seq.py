@@ -129,7 +129,7 @@ def _steps(t, name, dtype, shape):
     """(pointer, batch stride, step stride) of a [B, T, D] tensor."""
     _tensor(t, name, dtype, shape)
     sb, ss, sd = t.stride()
-    if sd != 1 and shape[2] > 1:
+    if sd != 1 and shape[2] > 1 and t.numel():
         raise ValueError(f"{name} must be contiguous along its last axis")
     return t.data_ptr(), sb, ss
 
