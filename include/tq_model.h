@@ -68,6 +68,36 @@ tq_status tq_selective_scan_grad(int32_t type, int64_t B, int64_t T, int64_t D, 
                                  int64_t dB_step, void *dC, int64_t dC_batch, int64_t dC_step, float *dA, float *dskip,
                                  float *ddt_bias, float *dh0, void *workspace, size_t workspace_bytes, void *stream);
 
+/* The short causal convolution over time, channel by channel, of B records of T
+ * steps with K taps (1 <= K <= 8):
+ *     u_t = bias + sum_k weight[k] x_{t - K + 1 + k},   y_t = silu ? u_t sigmoid(u_t) : u_t
+ * for t < lengths[b] (clamped to [0, T]; NULL: all T); past it y is zero and x is
+ * not looked at.  x and y are [B, T, D] with strides of their own, weight [K, D],
+ * bias [D] (NULL: zeros), all of `type`.  state [B, K - 1, D] (NULL: zeros) holds
+ * the inputs before the first step, the latest one last, and last [B, K - 1, D]
+ * (NULL: not wanted) receives the inputs before the step after the record's last
+ * one; it may be `state` itself: records are then extended in place.
+ * TQ_E_UNSUPPORTED for K > 8, D > 2^20 or B ceil(T / 8) ceil(D / 4) >= 2^31
+ * (for D < 8: B ceil(T / 8) D). */
+tq_status tq_causal_conv(int32_t type, int64_t B, int64_t T, int64_t D, int64_t K, const void *x, int64_t x_batch,
+                         int64_t x_step, const void *weight, const void *bias, const void *state,
+                         const int32_t *lengths, int32_t silu, void *y, int64_t y_batch, int64_t y_step, void *last,
+                         void *stream);
+
+/* Gradients of tq_causal_conv from dy, the gradient of y, and dlast (NULL:
+ * zeros), that of last: with g_t = dy_t silu'(u_t) (or dy_t),
+ *     dx_t = sum_k weight[k] g_{t + K - 1 - k}, dlast added to the record's last K - 1 inputs,
+ *     dweight[k] = sum_bt g_t x_{t - K + 1 + k},   dbias = sum_bt g_t,
+ * and dstate, the same as dx for the inputs that `state` holds; dx is zero past the
+ * record's length.  All have the inputs' type; dbias and dstate may be NULL: not
+ * wanted. */
+tq_status tq_causal_conv_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t K, size_t *bytes);
+tq_status tq_causal_conv_grad(int32_t type, int64_t B, int64_t T, int64_t D, int64_t K, const void *x, int64_t x_batch,
+                              int64_t x_step, const void *weight, const void *bias, const void *state,
+                              const int32_t *lengths, int32_t silu, const void *dy, int64_t dy_batch, int64_t dy_step,
+                              const void *dlast, void *dx, int64_t dx_batch, int64_t dx_step, void *dweight,
+                              void *dbias, void *dstate, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

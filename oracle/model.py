@@ -100,3 +100,48 @@ def selective_scan_grad(x, dt, A, Bm, Cm, skip, z, bias, h0, lengths, dy, dh_las
             r = a * l
         dh0[b] = r
     return dx, ddt, dA, dB, dC, dskip, dz, dbias, dh0
+
+
+def causal_conv(x, w, bias, state, lengths, silu):
+    """y, last, u (y before silu) and u's magnitude"""
+    B, T, D = x.shape
+    K = w.shape[0]
+    n = _count(lengths, B, T)
+    y, u, um = (np.zeros((B, T, D)) for _ in range(3))
+    last = np.zeros((B, K - 1, D))
+    for b in range(B):
+        xs = np.concatenate([np.zeros((K - 1, D)) if state is None else state[b], x[b, :n[b]]])
+        last[b] = xs[n[b]:]
+        for t in range(n[b]):
+            terms = w * xs[t:t + K]
+            u[b, t] = terms.sum(0) + (0 if bias is None else bias)
+            um[b, t] = np.abs(terms).sum(0) + (0 if bias is None else np.abs(bias))
+            y[b, t] = u[b, t] * sigmoid(u[b, t]) if silu else u[b, t]
+    return y, last, u, um
+
+
+def causal_conv_grad(x, w, bias, state, lengths, silu, dy, dlast, absolute=False):
+    """dx, dweight, dbias, dstate.  With `absolute` every term counts with its
+    magnitude; an error of u's sum moves silu' by at most half of it (|silu''| <=
+    1/2), so that K units of u's magnitude count beside silu's own terms."""
+    f = np.abs if absolute else lambda v: v
+    B, T, D = x.shape
+    K = w.shape[0]
+    n = _count(lengths, B, T)
+    _, _, u, um = causal_conv(x, w, bias, state, lengths, silu)
+    dx, dw, db, ds = np.zeros((B, T, D)), np.zeros((K, D)), np.zeros(D), np.zeros((B, K - 1, D))
+    for b in range(B):
+        xs = np.concatenate([np.zeros((K - 1, D)) if state is None else state[b], x[b, :n[b]]])
+        back = np.zeros_like(xs)
+        if dlast is not None:
+            back[n[b]:] += f(dlast[b])
+        for t in range(n[b]):
+            s = sigmoid(u[b, t])
+            slope = s + f(u[b, t]) * s * (1 - s) + (um[b, t] if absolute else 0) if silu else 1
+            g = f(dy[b, t]) * slope
+            for k in range(K):
+                back[t + k] += f(w[k]) * g
+                dw[k] += g * f(xs[t + k])
+            db += g
+        ds[b], dx[b, :n[b]] = back[:K - 1], back[K - 1:]
+    return dx, dw, db, ds

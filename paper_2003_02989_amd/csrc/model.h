@@ -35,4 +35,19 @@ size_t select_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t S);
 hipError_t launch_select(int32_t type, const SelectArgs &a, hipStream_t s);
 hipError_t launch_select_grad(int32_t type, const SelectArgs &a, hipStream_t s);
 
+struct ConvArgs {
+    int64_t B, T, D, K;
+    Steps x, dy;
+    StepsOut y, dx;
+    const void *weight, *bias, *state, *dlast;  // [K, D], [D], [B, K - 1, D]
+    const int32_t *lengths;
+    bool silu;
+    void *last, *dweight, *dbias, *dstate;
+    void *ws;
+};
+int64_t conv_items(int64_t B, int64_t T, int64_t D);  // threads of a call at most
+size_t conv_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t K);
+hipError_t launch_conv(int32_t type, const ConvArgs &a, hipStream_t s);
+hipError_t launch_conv_grad(int32_t type, const ConvArgs &a, hipStream_t s);
+
 } // namespace tq

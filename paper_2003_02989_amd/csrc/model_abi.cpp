@@ -9,7 +9,7 @@ using namespace tq;
 
 namespace {
 
-constexpr int64_t kMaxStates = 64;
+constexpr int64_t kMaxStates = 64, kMaxTaps = 8;
 
 void check_select(const char *call, int type, int64_t B, int64_t T, int64_t D, int64_t S)
 {
@@ -35,6 +35,19 @@ void check_steps(const char *call, const char *name, int64_t B, int64_t T, int64
 {
     check_strides(call, name, B, T, D, s.batch, s.step, true);
     check_array(call, name, s.p, align);
+}
+
+void check_conv(const char *call, int type, int64_t B, int64_t T, int64_t D, int64_t K)
+{
+    check_type(call, type);
+    check_size(call, "B", B);
+    check_size(call, "T", T);
+    check_size(call, "D", D);
+    if (K < 1) fail(TQ_E_INVALID, text(call, "a convolution needs one tap at least"));
+    if (K > kMaxTaps) fail(TQ_E_UNSUPPORTED, text(call, "K must be at most 8"));
+    if (D > kMaxWidth) fail(TQ_E_UNSUPPORTED, text(call, "D must be at most 2^20"));
+    if (conv_items(B, T, D) > kMaxIndex || conv_items(B, 1, D) > kMaxIndex)
+        fail(TQ_E_UNSUPPORTED, text(call, "B * ceil(T / 8) * ceil(D / 4) must be below 2^31"));
 }
 
 } // namespace
@@ -146,6 +159,75 @@ tq_status tq_selective_scan_grad(int32_t type, int64_t B, int64_t T, int64_t D, 
         a.A = A, a.skip = skip, a.dt_bias = dt_bias, a.states_in = states, a.lengths = lengths, a.dh_last = dh_last;
         a.dA = dA, a.dskip = dskip, a.ddt_bias = ddt_bias, a.dh0 = dh0, a.ws = workspace;
         hip_check(launch_select_grad(type, a, as_stream(stream)), "selective scan gradient launch");
+    });
+}
+
+tq_status tq_causal_conv(int32_t type, int64_t B, int64_t T, int64_t D, int64_t K, const void *x, int64_t x_batch,
+                         int64_t x_step, const void *weight, const void *bias, const void *state,
+                         const int32_t *lengths, int32_t silu, void *y, int64_t y_batch, int64_t y_step, void *last,
+                         void *stream)
+{
+    return guarded([&] {
+        const char *call = "causal_conv";
+        check_conv(call, type, B, T, D, K);
+        if (B == 0 || D == 0) return;
+        const size_t e = size_of(type);
+        ConvArgs a{};
+        a.B = B, a.T = T, a.D = D, a.K = K;
+        a.x = {x, x_batch, x_step}, a.y = {y, y_batch, y_step};
+        check_array(call, "weight", weight, e);
+        if (T) {
+            check_steps(call, "x", B, T, D, a.x, e);
+            check_steps(call, "y", B, T, D, a.y, e);
+        }
+        check_maybe("bias", bias, e);
+        check_maybe("state", state, e);
+        check_maybe("lengths", lengths, 4);
+        check_maybe("last", last, e);
+        a.weight = weight, a.bias = bias, a.state = state, a.lengths = lengths, a.silu = silu != 0, a.last = last;
+        hip_check(launch_conv(type, a, as_stream(stream)), "causal convolution launch");
+    });
+}
+
+tq_status tq_causal_conv_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t K, size_t *bytes)
+{
+    return guarded([&] {
+        check_conv("causal_conv_grad_workspace", TQ_F32, B, T, D, K);
+        give(bytes, D ? conv_grad_workspace(B, T, D, K) : 0);
+    });
+}
+
+tq_status tq_causal_conv_grad(int32_t type, int64_t B, int64_t T, int64_t D, int64_t K, const void *x, int64_t x_batch,
+                              int64_t x_step, const void *weight, const void *bias, const void *state,
+                              const int32_t *lengths, int32_t silu, const void *dy, int64_t dy_batch, int64_t dy_step,
+                              const void *dlast, void *dx, int64_t dx_batch, int64_t dx_step, void *dweight,
+                              void *dbias, void *dstate, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return guarded([&] {
+        const char *call = "causal_conv_grad";
+        check_conv(call, type, B, T, D, K);
+        if (D == 0) return;
+        const size_t e = size_of(type);
+        ConvArgs a{};
+        a.B = B, a.T = T, a.D = D, a.K = K;
+        a.x = {x, x_batch, x_step}, a.dy = {dy, dy_batch, dy_step}, a.dx = {dx, dx_batch, dx_step};
+        check_array(call, "weight", weight, e);
+        check_array(call, "dweight", dweight, e);
+        if (B && T) {
+            check_steps(call, "x", B, T, D, a.x, e);
+            check_steps(call, "dy", B, T, D, a.dy, e);
+            check_steps(call, "dx", B, T, D, a.dx, e);
+        }
+        check_maybe("bias", bias, e);
+        check_maybe("state", state, e);
+        check_maybe("lengths", lengths, 4);
+        check_maybe("dlast", dlast, e);
+        check_maybe("dbias", dbias, e);
+        check_maybe("dstate", dstate, e);
+        check_space(call, workspace, workspace_bytes, conv_grad_workspace(B, T, D, K));
+        a.weight = weight, a.bias = bias, a.state = state, a.lengths = lengths, a.silu = silu != 0, a.dlast = dlast;
+        a.dweight = dweight, a.dbias = dbias, a.dstate = dstate, a.ws = workspace;
+        hip_check(launch_conv_grad(type, a, as_stream(stream)), "causal convolution gradient launch");
     });
 }
 

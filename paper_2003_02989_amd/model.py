@@ -34,6 +34,10 @@ def lib():
             "tq_selective_scan_grad_workspace": [i64, i64, i64, i64, need],
             "tq_selective_scan_grad": [i32, i64, i64, i64, i64, *steps, *steps, vp, *steps, *steps, vp, *steps, vp, vp, vp,
                                        *steps, vp, *steps, *steps, *steps, *steps, *steps, vp, vp, vp, vp, vp, sz, vp],
+            "tq_causal_conv": [i32, i64, i64, i64, i64, *steps, vp, vp, vp, vp, i32, *steps, vp, vp],
+            "tq_causal_conv_grad_workspace": [i64, i64, i64, i64, need],
+            "tq_causal_conv_grad": [i32, i64, i64, i64, i64, *steps, vp, vp, vp, vp, i32, *steps, vp, *steps, vp, vp, vp, vp,
+                                    sz, vp],
         }
         for name, args in protos.items():
             f = getattr(L, name)
@@ -141,3 +145,60 @@ def selective_scan_grad(x, dt, A, B, C, states, dy, skip=None, z=None, dt_bias=N
     _call((_lib or lib()).tq_selective_scan_grad, *sizes, *args, sp, lp, *dys, dhp, *dxs, *ddts, *dzs, *dBs, *dCs,
           dA.data_ptr(), _ptr(dskip), _ptr(dbias), dh0.data_ptr(), _ptr(ws), n, _raw_stream(dev))
     return SelectiveGrads(dx, ddt, dA, dB, dC, dskip, dz, dbias, dh0)
+
+
+# --------------------------------------------------------- causal convolution
+
+def _conv_args(x, weight, bias, state, lengths, silu):
+    code, dev = _typed(x, "x")
+    if x.dim() != 3:
+        raise ValueError("x must be a [B, T, D] tensor")
+    N, T, D = shape = x.shape
+    dtype = x.dtype
+    wp = _dense(weight, "weight", dtype)
+    if weight.dim() != 2 or weight.shape[1] != D:
+        raise ValueError(f"weight must have shape [K, {D}], got {tuple(weight.shape)}")
+    K = weight.shape[0]
+    return dev, (code, N, T, D, K), (*_steps(x, "x", None, shape), wp, _dense(bias, "bias", dtype, shape[2:]),
+                                     _dense(state, "state", dtype, (N, K - 1, D)),
+                                     _dense(lengths, "lengths", torch.int32, shape[:1]), bool(silu))
+
+
+@_on_stream
+def causal_conv(x, weight, bias=None, state=None, lengths=None, silu=True, y=None, last=None):
+    """The causal convolution (tq_causal_conv) over the steps of x [B, T, D] with
+    weight [K, D] and bias [D], followed by silu if wanted; state [B, K - 1, D]
+    holds the inputs before the first step (None: zeros).  Returns (y, last), the
+    latter the inputs before the next step; it may be the state tensor: records
+    are then extended in place."""
+    dev, sizes, args = _conv_args(x, weight, bias, state, lengths, silu)
+    _, N, _, D, K = sizes
+    y, ys = _steps_out(y, "y", x)
+    if last is None:
+        last = x.new_empty((N, max(K - 1, 0), D))
+    _call((_lib or lib()).tq_causal_conv, *sizes, *args, *ys, _dense(last, "last", x.dtype, (N, K - 1, D)),
+          _raw_stream(dev))
+    return y, last
+
+
+ConvGrads = collections.namedtuple("ConvGrads", "dx dweight dbias dstate")
+
+
+@_on_stream
+def causal_conv_grad(x, weight, dy, bias=None, state=None, dlast=None, lengths=None, silu=True, dx=None):
+    """The gradients of causal_conv (tq_causal_conv_grad) from those of its y and
+    last (None: zeros): ConvGrads, with None for dbias and dstate where bias and
+    state are None."""
+    dev, sizes, args = _conv_args(x, weight, bias, state, lengths, silu)
+    _, N, T, D, K = sizes
+    dys = _steps(dy, "dy", x.dtype, x.shape)
+    dp = _dense(dlast, "dlast", x.dtype, (N, K - 1, D))
+    dx, dxs = _steps_out(dx, "dx", x)
+    dweight = torch.empty_like(weight)
+    dbias = None if bias is None else torch.empty_like(bias)
+    dstate = None if state is None else torch.empty_like(state)
+    n = _need("tq_causal_conv_grad_workspace", N, T, D, K)
+    ws = _space(x, n)
+    _call((_lib or lib()).tq_causal_conv_grad, *sizes, *args, *dys, dp, *dxs, dweight.data_ptr(), _ptr(dbias),
+          _ptr(dstate), _ptr(ws), n, _raw_stream(dev))
+    return ConvGrads(dx, dweight, dbias, dstate)

@@ -112,3 +112,81 @@ def test_selective_scan_without_the_optional_inputs(ty, B, T, D, S):
     c.check_forward(y, h, h0=False)
     c.check_forward(*c.forward(h0=False), h0=False)
     c.check_grads(c.grads(states, dh=False), dh=False, h0=False)
+
+
+# --------------------------------------------------------- causal convolution
+
+class Conv:
+    def __init__(self, ty, B, T, D, K, ragged=True, bare=False):
+        self.dtype, self.u, self.tiny = TYPES[ty]
+        rng = np.random.default_rng(B + T + D + K)
+        self.n = rng.integers(0, T + 1, B) if ragged else None
+        if ragged and B > 2:
+            self.n[0], self.n[1], self.n[2] = 0, T, min(T, 1)
+        x, dy = rng.standard_normal((B, T, D + 1)), rng.standard_normal((B, T, D + 2))
+        if ragged:
+            x[np.arange(T) >= self.n[:, None]] = dy[np.arange(T) >= self.n[:, None]] = np.nan
+        x, xv = put(x, self.dtype)
+        dy, dyv = put(dy, self.dtype)
+        self.x, self.xv, self.dy, self.dyv = x[..., 1:], xv[..., 1:], dy[..., :D], dyv[..., :D]
+        self.w, self.wv = put(rng.standard_normal((K, D)), self.dtype)
+        self.bias, self.biasv = put(rng.standard_normal(D), self.dtype)
+        self.state, self.statev = put(rng.standard_normal((B, K - 1, D)), self.dtype)
+        self.dlast, self.dlastv = put(rng.standard_normal((B, K - 1, D)), self.dtype)
+        if bare:
+            self.bias = self.biasv = self.state = self.statev = self.dlast = self.dlastv = None
+        self.lengths = None if self.n is None else torch.as_tensor(self.n.astype(np.int32)).cuda()
+        self.more = dict(bias=self.bias, state=self.state, lengths=self.lengths)
+
+    def check(self, silu):
+        K, D = self.wv.shape
+        B, T = self.xv.shape[:2]
+        y, last = model.causal_conv(self.x, self.w, silu=silu, **self.more)
+        wy, wl, wu, um = ref.causal_conv(self.xv, self.wv, self.biasv, self.statev, self.n, silu)
+        # u: K products and sums; |silu'| <= 1.1; sigmoid: an exponential whose argument
+        # is rounded, a reciprocal, a product
+        extra = 1.1 * (K + 1) * U * um + ((8 + np.abs(wu)) * U * np.abs(wy) if silu else 0)
+        check("y", y, wy, rounded(wy, extra, self.u, self.tiny))
+        assert torch.equal(last.double().cpu(), torch.as_tensor(wl))
+        g = model.causal_conv_grad(self.x, self.w, self.dy, dlast=self.dlast, silu=silu, **self.more)
+        a = (self.xv, self.wv, self.biasv, self.statev, self.n, silu, self.dyv, self.dlastv)
+        want, size = ref.causal_conv_grad(*a), ref.causal_conv_grad(*a, absolute=True)
+        most = np.abs(wu).max(initial=0)
+        for name, w, m in zip(("dx", "dweight", "dbias", "dstate"), want, size):
+            got = getattr(g, name)
+            if got is None:
+                assert name in ("dbias", "dstate") and self.bias is None
+                continue
+            n = B * T if name in ("dweight", "dbias") else 0
+            check(name, got, w, rounded(w, (2 * K + 14 + 2 * most + n) * U * m, self.u, self.tiny))
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("B,T,D,K", [(1, 1, 1, 4), (5, 1, 200, 4), (3, 5, 7, 2), (4, 9, 8, 3), (4, 40, 13, 4), (2, 70, 331, 8),
+                                     (5, 130, 33, 5), (3, 64, 64, 1), (9, 3, 20, 6), (3, 77, 40, 7), (3, 0, 6, 4)])
+def test_causal_conv_and_gradients(ty, B, T, D, K):
+    c = Conv(ty, B, T, D, K)
+    c.check(True)
+    c.check(False)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("B,T,D,K", [(2, 33, 21, 4), (300, 20, 260, 3)])
+def test_causal_conv_without_the_optional_inputs(ty, B, T, D, K):
+    Conv(ty, B, T, D, K, ragged=False, bare=True).check(True)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("D", [3, 8, 75])
+def test_causal_conv_step_by_step_in_place(ty, D):
+    """Records extended by a few steps at a time, those that have ended staying
+    as they are."""
+    c = Conv(ty, 5, 12, D, 4)
+    whole, last = model.causal_conv(c.x, c.w, **c.more)
+    state, ys = c.state.clone(), []
+    for t0, t1 in ((0, 1), (1, 2), (2, 4), (4, 9), (9, 10), (10, 12)):
+        on = torch.clamp(c.lengths - t0, 0, t1 - t0).int()
+        y, s = model.causal_conv(c.x[:, t0:t1], c.w, bias=c.bias, state=state, lengths=on, last=state)
+        assert s is state
+        ys.append(y)
+    assert torch.equal(torch.cat(ys, 1), whole) and torch.equal(state, last)

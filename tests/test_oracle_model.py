@@ -44,3 +44,30 @@ def test_selective_scan_of_constant_steps():
     want = d * x * (1 - a ** np.arange(1, T + 1)) / (1 - a)
     np.testing.assert_allclose(y[0, :, 0], 2 * want, rtol=1e-12)
     np.testing.assert_allclose(h[0, 0, 0], want[-1], rtol=1e-12)
+
+
+@pytest.mark.parametrize("silu", [True, False])
+@pytest.mark.parametrize("K", [1, 2, 4])
+@pytest.mark.parametrize("lengths", [None, [6, 0, 1, 2]])
+def test_causal_conv_gradients_match_differences(K, lengths, silu):
+    rng = np.random.default_rng(K)
+    B, T, D = 4, 6, 2
+    x, dy = rng.standard_normal((2, B, T, D))
+    state, dlast = rng.standard_normal((2, B, K - 1, D))
+    names = ["x", "w", "bias", "state"]
+    args = dict(zip(names, (x, rng.standard_normal((K, D)), rng.standard_normal(D), state)))
+    n = None if lengths is None else np.array(lengths)
+    got = ref.causal_conv_grad(*args.values(), n, silu, dy, dlast)
+    for name, g in zip(names, got):
+        def both(v, name=name):
+            y, last = ref.causal_conv(**{**args, name: v}, lengths=n, silu=silu)[:2]
+            return np.concatenate([y.ravel(), last.ravel()])
+        np.testing.assert_allclose(g, differences(both, args[name], np.concatenate([dy.ravel(), dlast.ravel()])), **TOL,
+                                   err_msg=name)
+
+
+def test_causal_conv_is_a_convolution():
+    rng = np.random.default_rng(3)
+    x, w = rng.standard_normal((1, 20, 1)), rng.standard_normal((4, 1))
+    y = ref.causal_conv(x, w, None, None, None, False)[0]
+    np.testing.assert_allclose(y[0, :, 0], np.convolve(x[0, :, 0], w[::-1, 0])[:20], rtol=1e-12, atol=1e-14)
