@@ -6,7 +6,9 @@
  * A selective model of records mixes a few neighbouring steps of a record
  * (tq_causal_conv) and carries a state along it whose decay and whose input
  * depend on each step (tq_selective_scan); both advance by single steps where
- * records are extended.
+ * records are extended.  Its gradients are clipped together (tq_clip_grad_norm), and
+ * a beam search answers with the most likely records: tq_beam_select chooses the
+ * beams' continuations, tq_beam_reorder gathers the states that go with them.
  */
 #ifndef TQ_MODEL_H
 #define TQ_MODEL_H
@@ -97,6 +99,52 @@ tq_status tq_causal_conv_grad(int32_t type, int64_t B, int64_t T, int64_t D, int
                               const int32_t *lengths, int32_t silu, const void *dy, int64_t dy_batch, int64_t dy_step,
                               const void *dlast, void *dx, int64_t dx_batch, int64_t dx_step, void *dweight,
                               void *dbias, void *dstate, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The norm of n tensors together, and the tensors cut to a largest one: with
+ *     norm = scale (sum over all elements of grads[i]^2)^{1/2},
+ *     outs[i] = grads[i] scale (norm <= max_norm ? 1 : max_norm / norm).
+ * grads, outs, counts, types and out_types are HOST arrays of n entries, read
+ * during the call: device pointers, numbers of elements and tq_dtypes.  outs[i] may
+ * be grads[i] where both have one type.  Squares are summed in 64 bits; norm, float
+ * on the device, is written always.  An infinite norm gives zeros for finite
+ * elements and NaN for infinite ones, a norm of NaN gives NaN.  max_norm >= 0 (it may
+ * be infinite), scale > 0 and finite (1 over the factor that a loss was scaled by).
+ * TQ_E_UNSUPPORTED for n >= 2^20 or a tensor of 2^40 elements. */
+tq_status tq_clip_grad_norm_workspace(int64_t n, const int64_t *counts, size_t *bytes);
+tq_status tq_clip_grad_norm(int64_t n, const void *const *grads, const int64_t *counts, const int32_t *types,
+                            float max_norm, float scale, void *const *outs, const int32_t *out_types, float *norm,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/* One step of a beam search over R records with W beams each (1 <= W <= 64) and
+ * logits [R * W, V], rows ld_logits apart: a candidate is a beam w and the id v that
+ * it goes on with, its score
+ *     scores[r, w] + logits[r, w, v] - log sum_u exp logits[r, w, u],
+ * formed in 64 bits.  The K best (1 <= K <= 64, K <= W V) of a record's W V
+ * candidates are given, best first: out_scores float [R, K], parents int32 [R, K]
+ * (w) and tokens [R, K] (v).  Candidates of one beam rank by their logits, those of
+ * different beams by their scores; ties go to the lower beam, then the lower id.
+ *  - `last` [R, W] (NULL: no beam has ended) holds the beams' latest ids: a beam whose
+ *    latest id is `end` goes on with `end` at its present score and with nothing else;
+ *    its logits are not looked at.  end < V where last is given.
+ *  - A score that is not below infinity (NaN among them) counts as -infinity.  A beam
+ *    whose score is -infinity is out of use: at the start of a search all but one.
+ *    Candidates at -infinity, such as ids that a logit of -infinity rules out, are
+ *    given only where there are no others; they rank by beam and id, those of a
+ *    beam that has others by id behind these.
+ * TQ_E_UNSUPPORTED for W or K > 64 or R W ceil(V / 4096) >= 2^31. */
+tq_status tq_beam_select_workspace(int32_t type, int64_t R, int64_t W, int64_t V, int64_t K, size_t *bytes);
+tq_status tq_beam_select(int32_t type, int64_t R, int64_t W, int64_t V, int64_t K, const void *logits,
+                         int64_t ld_logits, const float *scores, const uint64_t *last, uint64_t end, float *out_scores,
+                         int32_t *parents, uint64_t *tokens, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The states of the beams that a search goes on with, n tensors in one call:
+ * outs[i][r, k] = ins[i][r, parents[r, k]] for rows of row_bytes[i] bytes, ins[i]
+ * [R, W] and outs[i] [R, K] of them; zeros where a parent is not in [0, W).  ins,
+ * outs and row_bytes are HOST arrays of n entries, read during the call; parents
+ * int32 [R, K] lies on the device.  TQ_E_UNSUPPORTED for n >= 2^20, R K >= 2^31,
+ * rows of 2^40 bytes or R K ceil(row_bytes / 8192) >= 2^33. */
+tq_status tq_beam_reorder(int64_t n, const void *const *ins, void *const *outs, const int64_t *row_bytes, int64_t R,
+                          int64_t W, int64_t K, const int32_t *parents, void *stream);
 
 #ifdef __cplusplus
 }

@@ -145,3 +145,33 @@ def causal_conv_grad(x, w, bias, state, lengths, silu, dy, dlast, absolute=False
             db += g
         ds[b], dx[b, :n[b]] = back[:K - 1], back[K - 1:]
     return dx, dw, db, ds
+
+
+def beam_candidates(logits, scores, last=None, end=None):
+    """The scores [R, W, V] of all candidates."""
+    with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+        top = logits.max(-1, keepdims=True)
+        top = np.where(np.isfinite(top), top, 0)
+        lse = np.log(np.exp(logits - top).sum(-1, keepdims=True)) + top
+        c = scores[..., None] + (logits - lse)
+    if last is not None:
+        on = last == end
+        c[on] = -np.inf
+        c[..., end] = np.where(on, scores, c[..., end])
+    return np.where(c < np.inf, c, -np.inf)
+
+
+def beam_select(logits, scores, K, last=None, end=None):
+    """scores, parents and tokens [R, K] of the best candidates, by plain sorting:
+    score, then beam, then logit, then id."""
+    R, W, V = logits.shape
+    c = beam_candidates(logits, scores, last, end)
+    out = [np.zeros((R, K)), np.zeros((R, K), int), np.zeros((R, K), int)]
+    beam, word = np.divmod(np.arange(W * V), V)
+    for r in range(R):
+        flat = c[r].ravel()
+        # where nothing but the id is left to tell candidates apart
+        logit = np.where(flat > -np.inf, logits[r].ravel(), 0)
+        order = np.lexsort((word, -logit, beam, -flat))[:K]
+        out[0][r], out[1][r], out[2][r] = flat[order], beam[order], word[order]
+    return out

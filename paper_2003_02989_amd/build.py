@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtq.so")
 SOURCES = ["kernels.hip", "program.cpp", "tq_abi.cpp", "jit.cpp",
            "seq_abi.cpp", "seq_embed.hip", "seq_scan.hip", "seq_norm.hip", "seq_xent.hip",
-           "model_abi.cpp", "model_scan.hip", "model_conv.hip"]
+           "model_abi.cpp", "model_scan.hip", "model_conv.hip", "model_clip.hip", "model_beam.hip"]
 # device code the run-time specialised kernels are compiled with, in order
 JIT_HEADERS = ["tq_internal.h", "kernel_args.h", "device_ops.h"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -50,4 +50,43 @@ size_t conv_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t K);
 hipError_t launch_conv(int32_t type, const ConvArgs &a, hipStream_t s);
 hipError_t launch_conv_grad(int32_t type, const ConvArgs &a, hipStream_t s);
 
+struct ClipArgs {
+    int64_t n;
+    // host arrays, read during the call
+    const void *const *in;
+    void *const *out;
+    const int64_t *counts;
+    const int32_t *types, *out_types;
+    float max_norm, scale;
+    float *norm;
+    void *ws;
+};
+size_t clip_workspace(int64_t n, const int64_t *counts);
+hipError_t launch_clip(const ClipArgs &a, hipStream_t s);
+
+struct BeamArgs {
+    int64_t R, W, V, K;
+    const void *logits;
+    int64_t ld;
+    const float *scores;
+    const uint64_t *last;
+    uint64_t end;
+    float *out_scores;
+    int32_t *parents;
+    uint64_t *tokens;
+    void *ws;
+};
+size_t beam_workspace(int32_t type, int64_t R, int64_t W, int64_t V, int64_t K);
+hipError_t launch_beam(int32_t type, const BeamArgs &a, hipStream_t s);
+
+struct ReorderArgs {
+    int64_t n, R, W, K;
+    // host arrays, read during the call
+    const void *const *in;
+    void *const *out;
+    const int64_t *bytes;  // of a beam's row
+    const int32_t *parents;
+};
+hipError_t launch_reorder(const ReorderArgs &a, hipStream_t s);
+
 } // namespace tq

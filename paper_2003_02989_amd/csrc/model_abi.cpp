@@ -1,6 +1,7 @@
 // model_abi.cpp -- the extern "C" entry points of tq_model.h: every argument is
 // checked here, on the host, before anything is enqueued.
 #include <algorithm>
+#include <cmath>
 
 #include "abi_checks.h"
 #include "model.h"
@@ -9,7 +10,7 @@ using namespace tq;
 
 namespace {
 
-constexpr int64_t kMaxStates = 64, kMaxTaps = 8;
+constexpr int64_t kMaxStates = 64, kMaxTaps = 8, kMaxBeams = 64;
 
 void check_select(const char *call, int type, int64_t B, int64_t T, int64_t D, int64_t S)
 {
@@ -48,6 +49,33 @@ void check_conv(const char *call, int type, int64_t B, int64_t T, int64_t D, int
     if (D > kMaxWidth) fail(TQ_E_UNSUPPORTED, text(call, "D must be at most 2^20"));
     if (conv_items(B, T, D) > kMaxIndex || conv_items(B, 1, D) > kMaxIndex)
         fail(TQ_E_UNSUPPORTED, text(call, "B * ceil(T / 8) * ceil(D / 4) must be below 2^31"));
+}
+
+void check_list(const char *call, int64_t n)
+{
+    if (n < 0) fail(TQ_E_INVALID, text(call, "n must not be negative"));
+    if (n >= 1 << 20) fail(TQ_E_UNSUPPORTED, text(call, "n must be below 2^20"));
+}
+
+void check_counts(const char *call, const char *name, int64_t n, const int64_t *counts)
+{
+    if (n && !counts) fail(TQ_E_INVALID, text(call, name) + " is NULL");
+    for (int64_t i = 0; i < n; i++) {
+        if (counts[i] < 0) fail(TQ_E_INVALID, text(call, name) + " must not be negative");
+        if (counts[i] >= (int64_t)1 << 40) fail(TQ_E_UNSUPPORTED, text(call, name) + " must be below 2^40");
+    }
+}
+
+void check_beam(const char *call, int type, int64_t R, int64_t W, int64_t V, int64_t K)
+{
+    check_type(call, type);
+    check_size(call, "R", R);
+    check_size(call, "V", V);
+    if (W < 1 || K < 1 || V < 1) fail(TQ_E_INVALID, text(call, "W, V and K must be positive"));
+    if (W > kMaxBeams || K > kMaxBeams) fail(TQ_E_UNSUPPORTED, text(call, "W and K must be at most 64"));
+    if (K > W * V) fail(TQ_E_INVALID, text(call, "there are fewer than K candidates"));
+    if ((double)R * (double)W * (double)((V + 4095) / 4096) > kMaxIndex)
+        fail(TQ_E_UNSUPPORTED, text(call, "R * W * ceil(V / 4096) must be below 2^31"));
 }
 
 } // namespace
@@ -228,6 +256,102 @@ tq_status tq_causal_conv_grad(int32_t type, int64_t B, int64_t T, int64_t D, int
         a.weight = weight, a.bias = bias, a.state = state, a.lengths = lengths, a.silu = silu != 0, a.dlast = dlast;
         a.dweight = dweight, a.dbias = dbias, a.dstate = dstate, a.ws = workspace;
         hip_check(launch_conv_grad(type, a, as_stream(stream)), "causal convolution gradient launch");
+    });
+}
+
+tq_status tq_clip_grad_norm_workspace(int64_t n, const int64_t *counts, size_t *bytes)
+{
+    return guarded([&] {
+        const char *call = "clip_grad_norm_workspace";
+        check_list(call, n);
+        check_counts(call, "counts", n, counts);
+        give(bytes, clip_workspace(n, counts));
+    });
+}
+
+tq_status tq_clip_grad_norm(int64_t n, const void *const *grads, const int64_t *counts, const int32_t *types,
+                            float max_norm, float scale, void *const *outs, const int32_t *out_types, float *norm,
+                            void *workspace, size_t workspace_bytes, void *stream)
+{
+    return guarded([&] {
+        const char *call = "clip_grad_norm";
+        check_list(call, n);
+        check_counts(call, "counts", n, counts);
+        if (!(max_norm >= 0.f)) fail(TQ_E_INVALID, text(call, "max_norm must not be negative"));
+        if (!(scale > 0.f && std::isfinite(scale))) fail(TQ_E_INVALID, text(call, "scale must be positive and finite"));
+        if (n && (!grads || !types || !outs || !out_types)) fail(TQ_E_INVALID, text(call, "a list is NULL"));
+        for (int64_t i = 0; i < n; i++) {
+            check_type(call, types[i]);
+            check_type(call, out_types[i]);
+            if (counts[i] == 0) continue;
+            check_array(call, "grads", grads[i], size_of(types[i]));
+            check_array(call, "outs", outs[i], size_of(out_types[i]));
+            if (grads[i] == outs[i] && types[i] != out_types[i])
+                fail(TQ_E_INVALID, text(call, "a tensor in place keeps its type"));
+        }
+        check_array(call, "norm", norm, 4);
+        check_space(call, workspace, workspace_bytes, clip_workspace(n, counts));
+        hip_check(launch_clip({n, grads, outs, counts, types, out_types, max_norm, scale, norm, workspace},
+                              as_stream(stream)),
+                  "gradient clipping launch");
+    });
+}
+
+tq_status tq_beam_select_workspace(int32_t type, int64_t R, int64_t W, int64_t V, int64_t K, size_t *bytes)
+{
+    return guarded([&] {
+        check_beam("beam_select_workspace", type, R, W, V, K);
+        give(bytes, beam_workspace(type, R, W, V, K));
+    });
+}
+
+tq_status tq_beam_select(int32_t type, int64_t R, int64_t W, int64_t V, int64_t K, const void *logits,
+                         int64_t ld_logits, const float *scores, const uint64_t *last, uint64_t end, float *out_scores,
+                         int32_t *parents, uint64_t *tokens, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return guarded([&] {
+        const char *call = "beam_select";
+        check_beam(call, type, R, W, V, K);
+        if (R == 0) return;
+        check_ld(call, "ld_logits", ld_logits, V);
+        check_array(call, "logits", logits, size_of(type));
+        check_array(call, "scores", scores, 4);
+        check_maybe("last", last, 8);
+        if (last && end >= (uint64_t)V) fail(TQ_E_INVALID, text(call, "end must be an id below V"));
+        check_array(call, "out_scores", out_scores, 4);
+        check_array(call, "parents", parents, 4);
+        check_array(call, "tokens", tokens, 8);
+        check_space(call, workspace, workspace_bytes, beam_workspace(type, R, W, V, K));
+        BeamArgs a{};
+        a.R = R, a.W = W, a.V = V, a.K = K, a.logits = logits, a.ld = ld_logits, a.scores = scores, a.last = last;
+        a.end = end, a.out_scores = out_scores, a.parents = parents, a.tokens = tokens, a.ws = workspace;
+        hip_check(launch_beam(type, a, as_stream(stream)), "beam selection launch");
+    });
+}
+
+tq_status tq_beam_reorder(int64_t n, const void *const *ins, void *const *outs, const int64_t *row_bytes, int64_t R,
+                          int64_t W, int64_t K, const int32_t *parents, void *stream)
+{
+    return guarded([&] {
+        const char *call = "beam_reorder";
+        check_list(call, n);
+        check_counts(call, "row_bytes", n, row_bytes);
+        check_size(call, "R", R);
+        check_size(call, "W", W);
+        check_size(call, "K", K);
+        if ((double)R * (double)K > kMaxIndex) fail(TQ_E_UNSUPPORTED, text(call, "R * K must be below 2^31"));
+        if (n == 0 || R == 0 || K == 0) return;
+        if (!ins || !outs) fail(TQ_E_INVALID, text(call, "a list is NULL"));
+        for (int64_t i = 0; i < n; i++) {
+            if (row_bytes[i] == 0) continue;
+            if ((double)R * (double)K * (double)((row_bytes[i] + 8191) / 8192) >= (double)((int64_t)1 << 33))
+                fail(TQ_E_UNSUPPORTED, text(call, "R * K * ceil(row_bytes / 8192) must be below 2^33"));
+            if (W) check_array(call, "ins", ins[i], 1);
+            check_array(call, "outs", outs[i], 1);
+            if (ins[i] == outs[i]) fail(TQ_E_INVALID, text(call, "rows are not reordered in place"));
+        }
+        check_array(call, "parents", parents, 4);
+        hip_check(launch_reorder({n, R, W, K, ins, outs, row_bytes, parents}, as_stream(stream)), "beam reorder launch");
     });
 }
 

@@ -2,17 +2,19 @@
 (include/tq_model.h): argument marshalling only.
 
 Beside the sequence operators (seq.py), whose conventions hold here too: what a
-selective model of measurement records runs over the steps of a record.
+selective model of measurement records runs over the steps of a record, how its
+gradients are clipped and how a beam search answers with it.
 Tensors live on the current HIP device; outputs and workspaces that the caller
 does not give come from torch's allocator for the stream the call runs on.
 """
 import collections
 import ctypes
+import math
 
 import torch
 
 from . import tq
-from .seq import _call, _dense, _on_stream, _ptr, _raw_stream, _space, _steps, _steps_out, _tensor, _typed
+from .seq import _TYPES, _call, _dense, _on_stream, _ptr, _raw_stream, _rows, _space, _steps, _steps_out, _tensor, _typed
 
 STATES_PIECE = 16  # TQ_STATES_PIECE: steps per state that selective_scan keeps for its gradient
 
@@ -24,7 +26,7 @@ def lib():
     global _lib
     if _lib is None:
         L = tq.lib()
-        vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        vp, i32, i64, sz, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
         need = ctypes.POINTER(sz)
         steps = [vp, i64, i64]
         protos = {
@@ -38,6 +40,11 @@ def lib():
             "tq_causal_conv_grad_workspace": [i64, i64, i64, i64, need],
             "tq_causal_conv_grad": [i32, i64, i64, i64, i64, *steps, vp, vp, vp, vp, i32, *steps, vp, *steps, vp, vp, vp, vp,
                                     sz, vp],
+            "tq_clip_grad_norm_workspace": [i64, vp, need],
+            "tq_clip_grad_norm": [i64, vp, vp, vp, f32, f32, vp, vp, vp, vp, sz, vp],
+            "tq_beam_select_workspace": [i32, i64, i64, i64, i64, need],
+            "tq_beam_select": [i32, i64, i64, i64, i64, vp, i64, vp, vp, ctypes.c_uint64, vp, vp, vp, vp, sz, vp],
+            "tq_beam_reorder": [i64, vp, vp, vp, i64, i64, i64, vp, vp],
         }
         for name, args in protos.items():
             f = getattr(L, name)
@@ -202,3 +209,106 @@ def causal_conv_grad(x, weight, dy, bias=None, state=None, dlast=None, lengths=N
     _call((_lib or lib()).tq_causal_conv_grad, *sizes, *args, *dys, dp, *dxs, dweight.data_ptr(), _ptr(dbias),
           _ptr(dstate), _ptr(ws), n, _raw_stream(dev))
     return ConvGrads(dx, dweight, dbias, dstate)
+
+
+# ----------------------------------------------------------- gradient clipping
+
+def _list(kind, values):
+    return (kind * len(values))(*values)
+
+
+@_on_stream
+def clip_grad_norm(grads, max_norm, scale=1.0, out=None):
+    """(norm, outputs): the norm of all tensors of the list `grads` together, a
+    float32 scalar on the device, times `scale`, and the tensors times scale, cut
+    to max_norm where the norm is above it (tq_clip_grad_norm).  The outputs are
+    the contiguous gradients themselves, or the tensors of the list `out`, of their
+    shapes and any of the types."""
+    grads = list(grads)
+    outs = grads if out is None else list(out)
+    if len(outs) != len(grads):
+        raise ValueError(f"out must be a list of {len(grads)} tensors, got {len(outs)}")
+    if not grads:
+        raise ValueError("grads must hold one tensor at least")
+    n = len(grads)
+    ptrs, codes = [_dense(t, "grads", None) for t in grads], [_TYPES.get(t.dtype) for t in grads]
+    dev = grads[0].get_device()
+    if out is None:
+        out_ptrs, out_codes = ptrs, codes
+    else:
+        out_ptrs = [_dense(o, "out", None, g.shape) for o, g in zip(outs, grads)]
+        out_codes = [_TYPES.get(o.dtype) for o in outs]
+    if None in codes or None in out_codes:
+        raise TypeError("gradients must be float32, bfloat16 or float16")
+    counts = _list(ctypes.c_int64, [t.numel() for t in grads])
+    norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
+    need = ctypes.c_size_t()
+    L = _lib or lib()
+    _call(L.tq_clip_grad_norm_workspace, n, counts, ctypes.byref(need))
+    ws = _space(norm, need.value)
+    _call(L.tq_clip_grad_norm, n, _list(ctypes.c_void_p, ptrs), counts, _list(ctypes.c_int32, codes), max_norm, scale,
+          _list(ctypes.c_void_p, out_ptrs), _list(ctypes.c_int32, out_codes), norm.data_ptr(), _ptr(ws), need.value,
+          _raw_stream(dev))
+    return norm, outs
+
+
+# ----------------------------------------------------------------- beam search
+
+@_on_stream
+def beam_select(logits, scores, beams=None, last=None, end=-1):
+    """One step of a beam search (tq_beam_select): the best `beams` (None: as many
+    as there are) continuations of the beams of each record, from logits [R, W, V]
+    and scores float32 [R, W].  last int64 [R, W], the beams' latest ids: those that
+    are `end` go on as they are (None: no beam has ended).  Returns (scores float32,
+    parents int32, tokens int64), each [R, beams], best first: beam `parents` goes
+    on with id `tokens`."""
+    code, dev = _typed(logits, "logits")
+    if logits.dim() != 3:
+        raise ValueError("logits must be a [R, W, V] tensor")
+    zp, ld = _rows(logits, "logits")
+    R, W, V = logits.shape
+    K = W if beams is None else beams
+    sp = _dense(scores, "scores", torch.float32, (R, W))
+    lp = _dense(last, "last", torch.int64, (R, W))
+    shape = (R, max(K, 0))
+    best = torch.empty(shape, dtype=torch.float32, device=logits.device)
+    parents = torch.empty(shape, dtype=torch.int32, device=logits.device)
+    tokens = torch.empty(shape, dtype=torch.int64, device=logits.device)
+    n = _need("tq_beam_select_workspace", code, R, W, V, K)
+    ws = _space(logits, n)
+    _call((_lib or lib()).tq_beam_select, code, R, W, V, K, zp, ld, sp, lp, end & 0xffffffffffffffff, best.data_ptr(),
+          parents.data_ptr(), tokens.data_ptr(), _ptr(ws), n, _raw_stream(dev))
+    return best, parents, tokens
+
+
+@_on_stream
+def beam_reorder(states, parents, out=None):
+    """The states that go with beam_select's choice (tq_beam_reorder): for every
+    tensor [R, W, ...] of the list `states`, of any type, the rows
+    states[i][r, parents[r, k]] as a tensor [R, K, ...], new or that of the list
+    `out`; zeros where a parent is not one of the W."""
+    states = list(states)
+    pp = _dense(parents, "parents", torch.int32)
+    if parents.dim() != 2:
+        raise ValueError("parents must be a [R, K] tensor")
+    R, K = parents.shape
+    for t in states:
+        _tensor(t, "states")
+        if t.dim() < 2 or t.shape[0] != R:
+            raise ValueError(f"states must have shape [{R}, W, ...], got {tuple(t.shape)}")
+        if t.shape[1] != states[0].shape[1]:
+            raise ValueError("states must have one number of beams")
+    if out is None:
+        out = [t.new_empty((R, K) + t.shape[2:]) for t in states]
+    out = list(out)
+    if len(out) != len(states):
+        raise ValueError(f"out must be a list of {len(states)} tensors, got {len(out)}")
+    if not states:
+        return out
+    W = states[0].shape[1]
+    ins = [_dense(t, "states", None) for t in states]
+    outs = [_dense(o, "out", t.dtype, (R, K) + t.shape[2:]) for o, t in zip(out, states)]
+    rows = [math.prod(t.shape[2:]) * t.element_size() for t in states]
+    _call((_lib or lib()).tq_beam_reorder, len(states), _list(ctypes.c_void_p, ins), _list(ctypes.c_void_p, outs),
+          _list(ctypes.c_int64, rows), R, W, K, pp, _raw_stream(parents.get_device()))
+    return out

@@ -190,3 +190,140 @@ def test_causal_conv_step_by_step_in_place(ty, D):
         assert s is state
         ys.append(y)
     assert torch.equal(torch.cat(ys, 1), whole) and torch.equal(state, last)
+
+
+# ----------------------------------------------------------- gradient clipping
+
+CLIPS = [[(5,)], [(17, 64), (3, 2, 5), (0,), (1,), ()], [(300, 300), (7,)], [(2048,), (2047,), (2049,), (4096, 33)],
+         [(k % 7, 3) for k in range(230)], [(257, 129)] * 130]
+
+
+@pytest.mark.parametrize("max_norm,scale", [(1.0, 1.0), (1e9, 1.0), (0.5, 1 / 1024), (float("inf"), 0.25), (0.0, 1.0)])
+@pytest.mark.parametrize("shapes", CLIPS)
+def test_clip_grad_norm(shapes, max_norm, scale):
+    rng = np.random.default_rng(len(shapes))
+    kinds = list(TYPES.values())
+    grads, values, outs, kept = [], [], [], []
+    for k, shape in enumerate(shapes):
+        g, v = put(2 * rng.standard_normal(shape), kinds[k % 3][0])
+        grads.append(g)
+        values.append(v)
+        kept.append(kinds[k // 3 % 3])
+        outs.append(torch.full(g.shape, 9.0, dtype=kept[-1][0], device="cuda"))
+    before = [g.clone() for g in grads]
+    norm, got = model.clip_grad_norm(grads, max_norm, scale=scale, out=outs)
+    assert all(a is b for a, b in zip(got, outs)) and all(torch.equal(a, b) for a, b in zip(grads, before))
+    scale = float(np.float32(scale))
+    want = scale * np.sqrt(sum((v ** 2).sum() for v in values))
+    assert norm.shape == () and abs(float(norm) - want) <= U * want
+    c = scale * (1 if want <= max_norm else max_norm / want)
+    # the factor is rounded to fp32, then the product to fp32 and to the output's type
+    for o, v, (_, u, tiny) in zip(got, values, kept):
+        check("output", o, v * c, rounded(v * c, 2.1 * U * np.abs(v * c), u, tiny))
+    norm2, got2 = model.clip_grad_norm(grads, max_norm, scale=scale)
+    assert torch.equal(norm, norm2) and all(a is b for a, b in zip(got2, grads))
+    for o, v, (_, u, tiny) in zip(got2, values, (kinds[k % 3] for k in range(len(shapes)))):
+        check("in place", o, v * c, rounded(v * c, 2.1 * U * np.abs(v * c), u, tiny))
+
+
+@pytest.mark.parametrize("n", [1000, 300000])
+def test_clip_grad_norm_of_large_and_unbounded_values(n):
+    g = torch.full((n,), 1e30, device="cuda")
+    norm, (o,) = model.clip_grad_norm([g], 1.0, out=[torch.empty_like(g)])
+    want = 1e30 * n ** 0.5
+    assert abs(float(norm) - want) <= 1e-6 * want  # 1e30 in fp32 and a square root
+    assert torch.allclose(o, torch.full_like(o, n ** -0.5), rtol=1e-6, atol=0)
+    g[7] = float("inf")
+    norm, (o,) = model.clip_grad_norm([g], 1.0, out=[torch.empty_like(g)])
+    assert float(norm) == float("inf") and torch.isnan(o[7]) and int((o != 0).sum()) == 1
+    g[7] = float("nan")
+    norm, (o,) = model.clip_grad_norm([g], 1.0, out=[torch.empty_like(g)])
+    assert torch.isnan(norm) and torch.isnan(o).all()
+
+
+# ----------------------------------------------------------------- beam search
+
+def beam_check(z, zv, scores, K, last=None, end=None):
+    s, p, t = model.beam_select(z, torch.as_tensor(scores).float().cuda(), beams=K,
+                                last=None if last is None else torch.as_tensor(last).cuda(), end=-1 if end is None else end)
+    ws, wp, wt = ref.beam_select(zv, scores, K, last, end)
+    assert torch.equal(p.cpu(), torch.as_tensor(wp).int()) and torch.equal(t.cpu(), torch.as_tensor(wt))
+    # 64-bit scores, rounded once; the oracle's own are off by some 1e-14
+    np.testing.assert_allclose(s.double().cpu().numpy(), ws, rtol=1.01 * U, atol=1e-300)
+
+
+BEAMS = [(1, 1, 1, 1), (16, 4, 17, 4), (3, 2, 5, 10), (2, 5, 100, 7), (2, 8, 5000, 8), (3, 3, 8191, 16), (2, 4, 8193, 5),
+         (1, 3, 65537, 64), (2, 64, 257, 64), (1, 40, 9000, 33), (3, 1, 30000, 20), (5, 9, 4096, 9), (4, 64, 1, 64),
+         (2, 12, 4097, 1)]
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("R,W,V,K", BEAMS)
+def test_beam_select(ty, R, W, V, K):
+    """Ids and beams are the oracle's; 16-bit logits have many ties."""
+    rng = np.random.default_rng(R + W + V + K)
+    z, zv = put(2 * rng.standard_normal((R, W, V + 3)), TYPES[ty][0])
+    z, zv = z[..., :V], zv[..., :V]
+    scores = np.float32(-20 + rng.standard_normal((R, W)))
+    beam_check(z, zv, scores, K)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("R,W,V,K", [(6, 4, 17, 4), (5, 8, 9001, 8), (3, 64, 33, 64), (4, 3, 20000, 40)])
+def test_beam_select_ended_masked_and_unused_beams(ty, R, W, V, K):
+    rng = np.random.default_rng(R + W + V)
+    zv = 2 * rng.standard_normal((R, W, V))
+    zv[:, :, rng.random(V) < 0.3] = -np.inf
+    zv[0] = -np.inf           # nothing can follow
+    zv[1, 0, 1:] = -np.inf    # one id can
+    zv[1, 0, 0] = 0.25
+    zv[2, 0] = 0.5            # all alike
+    zv[2, 1, 3] = np.nan
+    zv[2, 2, 5] = np.inf
+    z, zv = put(zv, TYPES[ty][0])
+    scores = np.float32(-20 + rng.standard_normal((R, W)))
+    scores[1, 1:] = -np.inf   # a search that begins
+    scores[-1, 0], scores[-1, 1] = np.nan, np.inf
+    end = V // 2
+    last = rng.integers(0, V, (R, W))
+    last[rng.random((R, W)) < 0.4] = end
+    last[1] = 0
+    z[last == end] = float("nan")  # not looked at
+    zv = np.where((last == end)[..., None], 0.0, zv)
+    beam_check(z, zv, scores, K, last, end)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("V", [300, 70000])
+@pytest.mark.parametrize("kind", ["rising", "falling", "equal", "periodic", "zeros"])
+def test_beam_select_of_ordered_logits(ty, V, kind):
+    """Orders in which the best come last, first or in one lane."""
+    i = np.arange(V)
+    zv = {"rising": i / V, "falling": -i / V, "equal": np.full(V, 1.5), "periodic": (i % 512 == 77) * 5.0 + (i % 8 == 5),
+          "zeros": np.where(i % 3, 0.0, -0.0)}[kind]
+    z, zv = put(np.stack([zv, zv])[None].repeat(2, 0), TYPES[ty][0])
+    beam_check(z, zv, np.float32([[-1, -1.5], [-2, -2]]), 24)
+
+
+def test_beam_select_tells_close_scores_apart():
+    """Beams whose best candidates differ by less than fp32 resolves."""
+    rng = np.random.default_rng(4)
+    z, zv = put(rng.standard_normal((200, 16, 33)), torch.float32)
+    scores = np.float32(np.log(rng.random((200, 16))) * 1e-6 - 100)
+    beam_check(z, zv, scores, 16)
+
+
+@pytest.mark.parametrize("R,W,K", [(1, 1, 1), (7, 3, 5), (40, 8, 8), (3, 2, 0), (0, 4, 4)])
+def test_beam_reorder(R, W, K):
+    rng = np.random.default_rng(R + W + K)
+    shapes = [(5,), (), (16,), (3, 75), (64, 16), (2048,), (2049,), (4, 1031), (0, 3)] + [(k, 2) for k in range(1, 120)]
+    kinds = [torch.float32, torch.bfloat16, torch.float16, torch.int64, torch.uint8]
+    states = [torch.as_tensor(rng.integers(0, 100, (R, W) + s)).to(kinds[k % 5]).cuda() for k, s in enumerate(shapes)]
+    parents = torch.as_tensor(rng.integers(-1, W + 1, (R, K)).astype(np.int32)).cuda()
+    at = parents.long().clamp(0, W - 1)
+    good = (parents >= 0) & (parents < W)
+    row = torch.arange(R, device="cuda")[:, None]
+    for got, s in zip(model.beam_reorder(states, parents), states):
+        want = s[row, at]
+        want[~good] = 0
+        assert torch.equal(got, want)
