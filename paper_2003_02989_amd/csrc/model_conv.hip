@@ -17,9 +17,8 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "model.h"
+#include "model_device.h"
 #include "seq.h"
-#include "seq_device.h"
 
 namespace tq {
 namespace {
@@ -34,14 +33,6 @@ struct Geom {
     int64_t run;      // steps of a run, whole batches
     float *part;      // [rows][K + 1][D]
 };
-
-__device__ __forceinline__ float silu_slope(float u, float &y)
-{
-    const float e = expf(-fabsf(u)), r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
-    const float s = u >= 0.f ? r : er, c = u >= 0.f ? er : r;  // sigmoid(u), sigmoid(-u)
-    y = u * s;
-    return s * fmaf(u, c, 1.f);
-}
 
 // A thread's piece of a row: the last one ends with the row, the elements that it
 // shares with the one before belong to that.
@@ -143,7 +134,7 @@ template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv(C
                 float u = bias[j];
 #pragma unroll
                 for (int k = 0; k < K; k++) u = fmaf(w[k][j], x[i + k][j], u);
-                y[j] = a.silu ? u * __builtin_amdgcn_rcpf(1.f + expf(-u)) : u;
+                y[j] = a.silu ? u * sigmoid<T>(u) : u;
             }
             at.store(row_of<T>(a.y, b, t + i), y);
         }
@@ -221,10 +212,11 @@ template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv_g
                 for (int j = 0; j < V; j++) {
                     float &d = q[K - 1 + i][j];
                     if (a.silu) {
-                        float u = bias[j], y;
+                        float u = bias[j], s, c;
 #pragma unroll
                         for (int k = 0; k < K; k++) u = fmaf(w[k][j], x[i + k][j], u);
-                        d *= silu_slope(u, y);
+                        sigmoids<T>(u, s, c);
+                        d *= s * fmaf(u, c, 1.f);
                     }
                     if (!there) d = 0.f;
                     if (mine) {
