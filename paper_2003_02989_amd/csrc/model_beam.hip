@@ -13,12 +13,13 @@
 // that few elements are looked at again to be entered in the list of the K best,
 // which the lanes hold in order, one each.  Lists are of keys that no two elements
 // share: a value's bits in the order of values, then the id, lower ids first.
-// A second kernel joins a beam's segments and then the beams: a candidate's place is
-// the number of candidates before it, counted by binary search in every beam's list.
+// A second kernel joins a beam's segments and then the beams, whose lists it takes from
+// the front.
 // Where a beam is one segment, one kernel does both.
 //
 // Reordering the states is a copy of rows of any number of tensors in one launch.
 #include <algorithm>
+#include <type_traits>
 
 #include "model.h"
 #include "seq.h"
@@ -28,8 +29,9 @@ namespace tq {
 namespace {
 
 using Key = unsigned long long;
-constexpr int kPieces = 16;  // of 16 bytes, a lane's part of a segment
-template <class T> constexpr int kSegment = 64 * kPieces * kVec<T>;
+constexpr int kPieces = 8;  // of 16 bytes, a lane's part of a segment
+constexpr int kFewPieces = 2;
+template <class T, int P> constexpr int kSegment = 64 * P * kVec<T>;
 constexpr double kNone = -__builtin_inf();
 
 struct Geom {
@@ -54,16 +56,13 @@ __device__ __forceinline__ float value_of(Key k)
 }
 __device__ __forceinline__ uint32_t id_of(Key k) { return ~(uint32_t)k; }
 
-// exp(x) for x <= 0 to about 2^-50: x = n ln 2 + r, the series of e^r to r^12.
-// Below -690 the result is that at -690, which no sum of ids shows.
+// exp(x) for -700 <= x <= 0 to about 2^-47: x = n ln 2 + r, the series of e^r to r^11.
+// (The rounding of ln 2 costs n 2^-55.)
 __device__ __forceinline__ double exp_below(double x)
 {
-    x = x < -690. ? -690. : x;
     const double magic = 0x1.8p52, t = fma(x, 1.4426950408889634, magic), n = t - magic;
-    double r = fma(n, -0x1.62e42fefa39efp-1, x);
-    r = fma(n, -0x1.abc9e3b39803fp-56, r);
-    double p = 1. / 479001600.;
-    p = fma(p, r, 1. / 39916800.);
+    const double r = fma(n, -0x1.62e42fefa39efp-1, x);
+    double p = 1. / 39916800.;
     p = fma(p, r, 1. / 3628800.);
     p = fma(p, r, 1. / 362880.);
     p = fma(p, r, 1. / 40320.);
@@ -76,9 +75,13 @@ __device__ __forceinline__ double exp_below(double x)
     p = fma(p, r, 1.);
     p = fma(p, r, 1.);
     const uint64_t b = __builtin_bit_cast(uint64_t, p);
-    const uint32_t hi = (uint32_t)(b >> 32) + (__builtin_bit_cast(uint64_t, t) << 20);
+    const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, t) << 20);
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)b);
 }
+constexpr float kFar = 690.f;  // what is further below a maximum counts as if it were not
+
+// The larger one, NaN where one is NaN.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 template <class V> __device__ __forceinline__ V wave_sum(V v)
 {
@@ -89,13 +92,19 @@ template <class V> __device__ __forceinline__ V wave_sum(V v)
 __device__ __forceinline__ float wave_max(float v)
 {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
+    for (int d = 32; d > 0; d >>= 1) v = larger(v, __shfl_xor(v, d, 64));
     return v;
 }
 __device__ __forceinline__ Key lane_key(Key k, int lane)
 {
     return (Key)__builtin_amdgcn_readlane((uint32_t)(k >> 32), lane) << 32 |
            (uint32_t)__builtin_amdgcn_readlane((uint32_t)k, lane);
+}
+
+// The number of the lane before.
+__device__ __forceinline__ uint32_t before(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x138, 0xf, 0xf, true);  // a shift by one over the whole wavefront
 }
 
 // A wavefront's list of the K best keys, lane i the i-th; zeros where there are fewer.
@@ -106,8 +115,13 @@ struct Best {
     __device__ __forceinline__ void enter(Key k)
     {
         const int lane = threadIdx.x & 63, at = __popcll(__ballot(mine > k));
-        const Key left = __shfl_up(mine, 1, 64);
+        const Key left = (Key)before((uint32_t)(mine >> 32)) << 32 | before((uint32_t)mine);
         mine = lane < at || lane >= K ? mine : lane == at ? k : left;
+        least = lane_key(mine, K - 1);
+    }
+    __device__ __forceinline__ void start(Key k)
+    {
+        mine = k;
         least = lane_key(mine, K - 1);
     }
     // the keys of all lanes that are better than the least so far
@@ -120,9 +134,42 @@ struct Best {
     }
 };
 
-// Part [from, to) of a beam's logits: their maximum, the sum of their exponentials
-// relative to it, and the K best.
-template <class T> struct Segment {
+// 16 bytes as they are read, so that elements of 16 bits stay two to a register.
+template <class T> struct Piece {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const T *p, int n)  // n: elements there are
+    {
+        constexpr int V = kVec<T>;
+        if (n >= V) {
+            __builtin_memcpy(w, p, sizeof w);
+            return;
+        }
+        T v[V];
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            v[j] = (T)(float)kNone;
+            if (j < n) v[j] = p[j];
+        }
+        __builtin_memcpy(w, v, sizeof w);
+    }
+    __device__ __forceinline__ float get(int j) const
+    {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[j]);
+        else {
+            const uint16_t u = (uint16_t)(w[j / 2] >> (j % 2 * 16));
+            return (float)__builtin_bit_cast(T, u);
+        }
+    }
+    // what was made of it is not kept in registers
+    __device__ __forceinline__ void forget()
+    {
+        asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
+    }
+};
+
+// Part [from, to) of a beam's logits, of P pieces a lane: their maximum (NaN where one
+// is), the sum of their exponentials relative to it, and the K best.
+template <class T, int P> struct Segment {
     static constexpr int V = kVec<T>;
     float top;
     double sum;
@@ -131,59 +178,60 @@ template <class T> struct Segment {
     {
         const int lane = threadIdx.x & 63;
         const int n = (int)(to - from);
-        T v[kPieces][V];
+        Piece<T> v[P];
 #pragma unroll
-        for (int p = 0; p < kPieces; p++) {
+        for (int p = 0; p < P; p++) {
             const int at = (p * 64 + lane) * V;
-#pragma unroll
-            for (int j = 0; j < V; j++) v[p][j] = (T)(float)kNone;
-            if (at + V <= n) __builtin_memcpy(v[p], row + from + at, sizeof v[p]);
-            else if (at < n)
-#pragma unroll
-                for (int j = 0; j < V; j++)
-                    if (at + j < n) v[p][j] = row[from + at + j];
+            v[p].load(row + from + at, n - at);
         }
-        float mine = (float)kNone;
+        float mine = (float)kNone, tops[P];
 #pragma unroll
-        for (int p = 0; p < kPieces; p++) {
+        for (int p = 0; p < P; p++) {
+            tops[p] = v[p].get(0);
 #pragma unroll
-            for (int j = 0; j < V; j++) mine = fmaxf(mine, (float)v[p][j]);
+            for (int j = 1; j < V; j++) tops[p] = larger(tops[p], v[p].get(j));
+            mine = larger(mine, tops[p]);
         }
         top = wave_max(mine);
-        // of a segment of -infinity: nothing
-        const double base = top == (float)kNone ? 0. : (double)top;
+#pragma unroll
+        for (int p = 0; p < P; p++) v[p].forget();
         sum = 0.;
+        if (fabsf(top) < (float)-kNone) {
+            const double base = (double)top;
+            const float far = top - kFar;
 #pragma unroll
-        for (int p = 0; p < kPieces; p++) {
-            if (p * 64 * V < n) {
-                double s = 0.;
+            for (int p = 0; p < P; p++)
+                if (p * 64 * V < n) {
+                    double s = 0.;
 #pragma unroll
-                for (int j = 0; j < V; j++) s += exp_below((double)(float)v[p][j] - base);
-                sum += s;
-            }
+                    for (int j = 0; j < V; j++) s += exp_below((double)fmaxf(v[p].get(j), far) - base);
+                    sum += s;
+                    v[p].forget();
+                }
+            sum = wave_sum(sum);
         }
-        if (top == (float)kNone) sum = sum == sum ? 0. : sum;
-        sum = wave_sum(sum);
-        // a value that K of the lanes reach
+        // a value that K of the lanes reach, its first bits
         uint32_t bound = 0;
         const uint32_t high = lane * V < n ? ordered(mine) : 0;
 #pragma unroll
-        for (int bit = 31; bit >= 0; bit--) {
+        for (int bit = 31; bit >= 12; bit--) {
             const uint32_t more = bound | 1u << bit;
             if (__popcll(__ballot(high >= more)) >= K) bound = more;
         }
         Best list(K);
+        float least = bound ? value_of((Key)bound << 32) : (float)kNone;
+        if (least != least) least = (float)kNone;  // first bits that no value has
 #pragma unroll
-        for (int p = 0; p < kPieces; p++) {
+        for (int p = 0; p < P; p++) {
             const int at = (p * 64 + lane) * V;
-            if (p * 64 * V < n) {
+            if (p * 64 * V < n && __ballot(tops[p] >= least)) {
 #pragma unroll
                 for (int j = 0; j < V; j++) {
-                    const uint32_t o = ordered((float)v[p][j]);
-                    const bool reaches = o >= bound && at + j < n;
+                    const float z = v[p].get(j);
+                    const bool reaches = z >= least && at + j < n;
                     if (__ballot(reaches)) {
-                        list.offer(reaches ? (Key)o << 32 | (uint32_t)~(uint32_t)(from + at + j) : 0);
-                        bound = max(bound, (uint32_t)(list.least >> 32));
+                        list.offer(reaches ? (Key)ordered(z) << 32 | (uint32_t)~(uint32_t)(from + at + j) : 0);
+                        if (list.least) least = fmaxf(least, value_of(list.least));
                     }
                 }
             }
@@ -192,15 +240,11 @@ template <class T> struct Segment {
     }
 };
 
-// A record's beams and their candidates in LDS, each beam's K in order.
+// The K best candidates of each of a record's beams in LDS, in order.
 struct Lists {
-    double *score;   // [W][K]
-    uint32_t *id;    // [W][K]
-    int *count;      // [W]
-    __device__ Lists(char *lds, int W, int K)
-        : score((double *)lds), id((uint32_t *)(score + W * K)), count((int *)(id + W * K))
-    {
-    }
+    double *score;  // [W][K]
+    uint32_t *id;
+    __device__ Lists(char *lds, int W, int K) : score((double *)lds), id((uint32_t *)(score + W * K)) {}
 };
 
 __device__ __forceinline__ bool over(const BeamArgs &a, int64_t row) { return a.last && a.last[row] == a.end; }
@@ -212,7 +256,8 @@ __device__ __forceinline__ void list_beam(const BeamArgs &a, const Lists &l, int
     const int lane = threadIdx.x & 63, K = (int)a.K, n = (int)min((int64_t)K, a.V);
     const double score = a.scores[row];
     const bool ended = over(a, row), finite = fabs(score) < __builtin_inf();
-    const double lse = ended ? 0. : (double)top + log(sum);
+    // of nothing but -infinity: -infinity; NaN and infinity have no sum
+    const double lse = ended ? 0. : (double)top + (fabsf(top) < __builtin_inff() ? log(sum) : 0.);
     double s = kNone;
     uint32_t id = (uint32_t)lane;
     if (finite && ended) {  // the end, then the others
@@ -227,40 +272,64 @@ __device__ __forceinline__ void list_beam(const BeamArgs &a, const Lists &l, int
         l.score[w * K + lane] = s;
         l.id[w * K + lane] = id;
     }
-    if (lane == 0) l.count[w] = n;
 }
 
-// The places of all candidates among each other.
-__device__ __forceinline__ void pick(const BeamArgs &a, const Lists &l, int64_t r, int threads)
+// The largest one of a wavefront.
+__device__ __forceinline__ uint32_t wave_most(uint32_t v)
 {
-    const int W = (int)a.W, K = (int)a.K;
-    for (int c = threadIdx.x; c < W * K; c += threads) {
-        const int w = c / K, k = c - w * K;
-        if (k >= l.count[w]) continue;
-        const double s = l.score[c];
-        int place = k;
-        for (int o = 0; o < W && place < K; o++) {
-            if (o == w) continue;
-            // those of beam o that are before: better, or as good in a lower beam
-            int lo = 0, hi = l.count[o];
-            while (lo < hi) {
-                const int m = (lo + hi) / 2;
-                const double t = l.score[o * K + m];
-                if (t > s || (t == s && o < w)) lo = m + 1;
-                else hi = m;
-            }
-            place += lo;
+    const auto moved = [](uint32_t v, auto ctrl, auto rows) {
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    };
+    using std::integral_constant;
+    const integral_constant<int, 0xf> all{};
+    v = max(v, moved(v, integral_constant<int, 0x111>{}, all));  // lanes 1, 2, 4, 8 before in a row of 16
+    v = max(v, moved(v, integral_constant<int, 0x112>{}, all));
+    v = max(v, moved(v, integral_constant<int, 0x114>{}, all));
+    v = max(v, moved(v, integral_constant<int, 0x118>{}, all));
+    v = max(v, moved(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{}));  // the row before
+    v = max(v, moved(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{}));  // both rows before
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
+// The K best of all beams' candidates: a wavefront takes the best of what the beams
+// have left, a lane each, K times; the lower beam where they are as good.
+__device__ __forceinline__ void pick(const BeamArgs &a, const Lists &l, int64_t r)
+{
+    const int W = (int)a.W, K = (int)a.K, n = (int)min((int64_t)K, a.V);  // candidates of a beam
+    const int w = threadIdx.x;
+    if (w >= 64) return;
+    int at = 0;
+    double s = 0.;
+    uint32_t hi = 0, lo = 0;  // the score's bits in the order of scores; 0: none left
+    const auto next = [&] {
+        hi = lo = 0;
+        if (w >= W || at >= n) return;
+        s = l.score[w * K + at];
+        const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.);
+        const uint64_t o = u ^ ((uint64_t)((int64_t)u >> 63) | (uint64_t)1 << 63);
+        hi = (uint32_t)(o >> 32);
+        lo = (uint32_t)o;
+    };
+    next();
+    for (int k = 0; k < K; k++) {
+        const uint32_t most = wave_most(hi);
+        unsigned long long best = __ballot(hi == most);
+        if (__popcll(best) > 1) {
+            const uint32_t rest = wave_most(hi == most ? lo : 0);  // (of all lanes)
+            best = __ballot(hi == most && lo == rest);
         }
-        if (place < K) {
-            a.out_scores[r * K + place] = (float)s;
-            a.parents[r * K + place] = w;
-            a.tokens[r * K + place] = l.id[c];
+        if (w == __builtin_ctzll(best)) {
+            a.out_scores[r * K + k] = (float)s;
+            a.parents[r * K + k] = w;
+            a.tokens[r * K + k] = l.id[w * K + at];
+            at++;
+            next();
         }
     }
 }
 
 constexpr int kRowThreads = 256;
-template <class T> __global__ __launch_bounds__(kRowThreads) void k_beam_rows(BeamArgs a, Geom g)
+template <class T> __global__ __launch_bounds__(kRowThreads, 4) void k_beam_rows(BeamArgs a, Geom g)
 {
     const uint32_t item = block_of() * (kRowThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= g.rows * g.segments) return;
@@ -268,7 +337,7 @@ template <class T> __global__ __launch_bounds__(kRowThreads) void k_beam_rows(Be
     const uint32_t row = item / g.segments;
     if (over(a, row)) return;
     const int64_t from = (item - row * g.segments) * g.length;
-    const Segment<T> s((const T *)a.logits + row * a.ld, from, min(from + g.length, a.V), (int)a.K);
+    const Segment<T, kPieces> s((const T *)a.logits + row * a.ld, from, min(from + g.length, a.V), (int)a.K);
     if (lane == 0) {
         g.tops[item] = s.top;
         g.sums[item] = s.sum;
@@ -276,41 +345,46 @@ template <class T> __global__ __launch_bounds__(kRowThreads) void k_beam_rows(Be
     if (lane < a.K) g.keys[(int64_t)item * a.K + lane] = s.best;
 }
 
-constexpr int kPickThreads = 256;
-__global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a, Geom g)
+__global__ __launch_bounds__(1024) void k_beam_pick(BeamArgs a, Geom g)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int64_t r = block_of();
     if (r >= a.R) return;
     const Lists l(lds, (int)a.W, (int)a.K);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    for (int w = wave; w < a.W; w += kPickThreads / 64) {
+    for (int w = wave; w < a.W; w += blockDim.x / 64) {
         const int64_t row = r * a.W + w;
         float top = (float)kNone;
         double sum = 0.;
         Best list((int)a.K);
         if (!over(a, row)) {
             const int64_t at = row * g.segments;
-            for (uint32_t i = lane; i < g.segments; i += 64) top = fmaxf(top, g.tops[at + i]);
+            for (uint32_t i = lane; i < g.segments; i += 64) top = larger(top, g.tops[at + i]);
             top = wave_max(top);
-            for (uint32_t i = lane; i < g.segments; i += 64) {
-                const float t = g.tops[at + i];
-                const double s = g.sums[at + i];
-                // a sum that is not a number stays so; a segment of nothing adds nothing
-                sum += s == 0. ? 0. : s * exp_below((double)t - (double)top);
-            }
+            if (fabsf(top) < __builtin_inff())
+                for (uint32_t i = lane; i < g.segments; i += 64)
+                    sum += g.sums[at + i] * exp_below((double)fmaxf(g.tops[at + i], top - kFar) - (double)top);
             sum = wave_sum(sum);
-            const int n = (int)(g.segments * (uint32_t)a.K);
-            for (int i = lane; i - lane < n; i += 64) list.offer(i < n ? g.keys[at * a.K + i] : 0);
+            // the first segment's list, and what the others have that is better
+            const int K = (int)a.K;
+            const int64_t n = (int64_t)g.segments * K;
+            const Key *keys = g.keys + at * K;
+            Key next = K + lane < n ? keys[K + lane] : 0;
+            list.start(lane < K ? keys[lane] : 0);
+            for (int64_t i = K; i < n; i += 64) {
+                const Key now = next;
+                if (i + 64 < n) next = i + 64 + lane < n ? keys[i + 64 + lane] : 0;
+                list.offer(now);
+            }
         }
         list_beam(a, l, w, row, list.mine, top, sum);
     }
     __syncthreads();
-    pick(a, l, r, kPickThreads);
+    pick(a, l, r);
 }
 
 // Beams of one segment.
-template <class T> __global__ __launch_bounds__(512) void k_beam_small(BeamArgs a)
+template <class T, int P> __global__ __launch_bounds__(512) void k_beam_small(BeamArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int64_t r = block_of();
@@ -323,16 +397,16 @@ template <class T> __global__ __launch_bounds__(512) void k_beam_small(BeamArgs 
             list_beam(a, l, w, row, 0, 0.f, 1.);
             continue;
         }
-        const Segment<T> s((const T *)a.logits + row * a.ld, 0, a.V, (int)a.K);
+        const Segment<T, P> s((const T *)a.logits + row * a.ld, 0, a.V, (int)a.K);
         list_beam(a, l, w, row, s.best, s.top, s.sum);
     }
     __syncthreads();
-    pick(a, l, r, (int)blockDim.x);
+    pick(a, l, r);
 }
 
-size_t lds_of(const BeamArgs &a) { return (size_t)a.W * ((size_t)a.K * 12 + 4); }
+size_t lds_of(const BeamArgs &a) { return (size_t)a.W * (size_t)a.K * 12; }
 
-int64_t segment_of(int32_t type) { return type == TQ_F32 ? kSegment<float> : kSegment<_Float16>; }
+int64_t segment_of(int32_t type) { return type == TQ_F32 ? kSegment<float, kPieces> : kSegment<_Float16, kPieces>; }
 
 size_t place(int32_t type, const BeamArgs &a, Geom &g)
 {
@@ -356,11 +430,12 @@ template <class T> hipError_t beam_t(int32_t type, const BeamArgs &a, hipStream_
     place(type, a, g);
     if (g.segments == 1) {
         const unsigned threads = 64 * (unsigned)std::min<int64_t>(a.W, 8);
-        k_beam_small<T><<<grid_of(a.R), threads, lds_of(a), s>>>(a);
+        if (a.V <= kSegment<T, kFewPieces>) k_beam_small<T, kFewPieces><<<grid_of(a.R), threads, lds_of(a), s>>>(a);
+        else k_beam_small<T, kPieces><<<grid_of(a.R), threads, lds_of(a), s>>>(a);
     } else {
         const int64_t waves = (int64_t)g.rows * g.segments, per = kRowThreads / 64;
         k_beam_rows<T><<<grid_of((waves + per - 1) / per), kRowThreads, 0, s>>>(a, g);
-        k_beam_pick<<<grid_of(a.R), kPickThreads, lds_of(a), s>>>(a, g);
+        k_beam_pick<<<grid_of(a.R), 64 * (unsigned)std::min<int64_t>(a.W, 16), lds_of(a), s>>>(a, g);
     }
     return hipGetLastError();
 }
