@@ -22,9 +22,7 @@ namespace tq {
 namespace {
 
 constexpr int kTensors = 100;          // of a launch: their places are kernel arguments
-constexpr int kLane = 4;               // elements of a lane's access
-constexpr int kSteps = 8;              // accesses of a chunk
-constexpr int kChunk = 64 * kLane * kSteps;
+constexpr int kChunk = 4096;           // elements: 8 accesses of 16 bytes a lane, 16 in fp32
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kBlocks = 1024;          // of a launch at most: 16 wavefronts per compute unit
 constexpr int kFew = 1024;             // threads of the only workgroup
@@ -69,24 +67,36 @@ __device__ __forceinline__ int tensor_of(const Tensors &t, uint32_t chunk)
     return lo;
 }
 
+// The sum of squares of up to a chunk.  Four sums a lane: what follows another addition
+// waits for it.
 template <class T> __device__ __forceinline__ double squares(const T *p, int64_t n)
 {
+    constexpr int V = kVec<T>, N = kChunk / (64 * V);
     const int lane = threadIdx.x & 63;
-    double s[kLane] = {};
+    double s[4] = {};
+    const auto add = [&](const T(&v)[V]) {
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            const double d = (double)(float)v[j];
+            s[j % 4] = fma(d, d, s[j % 4]);
+        }
+    };
     if (n >= kChunk) {
-        T v[kSteps][kLane];
+        T v[N][V];
 #pragma unroll
-        for (int k = 0; k < kSteps; k++) __builtin_memcpy(v[k], p + (k * 64 + lane) * kLane, sizeof v[k]);
+        for (int k = 0; k < N; k++) __builtin_memcpy(v[k], p + (k * 64 + lane) * V, sizeof v[k]);
 #pragma unroll
-        for (int k = 0; k < kSteps; k++)
-#pragma unroll
-            for (int j = 0; j < kLane; j++) {
-                const double d = (double)(float)v[k][j];
-                s[j] = fma(d, d, s[j]);
-            }
+        for (int k = 0; k < N; k++) add(v[k]);
     } else {
-        for (int64_t at = lane; at < n; at += 64) {
-            const double d = (double)(float)p[at];
+        const int whole = (int)n / V;
+#pragma unroll 4
+        for (int k = lane; k < whole; k += 64) {
+            T v[V];
+            __builtin_memcpy(v, p + k * V, sizeof v);
+            add(v);
+        }
+        if (lane < (int)n - whole * V) {
+            const double d = (double)(float)p[whole * V + lane];
             s[0] = fma(d, d, s[0]);
         }
     }
@@ -95,20 +105,30 @@ template <class T> __device__ __forceinline__ double squares(const T *p, int64_t
 
 template <class T, class O> __device__ __forceinline__ void scaled(const T *p, O *o, int64_t n, float c)
 {
+    constexpr int V = kVec<T>, N = kChunk / (64 * V);
     const int lane = threadIdx.x & 63;
+    const auto put = [&](int k, const T(&v)[V]) {
+        float f[V];
+#pragma unroll
+        for (int j = 0; j < V; j++) f[j] = (float)v[j] * c;
+        store_vec<V>(o + k * V, f);
+    };
     if (n >= kChunk) {
-        T v[kSteps][kLane];
+        T v[N][V];
 #pragma unroll
-        for (int k = 0; k < kSteps; k++) __builtin_memcpy(v[k], p + (k * 64 + lane) * kLane, sizeof v[k]);
+        for (int k = 0; k < N; k++) __builtin_memcpy(v[k], p + (k * 64 + lane) * V, sizeof v[k]);
 #pragma unroll
-        for (int k = 0; k < kSteps; k++) {
-            float f[kLane];
-#pragma unroll
-            for (int j = 0; j < kLane; j++) f[j] = (float)v[k][j] * c;
-            store_vec<kLane>(o + (k * 64 + lane) * kLane, f);
-        }
+        for (int k = 0; k < N; k++) put(k * 64 + lane, v[k]);
     } else {
-        for (int64_t at = lane; at < n; at += 64) o[at] = (O)((float)p[at] * c);
+        const int whole = (int)n / V;
+#pragma unroll 4
+        for (int k = lane; k < whole; k += 64) {
+            T v[V];
+            __builtin_memcpy(v, p + k * V, sizeof v);
+            put(k, v);
+        }
+        const int at = whole * V + lane;
+        if (at < (int)n) o[at] = (O)((float)p[at] * c);
     }
 }
 

@@ -4,9 +4,10 @@
 //
 // channel by channel, the K - 1 inputs before the first step being the record's
 // state.  Bound by memory: x is read and y written once.  A thread holds a piece of
-// a row (16 bytes; 4 elements for the gradient, which holds more per element) over
-// a run of steps, the last K - 1 inputs in registers, the reads of a batch of steps
-// on their way together.
+// a row (16 bytes; 2 elements for the gradient, which holds more per element: 3 x
+// 20011 x 331 f16, forward and gradient, 68 us, with 4 elements 82) over a run of
+// steps, the last K - 1 inputs in registers, the next batch of steps on its way while
+// one is worked on.  16 x 2048 x 2112 bf16, 4 taps: 62 us, 4.5 TB/s.
 //
 // The gradient walks a run forwards, forms u again and with it g_t = dy_t silu'(u_t);
 //   dx_t = sum_k w_k g_{t+K-1-k}
@@ -23,7 +24,9 @@
 namespace tq {
 namespace {
 
-constexpr int kBatch = 8;  // steps that are read together; K - 1 at most
+// steps that are read together
+constexpr int kBatch = 8, kGradBatch = 4;
+constexpr int kLeast = 8;   // steps of a run at least: K - 1 and more
 
 struct Geom {
     uint32_t items;   // threads with work
@@ -71,7 +74,7 @@ template <class T> __device__ __forceinline__ T *row_of(const StepsOut &s, int64
     return (T *)s.p + b * s.batch + t * s.step;
 }
 
-template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv(ConvArgs a, Geom g)
+template <class T, int V, int K, int N> __global__ __launch_bounds__(256) void k_conv(ConvArgs a, Geom g)
 {
     const uint32_t item = block_of() * 256 + threadIdx.x;
     if (item >= g.items) return;
@@ -79,7 +82,7 @@ template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv(C
     const Piece<V> at(item - row * g.pieces, a.D);
     const int64_t b = record, t0 = run * g.run, t1 = min(t0 + g.run, a.T);
     const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), a.T) : a.T, n1 = min(t1, len);
-    float w[K][V], bias[V], x[kBatch + K - 1][V];
+    float w[K][V], bias[V], x[N + K - 1][V];
 #pragma unroll
     for (int k = 0; k < K; k++) load_vec<V>((const T *)a.weight + k * a.D + at.c, w[k]);
 #pragma unroll
@@ -117,16 +120,20 @@ template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv(C
 #pragma unroll
         for (int k = 0; k + 1 < K; k++) load_vec<V>(row_of<T>(a.x, b, t0 - (K - 1) + k) + at.c, x[k]);
     }
-    for (int64_t t = t0; t < n1; t += kBatch) {
-        Raw<T, V> in[kBatch];
+    Raw<T, V> in[N];
+    const auto fetch = [&](int64_t t) {
 #pragma unroll
-        for (int i = 0; i < kBatch; i++) in[i].load(row_of<T>(a.x, b, min(t + i, n1 - 1)) + at.c);
+        for (int i = 0; i < N; i++) in[i].load(row_of<T>(a.x, b, min(t + i, n1 - 1)) + at.c);
+    };
+    if (t0 < n1) fetch(t0);
+    for (int64_t t = t0; t < n1; t += N) {
 #pragma unroll
-        for (int i = 0; i < kBatch; i++)
+        for (int i = 0; i < N; i++)
 #pragma unroll
             for (int j = 0; j < V; j++) x[K - 1 + i][j] = (float)in[i].v[j];
+        if (t + N < n1) fetch(t + N);  // on its way meanwhile
 #pragma unroll
-        for (int i = 0; i < kBatch; i++) {
+        for (int i = 0; i < N; i++) {
             if (t + i >= n1) break;
             float y[V];
 #pragma unroll
@@ -141,13 +148,15 @@ template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv(C
 #pragma unroll
         for (int k = 0; k + 1 < K; k++)
 #pragma unroll
-            for (int j = 0; j < V; j++) x[k][j] = x[kBatch + k][j];
+            for (int j = 0; j < V; j++) x[k][j] = x[N + k][j];
     }
     const float none[V] = {};
     for (int64_t t = max(t0, len); t < t1; t++) at.store(row_of<T>(a.y, b, t), none);
 }
 
-template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv_grad(ConvArgs a, Geom g)
+// (four wavefronts per SIMD where the registers of 16-bit rows and few taps allow it)
+template <class T, int V, int K>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && K <= 4 ? 4 : 2) void k_conv_grad(ConvArgs a, Geom g)
 {
     const uint32_t item = block_of() * 256 + threadIdx.x;
     if (item >= g.items) return;
@@ -180,7 +189,7 @@ template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv_g
                 for (int j = 0; j < V; j++) f[j] += d[j];
             }
         };
-        float x[kBatch + K - 1][V], q[kBatch + K - 1][V];
+        float x[kGradBatch + K - 1][V], q[kGradBatch + K - 1][V];
 #pragma unroll
         for (int k = 0; k + 1 < K; k++) {
 #pragma unroll
@@ -188,63 +197,72 @@ template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv_g
             if (run > 0) load_vec<V>(row_of<T>(a.x, b, t0 - (K - 1) + k) + at.c, x[k]);
             else if (a.state) load_vec<V>((const T *)a.state + (b * (K - 1) + k) * a.D + at.c, x[k]);
         }
-        // dx of the K - 1 steps before a step follow from it: on to K - 1 past the end
-        for (int64_t t = t0; t < n1 + K - 1; t += kBatch) {
-            if (t < len) {
-                Raw<T, V> in[kBatch], up[kBatch];
+        Raw<T, V> in[kGradBatch], up[kGradBatch];
+        const auto fetch = [&](int64_t t) {
 #pragma unroll
-                for (int i = 0; i < kBatch; i++) {
-                    in[i].load(row_of<T>(a.x, b, min(t + i, len - 1)) + at.c);
-                    up[i].load(row_of<T>(a.dy, b, min(t + i, len - 1)) + at.c);
-                }
-#pragma unroll
-                for (int i = 0; i < kBatch; i++)
-#pragma unroll
-                    for (int j = 0; j < V; j++) {
-                        x[K - 1 + i][j] = (float)in[i].v[j];
-                        q[K - 1 + i][j] = (float)up[i].v[j];
-                    }
+            for (int i = 0; i < kGradBatch; i++) {
+                in[i].load(row_of<T>(a.x, b, min(t + i, len - 1)) + at.c);
+                up[i].load(row_of<T>(a.dy, b, min(t + i, len - 1)) + at.c);
             }
+        };
+        // A batch of steps from t on; `whole`: all of the run's, and so are those whose
+        // dx they complete, none of which the state after the record holds.
+        const auto batch = [&](int64_t t, auto whole) {
+            constexpr bool kWhole = decltype(whole)::value;
 #pragma unroll
-            for (int i = 0; i < kBatch; i++) {
-                const bool there = t + i < len, mine = t + i < n1;
+            for (int i = 0; i < kGradBatch; i++) {
 #pragma unroll
                 for (int j = 0; j < V; j++) {
                     float &d = q[K - 1 + i][j];
                     if (a.silu) {
-                        float u = bias[j], s, c;
+                        float u = bias[j];
 #pragma unroll
                         for (int k = 0; k < K; k++) u = fmaf(w[k][j], x[i + k][j], u);
-                        sigmoids<T>(u, s, c);
-                        d *= s * fmaf(u, c, 1.f);
+                        const float s = sigmoid<T>(u);
+                        d *= s * fmaf(u, 1.f - s, 1.f);
                     }
-                    if (!there) d = 0.f;
-                    if (mine) {
+                    if (!kWhole && t + i >= len) d = 0.f;
+                    if (kWhole || t + i < n1) {
                         db[j] += d;
 #pragma unroll
                         for (int k = 0; k < K; k++) dw[k][j] = fmaf(d, x[i + k][j], dw[k][j]);
                     }
                 }
                 const int64_t o = t + i - (K - 1);  // the step whose dx is known now
-                if (o < n1 && (o >= t0 || (run == 0 && o < 0 && a.dstate))) {
-                    float f[V];
+                if (!kWhole && !(o < n1 && (o >= t0 || (run == 0 && o < 0 && a.dstate)))) continue;
+                float f[V];
+#pragma unroll
+                for (int j = 0; j < V; j++) {
+                    f[j] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < K; k++) f[j] = fmaf(w[k][j], q[i + K - 1 - k][j], f[j]);
+                }
+                if (!kWhole) returned(o, f);
+                if (kWhole || o >= 0) at.store(row_of<T>(a.dx, b, o), f);
+                else at.store((T *)a.dstate + (b * (K - 1) + o + K - 1) * a.D, f);
+            }
+        };
+        if (t0 < len) fetch(t0);
+        // dx of the K - 1 steps before a step follow from it: on to K - 1 past the end
+        for (int64_t t = t0; t < n1 + K - 1; t += kGradBatch) {
+            if (t < len) {
+#pragma unroll
+                for (int i = 0; i < kGradBatch; i++)
 #pragma unroll
                     for (int j = 0; j < V; j++) {
-                        f[j] = 0.f;
-#pragma unroll
-                        for (int k = 0; k < K; k++) f[j] = fmaf(w[k][j], q[i + K - 1 - k][j], f[j]);
+                        x[K - 1 + i][j] = (float)in[i].v[j];
+                        q[K - 1 + i][j] = (float)up[i].v[j];
                     }
-                    returned(o, f);
-                    if (o >= 0) at.store(row_of<T>(a.dx, b, o), f);
-                    else at.store((T *)a.dstate + (b * (K - 1) + o + K - 1) * a.D, f);
-                }
+                if (t + kGradBatch < min(n1 + K - 1, len)) fetch(t + kGradBatch);  // on its way meanwhile
             }
+            if (t >= t0 + K - 1 && t + kGradBatch <= n1) batch(t, std::true_type{});
+            else batch(t, std::false_type{});
 #pragma unroll
             for (int k = 0; k + 1 < K; k++)
 #pragma unroll
                 for (int j = 0; j < V; j++) {
-                    x[k][j] = x[kBatch + k][j];
-                    q[k][j] = q[kBatch + k][j];
+                    x[k][j] = x[kGradBatch + k][j];
+                    q[k][j] = q[kGradBatch + k][j];
                 }
         }
     }
@@ -254,37 +272,42 @@ template <class T, int V, int K> __global__ __launch_bounds__(256) void k_conv_g
     at.store(out + K * a.D, db);
 }
 
-// dweight and dbias: the rows' sums in order, 64 of the (K + 1) D columns per
-// workgroup, its wavefronts taking every 16th row.
-constexpr int kJoinWaves = 16;
-template <class T> __global__ __launch_bounds__(kJoinWaves * 64) void k_conv_join(ConvArgs a, Geom g)
+// dweight and dbias: the rows' sums in order, 16 of the (K + 1) D columns per
+// workgroup, its 64 groups of 16 lanes taking every 64th row.
+constexpr int kJoin = 64, kColumns = 16;
+template <class T> __global__ __launch_bounds__(kJoin * kColumns) void k_conv_join(ConvArgs a, Geom g)
 {
-    __shared__ float red[kJoinWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)block_of() * 64 + lane, columns = (a.K + 1) * a.D;
+    __shared__ float red[kJoin][kColumns + 1];
+    const int lane = threadIdx.x % kColumns, group = threadIdx.x / kColumns;
+    const int64_t c = (int64_t)block_of() * kColumns + lane, columns = (a.K + 1) * a.D;
     float s = 0.f;
     if (c < columns)
 #pragma unroll 8
-        for (uint32_t r = wave; r < g.rows; r += kJoinWaves) s += g.part[r * columns + c];
-    red[wave][lane] = s;
+        for (uint32_t r = group; r < g.rows; r += kJoin) s += g.part[r * columns + c];
+    red[group][lane] = s;
     __syncthreads();
-    if (wave || c >= columns) return;
-    s = 0.f;
 #pragma unroll
-    for (int w = 0; w < kJoinWaves; w++) s += red[w][lane];
+    for (int n = kJoin / 2; n > 0; n /= 2) {
+        if (group < n) red[group][lane] += red[group + n][lane];
+        __syncthreads();
+    }
+    if (group || c >= columns) return;
+    s = red[0][lane];
     if (c < a.K * a.D) ((T *)a.dweight)[c] = (T)s;
     else if (a.dbias) ((T *)a.dbias)[c - a.K * a.D] = (T)s;
 }
 
-template <class T, bool GRAD> constexpr int kPiece = GRAD ? 4 : kVec<T>;
+template <class T, bool GRAD> constexpr int kPiece = GRAD ? 2 : kVec<T>;
 
-// Steps of a run: as many as leave threads enough to fill the chip.
+// Steps of a run: as many as leave threads enough to fill the chip; each reads the K - 1
+// steps before it once more, and the gradient those behind.
 Geom geom_of(const ConvArgs &a, int V, bool grad)
 {
     Geom g{};
     g.pieces = (uint32_t)((a.D + V - 1) / V);
+    const double threads = grad ? 256 * 512 : 256 * 1024;
     g.run = 64;
-    while (g.run > kBatch && (double)a.B * (double)((a.T + g.run - 1) / g.run) * g.pieces < 256 * 512) g.run /= 2;
+    while (g.run > kLeast && (double)a.B * (double)((a.T + g.run - 1) / g.run) * g.pieces < threads) g.run /= 2;
     g.runs = (uint32_t)std::max<int64_t>(1, (a.T + g.run - 1) / g.run);
     g.rows = (uint32_t)(a.B * g.runs);
     if (grad) g.rows = (uint32_t)std::min<int64_t>(g.rows, std::max<int64_t>(1, 256 * 1024 / g.pieces));
@@ -309,7 +332,7 @@ template <class F> hipError_t by_taps(int K, F &&f)
 // Elements of a piece; rows without a whole one: one element each.
 int piece_of(int32_t type, int64_t D, bool grad)
 {
-    const int v = grad || type == TQ_F32 ? 4 : 8;
+    const int v = grad ? 2 : type == TQ_F32 ? 4 : 8;
     return D < v ? 1 : v;
 }
 
@@ -319,8 +342,9 @@ template <class T> hipError_t conv_t(const ConvArgs &a, int V, hipStream_t s)
     const dim3 grid = grid_of(((int64_t)g.items + 255) / 256);
     return by_taps((int)a.K, [&](auto k) {
         constexpr int K = decltype(k)::value;
-        if (V == 1) k_conv<T, 1, K><<<grid, 256, 0, s>>>(a, g);
-        else k_conv<T, kPiece<T, false>, K><<<grid, 256, 0, s>>>(a, g);
+        if (V == 1) k_conv<T, 1, K, kBatch><<<grid, 256, 0, s>>>(a, g);
+        else if (a.T == 1) k_conv<T, kPiece<T, false>, K, 1><<<grid, 256, 0, s>>>(a, g);
+        else k_conv<T, kPiece<T, false>, K, kBatch><<<grid, 256, 0, s>>>(a, g);
         return hipGetLastError();
     });
 }
@@ -338,7 +362,7 @@ template <class T> hipError_t conv_grad_t(const ConvArgs &a, int V, hipStream_t 
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    k_conv_join<T><<<grid_of(((a.K + 1) * a.D + 63) / 64), kJoinWaves * 64, 0, s>>>(a, g);
+    k_conv_join<T><<<grid_of(((a.K + 1) * a.D + kColumns - 1) / kColumns), kJoin * kColumns, 0, s>>>(a, g);
     return hipGetLastError();
 }
 
@@ -346,7 +370,7 @@ template <class T> hipError_t conv_grad_t(const ConvArgs &a, int V, hipStream_t 
 
 int64_t conv_items(int64_t B, int64_t T, int64_t D)
 {
-    const double n = (double)B * (double)((T + kBatch - 1) / kBatch) *
+    const double n = (double)B * (double)((T + kLeast - 1) / kLeast) *
                      (double)(D < 8 ? D : (D + 3) / 4);
     return n > 1e15 ? (int64_t)1e15 : (int64_t)n;
 }

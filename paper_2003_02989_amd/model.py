@@ -14,7 +14,7 @@ import math
 import torch
 
 from . import tq
-from .seq import _TYPES, _call, _dense, _on_stream, _ptr, _raw_stream, _rows, _space, _steps, _steps_out, _tensor, _typed
+from .seq import _TYPES, _call, _dense, _many, _on_stream, _ptr, _raw_stream, _rows, _space, _steps, _steps_out, _tensor, _typed
 
 STATES_PIECE = 16  # TQ_STATES_PIECE: steps per state that selective_scan keeps for its gradient
 
@@ -217,6 +217,21 @@ def _list(kind, values):
     return (kind * len(values))(*values)
 
 
+def _tensors(ts, name, like=None):
+    """(pointers, type codes) of contiguous tensors, of the shapes of `like`."""
+    ptrs, codes = [], []
+    for i, t in enumerate(ts):
+        # (what _dense checks, without a call for each where all is well)
+        if like is not None or _many or not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+            _dense(t, name, None, None if like is None else like[i].shape)
+        code = _TYPES.get(t.dtype)
+        if code is None:
+            raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+        ptrs.append(t.data_ptr())
+        codes.append(code)
+    return ptrs, codes
+
+
 @_on_stream
 def clip_grad_norm(grads, max_norm, scale=1.0, out=None):
     """(norm, outputs): the norm of all tensors of the list `grads` together, a
@@ -231,15 +246,9 @@ def clip_grad_norm(grads, max_norm, scale=1.0, out=None):
     if not grads:
         raise ValueError("grads must hold one tensor at least")
     n = len(grads)
-    ptrs, codes = [_dense(t, "grads", None) for t in grads], [_TYPES.get(t.dtype) for t in grads]
+    ptrs, codes = _tensors(grads, "grads")
     dev = grads[0].get_device()
-    if out is None:
-        out_ptrs, out_codes = ptrs, codes
-    else:
-        out_ptrs = [_dense(o, "out", None, g.shape) for o, g in zip(outs, grads)]
-        out_codes = [_TYPES.get(o.dtype) for o in outs]
-    if None in codes or None in out_codes:
-        raise TypeError("gradients must be float32, bfloat16 or float16")
+    out_ptrs, out_codes = (ptrs, codes) if out is None else _tensors(outs, "out", grads)
     counts = _list(ctypes.c_int64, [t.numel() for t in grads])
     norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
     need = ctypes.c_size_t()
