@@ -131,7 +131,7 @@ tq_status tq_clip_grad_norm(int64_t n, const void *const *grads, const int64_t *
  *    Candidates at -infinity, such as ids that a logit of -infinity rules out, are
  *    given only where there are no others; they rank by beam and id, those of a
  *    beam that has others by id behind these.
- * TQ_E_UNSUPPORTED for W or K > 64 or R W ceil(V / 4096) >= 2^31. */
+ * TQ_E_UNSUPPORTED for W or K > 64 or R W ceil(V / 2048) >= 2^31. */
 tq_status tq_beam_select_workspace(int32_t type, int64_t R, int64_t W, int64_t V, int64_t K, size_t *bytes);
 tq_status tq_beam_select(int32_t type, int64_t R, int64_t W, int64_t V, int64_t K, const void *logits,
                          int64_t ld_logits, const float *scores, const uint64_t *last, uint64_t end, float *out_scores,

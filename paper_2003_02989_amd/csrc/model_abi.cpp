@@ -48,7 +48,7 @@ void check_conv(const char *call, int type, int64_t B, int64_t T, int64_t D, int
     if (K > kMaxTaps) fail(TQ_E_UNSUPPORTED, text(call, "K must be at most 8"));
     if (D > kMaxWidth) fail(TQ_E_UNSUPPORTED, text(call, "D must be at most 2^20"));
     if (conv_items(B, T, D) > kMaxIndex || conv_items(B, 1, D) > kMaxIndex)
-        fail(TQ_E_UNSUPPORTED, text(call, "B * ceil(T / 8) * ceil(D / 4) must be below 2^31"));
+        fail(TQ_E_UNSUPPORTED, text(call, "B * ceil(T / 8) * ceil(D / 4), for D < 8 times D, must be below 2^31"));
 }
 
 void check_list(const char *call, int64_t n)
@@ -74,8 +74,8 @@ void check_beam(const char *call, int type, int64_t R, int64_t W, int64_t V, int
     if (W < 1 || K < 1 || V < 1) fail(TQ_E_INVALID, text(call, "W, V and K must be positive"));
     if (W > kMaxBeams || K > kMaxBeams) fail(TQ_E_UNSUPPORTED, text(call, "W and K must be at most 64"));
     if (K > W * V) fail(TQ_E_INVALID, text(call, "there are fewer than K candidates"));
-    if ((double)R * (double)W * (double)((V + 4095) / 4096) > kMaxIndex)
-        fail(TQ_E_UNSUPPORTED, text(call, "R * W * ceil(V / 4096) must be below 2^31"));
+    if ((double)R * (double)W * (double)((V + 2047) / 2048) > kMaxIndex)
+        fail(TQ_E_UNSUPPORTED, text(call, "R * W * ceil(V / 2048) must be below 2^31"));
 }
 
 } // namespace

@@ -32,6 +32,7 @@ using Key = unsigned long long;
 constexpr int kPieces = 8;  // of 16 bytes, a lane's part of a segment
 constexpr int kFewPieces = 2;
 template <class T, int P> constexpr int kSegment = 64 * P * kVec<T>;
+static_assert(kSegment<float, kPieces> >= 2048, "the limit of a call counts segments of 2048");
 constexpr double kNone = -__builtin_inf();
 
 struct Geom {

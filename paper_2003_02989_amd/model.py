@@ -162,6 +162,7 @@ def _conv_args(x, weight, bias, state, lengths, silu):
         raise ValueError("x must be a [B, T, D] tensor")
     N, T, D = shape = x.shape
     dtype = x.dtype
+    _tensor(weight, "weight", dtype)
     wp = _dense(weight, "weight", dtype)
     if weight.dim() != 2 or weight.shape[1] != D:
         raise ValueError(f"weight must have shape [K, {D}], got {tuple(weight.shape)}")
@@ -223,7 +224,8 @@ def _tensors(ts, name, like=None):
     for i, t in enumerate(ts):
         # (what _dense checks, without a call for each where all is well)
         if like is not None or _many or not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
-            _dense(t, name, None, None if like is None else like[i].shape)
+            _tensor(t, name, None, None if like is None else like[i].shape)
+            _dense(t, name, None)
         code = _TYPES.get(t.dtype)
         if code is None:
             raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
@@ -297,6 +299,7 @@ def beam_reorder(states, parents, out=None):
     states[i][r, parents[r, k]] as a tensor [R, K, ...], new or that of the list
     `out`; zeros where a parent is not one of the W."""
     states = list(states)
+    _tensor(parents, "parents", torch.int32)
     pp = _dense(parents, "parents", torch.int32)
     if parents.dim() != 2:
         raise ValueError("parents must be a [R, K] tensor")
