@@ -57,28 +57,31 @@ __device__ __forceinline__ float value_of(Key k)
 }
 __device__ __forceinline__ uint32_t id_of(Key k) { return ~(uint32_t)k; }
 
-// exp(x) for -700 <= x <= 0 to about 2^-47: x = n ln 2 + r, the series of e^r to r^11.
-// (The rounding of ln 2 costs n 2^-55.)
-__device__ __forceinline__ double exp_below(double x)
-{
-    const double magic = 0x1.8p52, t = fma(x, 1.4426950408889634, magic), n = t - magic;
-    const double r = fma(n, -0x1.62e42fefa39efp-1, x);
-    double p = 1. / 39916800.;
-    p = fma(p, r, 1. / 3628800.);
-    p = fma(p, r, 1. / 362880.);
-    p = fma(p, r, 1. / 40320.);
-    p = fma(p, r, 1. / 5040.);
-    p = fma(p, r, 1. / 720.);
-    p = fma(p, r, 1. / 120.);
-    p = fma(p, r, 1. / 24.);
-    p = fma(p, r, 1. / 6.);
-    p = fma(p, r, .5);
-    p = fma(p, r, 1.);
-    p = fma(p, r, 1.);
-    const uint64_t b = __builtin_bit_cast(uint64_t, p);
-    const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, t) << 20);
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)b);
-}
+// exp(x) for -700 <= x <= 0 to about 2^-42: x = n ln 2 + r, the series of e^r to r^10.
+// (The rounding of ln 2 costs n 2^-55.)  An instruction takes one constant from scalar
+// registers; two are held in vector registers for those that need two.
+struct Exp {
+    double magic = 0x1.8p52, last = 1. / 3628800.;
+    __device__ __forceinline__ Exp() { asm("" : "+v"(magic), "+v"(last)); }
+    __device__ __forceinline__ double operator()(double x) const
+    {
+        const double t = fma(x, 1.4426950408889634, magic), n = t - magic;
+        const double r = fma(n, -0x1.62e42fefa39efp-1, x);
+        double p = fma(last, r, 1. / 362880.);
+        p = fma(p, r, 1. / 40320.);
+        p = fma(p, r, 1. / 5040.);
+        p = fma(p, r, 1. / 720.);
+        p = fma(p, r, 1. / 120.);
+        p = fma(p, r, 1. / 24.);
+        p = fma(p, r, 1. / 6.);
+        p = fma(p, r, .5);
+        p = fma(p, r, 1.);
+        p = fma(p, r, 1.);
+        const uint64_t b = __builtin_bit_cast(uint64_t, p);
+        const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, t) << 20);
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)b);
+    }
+};
 constexpr float kFar = 690.f;  // what is further below a maximum counts as if it were not
 
 // The larger one, NaN where one is NaN.
@@ -198,6 +201,7 @@ template <class T, int P> struct Segment {
         for (int p = 0; p < P; p++) v[p].forget();
         sum = 0.;
         if (fabsf(top) < (float)-kNone) {
+            const Exp exp_below;
             const double base = (double)top;
             const float far = top - kFar;
 #pragma unroll
@@ -215,7 +219,7 @@ template <class T, int P> struct Segment {
         uint32_t bound = 0;
         const uint32_t high = lane * V < n ? ordered(mine) : 0;
 #pragma unroll
-        for (int bit = 31; bit >= 12; bit--) {
+        for (int bit = 31; bit >= 16; bit--) {
             const uint32_t more = bound | 1u << bit;
             if (__popcll(__ballot(high >= more)) >= K) bound = more;
         }
@@ -362,6 +366,7 @@ __global__ __launch_bounds__(1024) void k_beam_pick(BeamArgs a, Geom g)
             const int64_t at = row * g.segments;
             for (uint32_t i = lane; i < g.segments; i += 64) top = larger(top, g.tops[at + i]);
             top = wave_max(top);
+            const Exp exp_below;
             if (fabsf(top) < __builtin_inff())
                 for (uint32_t i = lane; i < g.segments; i += 64)
                     sum += g.sums[at + i] * exp_below((double)fmaxf(g.tops[at + i], top - kFar) - (double)top);
