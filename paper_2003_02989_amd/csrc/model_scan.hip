@@ -327,35 +327,37 @@ template <class T, int W, bool ENDS> __global__ __launch_bounds__(64 * W) void k
 // Turns what the chunks end with into what they start with, chunk by chunk, in
 // place: a lane has a channel's state.  Forwards from h0, the first chunk's end being
 // the state itself; backwards from the record's last chunk, whose end is it.
-template <bool BACK> __global__ __launch_bounds__(256) void k_select_chain(SelectArgs a, Geom g)
+template <bool BACK> __global__ __launch_bounds__(64) void k_select_chain(SelectArgs a, Geom g)
 {
-    const int64_t i = (int64_t)block_of() * 256 + threadIdx.x, sd = a.S * a.D;
+    const int64_t i = (int64_t)block_of() * 64 + threadIdx.x, sd = a.S * a.D;
     if (i >= a.B * sd) return;
     const int64_t b = i / sd, n = i - b * sd, s = n / a.D, d = n - s * a.D;
     const float A = exponent(a.A[d * a.S + s]);
     const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), a.T) : a.T;
     const int top = BACK ? (int)(max(len - 1, (int64_t)0) / g.chunk) : g.chunks - 1;
     float h = BACK || !a.h0 ? 0.f : a.h0[(b * a.D + d) * a.S + s];
-    float *end = g.ends + b * g.chunks * sd + n;
-    const float *sum = g.sums + b * g.chunks * a.D + d;
-    constexpr int N = 16;  // read together
-    for (int k0 = 0; k0 <= top; k0 += N) {
+    const int64_t first = b * g.chunks + (BACK ? top : 0), along = BACK ? -1 : 1;
+    float *end = g.ends + first * sd + n;
+    const float *sum = g.sums + first * a.D + d;
+    const auto step = [&](int k, float *at, float e, float w) {
+        *at = h;
+        h = k == 0 ? e : fmaf(__builtin_amdgcn_exp2f(w * A), h, e);
+    };
+    constexpr int N = 32;  // read together
+    int k = 0;
+    for (; k + N <= top; k += N, end += along * N * sd, sum += along * N * a.D) {
         float e[N], w[N];
 #pragma unroll
-        for (int k = 0; k < N; k++) {
-            // what a chunk ends with is not known of the last one taken
-            const int c = min(k0 + k, top - 1 > 0 ? top - 1 : 0), at = BACK ? top - c : c;
-            e[k] = end[at * sd];
-            w[k] = sum[(int64_t)at * a.D];
+        for (int j = 0; j < N; j++) {
+            e[j] = end[along * j * sd];
+            w[j] = sum[along * j * a.D];
         }
 #pragma unroll
-        for (int k = 0; k < N; k++) {
-            if (k0 + k > top) break;
-            const int at = BACK ? top - (k0 + k) : k0 + k;
-            end[at * sd] = h;
-            h = k0 + k == 0 ? e[k] : fmaf(__builtin_amdgcn_exp2f(w[k] * A), h, e[k]);
-        }
+        for (int j = 0; j < N; j++) step(k + j, end + along * j * sd, e[j], w[j]);
     }
+#pragma unroll 4
+    for (; k < top; k++, end += along * sd, sum += along * a.D) step(k, end, *end, *sum);
+    *end = h;  // the last one's own end is not needed
 }
 
 // ---------------------------------------------------------------- backward
@@ -701,10 +703,11 @@ template <class T> __global__ __launch_bounds__(256) void k_select_join_bc(Selec
 }
 
 // dA, dskip and ddt_bias: the workgroups' parts in order, 64 channels of one state
-// per workgroup, its wavefronts taking every fourth part.
-__global__ __launch_bounds__(256) void k_select_join(SelectArgs a, Geom g)
+// per workgroup, its wavefronts taking every 16th part.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void k_select_join(SelectArgs a, Geom g)
 {
-    __shared__ float red[4][64];
+    __shared__ float red[kJoinWaves][64];
     const uint32_t block = block_of();
     if (block >= g.slabs * (uint32_t)(a.S + 2)) return;
     const int n = (int)(block / g.slabs), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -713,12 +716,14 @@ __global__ __launch_bounds__(256) void k_select_join(SelectArgs a, Geom g)
     const int64_t step = (n < a.S ? a.S : 2) * a.D;
     float s = 0.f;
     if (d < a.D)
-#pragma unroll 4
-        for (uint32_t r = wave; r < g.rows; r += 4) s += from[r * step + d];
+#pragma unroll 8
+        for (uint32_t r = wave; r < g.rows; r += kJoinWaves) s += from[r * step + d];
     red[wave][lane] = s;
     __syncthreads();
     if (wave || d >= a.D) return;
-    s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinWaves; w++) s += red[w][lane];
     if (n < a.S) a.dA[d * a.S + n] = s;
     else if (n == a.S && a.dskip) a.dskip[d] = s;
     else if (n == a.S + 1 && a.ddt_bias) a.ddt_bias[d] = s;
@@ -843,7 +848,7 @@ template <class T, int W> hipError_t select_w(const SelectArgs &a, Geom g, hipSt
         const int64_t blocks = a.B * (g.chunks - 1) * g.slabs;
         g.blocks = (uint32_t)blocks;
         k_select<T, W, true><<<grid_of(blocks), 64 * W, 0, s>>>(a, g);
-        k_select_chain<false><<<grid_of((a.B * a.S * a.D + 255) / 256), 256, 0, s>>>(a, g);
+        k_select_chain<false><<<grid_of((a.B * a.S * a.D + 63) / 64), 64, 0, s>>>(a, g);
     }
     const int64_t blocks = a.B * g.chunks * g.slabs;
     g.blocks = (uint32_t)blocks;
@@ -900,7 +905,7 @@ template <class T, int W> void back_w(const SelectArgs &a, Geom g, hipStream_t s
     const int64_t blocks = a.B * (g.chunks - 1) * g.slabs;
     g.blocks = (uint32_t)blocks;
     k_select_back<T, W><<<grid_of(blocks), 64 * W, 0, s>>>(a, g);
-    k_select_chain<true><<<grid_of((a.B * a.S * a.D + 255) / 256), 256, 0, s>>>(a, g);
+    k_select_chain<true><<<grid_of((a.B * a.S * a.D + 63) / 64), 64, 0, s>>>(a, g);
 }
 
 template <class T> hipError_t grad_t(const SelectArgs &a, hipStream_t s)
@@ -924,7 +929,7 @@ template <class T> hipError_t grad_t(const SelectArgs &a, hipStream_t s)
     if (e != hipSuccess) return e;
     const int64_t n = a.B * a.T * 2 * a.S;
     if (n) k_select_join_bc<T><<<grid_of((n + 255) / 256), 256, 0, s>>>(a, g);
-    k_select_join<<<grid_of((int64_t)g.slabs * (a.S + 2)), 256, 0, s>>>(a, g);
+    k_select_join<<<grid_of((int64_t)g.slabs * (a.S + 2)), 64 * kJoinWaves, 0, s>>>(a, g);
     return hipGetLastError();
 }
 
