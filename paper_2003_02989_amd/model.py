@@ -221,10 +221,10 @@ def _list(kind, values):
 def _tensors(ts, name, like=None):
     """(pointers, type codes) of contiguous tensors, of the shapes of `like`."""
     ptrs, codes = [], []
-    for i, t in enumerate(ts):
-        # (what _dense checks, without a call for each where all is well)
-        if like is not None or _many or not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
-            _tensor(t, name, None, None if like is None else like[i].shape)
+    for t, k in zip(ts, ts if like is None else like):
+        # (what _tensor and _dense check, without their calls where all is well)
+        if _many or not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous() or t.shape != k.shape:
+            _tensor(t, name, None, None if k is t else k.shape)
             _dense(t, name, None)
         code = _TYPES.get(t.dtype)
         if code is None:
@@ -318,9 +318,12 @@ def beam_reorder(states, parents, out=None):
     if not states:
         return out
     W = states[0].shape[1]
-    ins = [_dense(t, "states", None) for t in states]
-    outs = [_dense(o, "out", t.dtype, (R, K) + t.shape[2:]) for o, t in zip(out, states)]
-    rows = [math.prod(t.shape[2:]) * t.element_size() for t in states]
+    ins, outs, rows = [], [], []
+    for t, o in zip(states, out):
+        row = t.shape[2:]
+        ins.append(_dense(t, "states", None))
+        outs.append(_dense(o, "out", t.dtype, (R, K) + row))
+        rows.append(math.prod(row) * t.element_size())
     _call((_lib or lib()).tq_beam_reorder, len(states), _list(ctypes.c_void_p, ins), _list(ctypes.c_void_p, outs),
           _list(ctypes.c_int64, rows), R, W, K, pp, _raw_stream(parents.get_device()))
     return out
