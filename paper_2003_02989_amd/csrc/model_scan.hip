@@ -454,16 +454,28 @@ struct LaneSums {
         const float keep = high ? b : a, give = high ? a : b;
         return keep + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, give), kDpp, 0xf, 0xf, true));
     }
-    // the rows keep value 0, 2, 1, 3
-    __device__ __forceinline__ static float rows(const float *v)
+    // of both fours; the rows keep value 0, 2, 1, 3.  (All exchanges of a kind in a row:
+    // what was written just before is waited for.)
+    __device__ __forceinline__ static void rows(const float (&v)[8], float (&sum)[2])
     {
         const auto bits = [](float f) { return __builtin_bit_cast(unsigned, f); };
         const auto val = [](unsigned u) { return __builtin_bit_cast(float, u); };
-        const auto p = __builtin_amdgcn_permlane32_swap(bits(v[0]), bits(v[1]), false, false);
-        const auto q = __builtin_amdgcn_permlane32_swap(bits(v[2]), bits(v[3]), false, false);
-        const float m = val(p[0]) + val(p[1]), n = val(q[0]) + val(q[1]);  // halves: value 0, 1; value 2, 3
-        const auto r = __builtin_amdgcn_permlane16_swap(bits(m), bits(n), false, false);
-        return val(r[0]) + val(r[1]);
+        float m[4];
+        unsigned a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const auto p = __builtin_amdgcn_permlane32_swap(bits(v[2 * i]), bits(v[2 * i + 1]), false, false);
+            a[i] = p[0], b[i] = p[1];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) m[i] = val(a[i]) + val(b[i]);  // halves: value 2 i, 2 i + 1
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const auto p = __builtin_amdgcn_permlane16_swap(bits(m[2 * i]), bits(m[2 * i + 1]), false, false);
+            a[i] = p[0], b[i] = p[1];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; i++) sum[i] = val(a[i]) + val(b[i]);
     }
     __device__ __forceinline__ static void enter(int t, float v, float (&held)[4])
     {
@@ -476,8 +488,10 @@ struct LaneSums {
     // the steps come from the last (15) to the first
     __device__ __forceinline__ void add(int t, const float (&v)[8])
     {
-        enter(t, rows(v), held[0]);
-        enter(t, rows(v + 4), held[1]);
+        float sum[2];
+        rows(v, sum);
+        enter(t, sum[0], held[0]);
+        enter(t, sum[1], held[1]);
     }
     // of four of the values, in the lanes of the step and value below
     __device__ __forceinline__ float sum(int four) const { return held[four][0]; }
