@@ -82,7 +82,7 @@ struct Exp {
         return __builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)b);
     }
 };
-constexpr float kFar = 690.f;  // what is further below a maximum counts as if it were not
+constexpr double kFar = -690.;  // what is further below a maximum counts as if it were not
 
 // The larger one, NaN where one is NaN.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
@@ -242,13 +242,12 @@ template <class T, int P> struct Segment {
         if (fabsf(top) < (float)-kNone) {
             const Exp exp_below;
             const double base = (double)top;
-            const float far = top - kFar;
 #pragma unroll
             for (int p = 0; p < P; p++)
                 if (p * 64 * V < n) {
                     double s = 0.;
 #pragma unroll
-                    for (int j = 0; j < V; j++) s += exp_below((double)fmaxf(v[p].get(j), far) - base);
+                    for (int j = 0; j < V; j++) s += exp_below(fmax((double)v[p].get(j) - base, kFar));
                     sum += s;
                     v[p].forget();
                 }
@@ -419,7 +418,7 @@ __global__ __launch_bounds__(1024) void k_beam_pick(BeamArgs a, Geom g)
             const Exp exp_below;
             if (fabsf(top) < __builtin_inff())
                 for (uint32_t i = lane; i < g.segments; i += 64)
-                    sum += g.sums[at + i] * exp_below((double)fmaxf(g.tops[at + i], top - kFar) - (double)top);
+                    sum += g.sums[at + i] * exp_below(fmax((double)g.tops[at + i] - (double)top, kFar));
             sum = wave_sum(sum);
             // the best of the segments' lists, as in a segment
             const int K = (int)a.K;

@@ -305,6 +305,17 @@ def test_beam_select_of_ordered_logits(ty, V, kind):
     beam_check(z, zv, np.float32([[-1, -1.5], [-2, -2]]), 24)
 
 
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("V", [40, 9000])
+def test_beam_select_of_logits_far_apart(ty, V):
+    """Maxima whose neighbours in fp32 are hundreds away, and sums of one term."""
+    i = np.arange(V)
+    far = 60000.0 if ty == "f16" else 3e38
+    zv = np.stack([np.where(i == 5, far, i % 11), np.where(i % 7 == 3, -far, i % 13 - far / 2), (i % 3 - 1) * 1e4])
+    z, zv = put(zv[None], TYPES[ty][0])
+    beam_check(z, zv, np.float32([[-1, -1.5, -0.5]]), 12)
+
+
 def test_beam_select_tells_close_scores_apart():
     """Beams whose best candidates differ by less than fp32 resolves."""
     rng = np.random.default_rng(4)
