@@ -14,7 +14,7 @@ import math
 import torch
 
 from . import tq
-from .seq import _TYPES, _call, _dense, _many, _on_stream, _ptr, _raw_stream, _rows, _space, _steps, _steps_out, _tensor, _typed
+from .seq import _TYPES, _call, _dense, _many, _on_stream, _ptr, _raw_stream, _rows, _space, _steps, _tensor, _typed
 
 STATES_PIECE = 16  # TQ_STATES_PIECE: steps per state that selective_scan keeps for its gradient
 
@@ -70,6 +70,24 @@ def _need(fn, *sizes):
     return n
 
 
+def _given_or_new(t, name, like):
+    """A given output of the shape of `like` [B, T, N], or a new one, dense: (tensor,
+    its steps)."""
+    if t is not None:
+        return t, _steps(t, name, like.dtype, like.shape)
+    _, T, N = shape = like.shape
+    t = like.new_empty(shape)
+    return t, (t.data_ptr(), T * N, N)
+
+
+def _floats(t, name, like, shape):
+    """A given float32 output, or a new one, dense: (tensor, its pointer)."""
+    if t is not None:
+        return t, _dense(t, name, torch.float32, shape)
+    t = torch.empty(shape, dtype=torch.float32, device=like.device)
+    return t, t.data_ptr()
+
+
 # ------------------------------------------------------------- selective scan
 
 SelectiveGrads = collections.namedtuple("SelectiveGrads", "dx ddt dA dB dC dskip dz ddt_bias dh0")
@@ -108,17 +126,14 @@ def selective_scan(x, dt, A, B, C, skip=None, z=None, dt_bias=None, h0=None, len
     dev, sizes, args, lp = _select_args(x, dt, A, B, C, skip, z, dt_bias, lengths)
     _, N, T, D, S = sizes
     hp = _dense(h0, "h0", torch.float32, (N, D, S))
-    y, ys = _steps_out(y, "y", x)
-    if h_last is None:
-        h_last = torch.empty((N, D, S), dtype=torch.float32, device=x.device)
-    pieces = -(-T // STATES_PIECE)
-    if states is None and keep:
-        states = torch.empty((N, pieces, S, D), dtype=torch.float32, device=x.device)
+    y, ys = _given_or_new(y, "y", x)
+    h_last, hlp = _floats(h_last, "h_last", x, (N, D, S))
+    sp = None
+    if keep or states is not None:
+        states, sp = _floats(states, "states", x, (N, -(-T // STATES_PIECE), S, D))
     n = _need("tq_selective_scan_workspace", N, T, D, S)
     ws = _space(x, n)
-    _call((_lib or lib()).tq_selective_scan, *sizes, *args, hp, lp, *ys,
-          _dense(h_last, "h_last", torch.float32, (N, D, S)),
-          _dense(states, "states", torch.float32, (N, pieces, S, D)), _ptr(ws), n, _raw_stream(dev))
+    _call((_lib or lib()).tq_selective_scan, *sizes, *args, hp, lp, *ys, hlp, sp, _ptr(ws), n, _raw_stream(dev))
     return (y, h_last, states) if states is not None else (y, h_last)
 
 
@@ -133,16 +148,16 @@ def selective_scan_grad(x, dt, A, B, C, states, dy, skip=None, z=None, dt_bias=N
     sp = _dense(states, "states", torch.float32, (N, -(-T // STATES_PIECE), S, D))
     dys = _steps(dy, "dy", x.dtype, x.shape)
     dhp = _dense(dh_last, "dh_last", torch.float32, (N, D, S))
-    dx, dxs = _steps_out(dx, "dx", x)
-    ddt, ddts = _steps_out(ddt, "ddt", x)
-    dB, dBs = _steps_out(dB, "dB", B)
-    dC, dCs = _steps_out(dC, "dC", C)
+    dx, dxs = _given_or_new(dx, "dx", x)
+    ddt, ddts = _given_or_new(ddt, "ddt", x)
+    dB, dBs = _given_or_new(dB, "dB", B)
+    dC, dCs = _given_or_new(dC, "dC", C)
     if z is None:
         if dz is not None:
             raise ValueError("dz goes with z")
         dzs = _NONE
     else:
-        dz, dzs = _steps_out(dz, "dz", x)
+        dz, dzs = _given_or_new(dz, "dz", x)
     dA = torch.empty((D, S), dtype=torch.float32, device=x.device)
     dskip = None if skip is None else torch.empty((D,), dtype=torch.float32, device=x.device)
     dbias = None if dt_bias is None else torch.empty((D,), dtype=torch.float32, device=x.device)
@@ -181,11 +196,13 @@ def causal_conv(x, weight, bias=None, state=None, lengths=None, silu=True, y=Non
     are then extended in place."""
     dev, sizes, args = _conv_args(x, weight, bias, state, lengths, silu)
     _, N, _, D, K = sizes
-    y, ys = _steps_out(y, "y", x)
+    y, ys = _given_or_new(y, "y", x)
     if last is None:
         last = x.new_empty((N, max(K - 1, 0), D))
-    _call((_lib or lib()).tq_causal_conv, *sizes, *args, *ys, _dense(last, "last", x.dtype, (N, K - 1, D)),
-          _raw_stream(dev))
+        lp = last.data_ptr()
+    else:
+        lp = _dense(last, "last", x.dtype, (N, K - 1, D))
+    _call((_lib or lib()).tq_causal_conv, *sizes, *args, *ys, lp, _raw_stream(dev))
     return y, last
 
 
@@ -201,7 +218,7 @@ def causal_conv_grad(x, weight, dy, bias=None, state=None, dlast=None, lengths=N
     _, N, T, D, K = sizes
     dys = _steps(dy, "dy", x.dtype, x.shape)
     dp = _dense(dlast, "dlast", x.dtype, (N, K - 1, D))
-    dx, dxs = _steps_out(dx, "dx", x)
+    dx, dxs = _given_or_new(dx, "dx", x)
     dweight = torch.empty_like(weight)
     dbias = None if bias is None else torch.empty_like(bias)
     dstate = None if state is None else torch.empty_like(state)
