@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && K <= 4 ? 4 : 2) void k_conv_
         const int64_t b = record, t0 = run * g.run, t1 = min(t0 + g.run, a.T);
         const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), a.T) : a.T, n1 = min(t1, len);
         const float none[V] = {};
-        for (int64_t t = max(t0, len); t < t1; t++) at.store(row_of<T>(a.dx, b, t), none);
+        for (int64_t t = max(t0, len); t < t1; t++) store_vec<V>(row_of<T>(a.dx, b, t) + at.c, none);
         if (t0 >= len && run > 0) continue;
         // what comes back from the state after the record: to its last K - 1 inputs
         const auto returned = [&](int64_t t, float (&f)[V]) {
@@ -198,15 +198,30 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && K <= 4 ? 4 : 2) void k_conv_
             else if (a.state) load_vec<V>((const T *)a.state + (b * (K - 1) + k) * a.D + at.c, x[k]);
         }
         Raw<T, V> in[kGradBatch], up[kGradBatch];
+        // the rows of the next read, and of the step that a batch begins with
+        const T *px = row_of<T>(a.x, b, t0) + at.c, *pdy = row_of<T>(a.dy, b, t0) + at.c;
+        T *pdx = row_of<T>(a.dx, b, t0) + at.c;
         const auto fetch = [&](int64_t t) {
+            const int left = (int)min(len - 1 - t, (int64_t)kGradBatch);  // the last step there is
+            if (__ballot(left < kGradBatch - 1) == 0) {
 #pragma unroll
-            for (int i = 0; i < kGradBatch; i++) {
-                in[i].load(row_of<T>(a.x, b, min(t + i, len - 1)) + at.c);
-                up[i].load(row_of<T>(a.dy, b, min(t + i, len - 1)) + at.c);
+                for (int i = 0; i < kGradBatch; i++) {
+                    in[i].load(px + i * a.x.step);
+                    up[i].load(pdy + i * a.dy.step);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kGradBatch; i++) {
+                    in[i].load(px + min(i, left) * a.x.step);
+                    up[i].load(pdy + min(i, left) * a.dy.step);
+                }
             }
+            px += kGradBatch * a.x.step;
+            pdy += kGradBatch * a.dy.step;
         };
         // A batch of steps from t on; `whole`: all of the run's, and so are those whose
-        // dx they complete, none of which the state after the record holds.
+        // dx they complete, none of which the state after the record holds.  (A row's last
+        // piece is stored whole: what it shares with the one before is the same in both.)
         const auto batch = [&](int64_t t, auto whole) {
             constexpr bool kWhole = decltype(whole)::value;
 #pragma unroll
@@ -238,9 +253,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && K <= 4 ? 4 : 2) void k_conv_
                     for (int k = 0; k < K; k++) f[j] = fmaf(w[k][j], q[i + K - 1 - k][j], f[j]);
                 }
                 if (!kWhole) returned(o, f);
-                if (kWhole || o >= 0) at.store(row_of<T>(a.dx, b, o), f);
-                else at.store((T *)a.dstate + (b * (K - 1) + o + K - 1) * a.D, f);
+                if (kWhole || o >= 0) store_vec<V>(pdx + (i - (K - 1)) * a.dx.step, f);
+                else store_vec<V>((T *)a.dstate + (b * (K - 1) + o + K - 1) * a.D + at.c, f);
             }
+            pdx += kGradBatch * a.dx.step;
         };
         if (t0 < len) fetch(t0);
         // dx of the K - 1 steps before a step follow from it: on to K - 1 past the end
@@ -268,8 +284,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && K <= 4 ? 4 : 2) void k_conv_
     }
     float *out = g.part + (int64_t)first * (K + 1) * a.D;
 #pragma unroll
-    for (int k = 0; k < K; k++) at.store(out + k * a.D, dw[k]);
-    at.store(out + K * a.D, db);
+    for (int k = 0; k < K; k++) store_vec<V>(out + k * a.D + at.c, dw[k]);
+    store_vec<V>(out + K * a.D + at.c, db);
 }
 
 // dweight and dbias: the rows' sums in order, 16 of the (K + 1) D columns per
@@ -310,7 +326,9 @@ Geom geom_of(const ConvArgs &a, int V, bool grad)
     while (g.run > kLeast && (double)a.B * (double)((a.T + g.run - 1) / g.run) * g.pieces < threads) g.run /= 2;
     g.runs = (uint32_t)std::max<int64_t>(1, (a.T + g.run - 1) / g.run);
     g.rows = (uint32_t)(a.B * g.runs);
-    if (grad) g.rows = (uint32_t)std::min<int64_t>(g.rows, std::max<int64_t>(1, 256 * 1024 / g.pieces));
+    // records of different lengths are evened out by more rows of fewer runs
+    const int64_t most = a.lengths ? 256 * 2048 : 256 * 1024;
+    if (grad) g.rows = (uint32_t)std::min<int64_t>(g.rows, std::max<int64_t>(1, most / g.pieces));
     g.items = g.rows * g.pieces;
     return g;
 }
@@ -377,8 +395,9 @@ int64_t conv_items(int64_t B, int64_t T, int64_t D)
 
 size_t conv_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t K)
 {
+    static const int32_t some = 0;
     ConvArgs a{};
-    a.B = B, a.T = T, a.D = D, a.K = K;
+    a.B = B, a.T = T, a.D = D, a.K = K, a.lengths = &some;  // at most
     return sizeof(float) * geom_of(a, piece_of(TQ_F32, D, true), true).rows * (size_t)(K + 1) * (size_t)D;
 }
 
