@@ -90,7 +90,7 @@ class Scan:
 
 
 SCANS = [(1, 1, 5, 1), (3, 1, 70, 16), (2, 7, 64, 4), (4, 16, 65, 16), (3, 17, 130, 5), (3, 40, 33, 64), (4, 33, 70, 33),
-         (2, 50, 10, 20), (1, 300, 20, 16), (2, 1000, 9, 3), (5, 450, 66, 9), (3, 0, 7, 4), (70, 2, 3, 2)]
+         (5, 3, 66, 40), (3, 4, 9, 7), (2, 5, 40, 16), (2, 50, 10, 20), (1, 300, 20, 16), (2, 1000, 9, 3), (5, 450, 66, 9), (3, 0, 7, 4), (70, 2, 3, 2)]
 
 
 @pytest.mark.parametrize("ty", TYPES)
