@@ -34,7 +34,8 @@ extern "C" {
  * states, when not NULL, receives what tq_selective_scan_grad starts from: float
  * [B, ceil(T / TQ_STATES_PIECE), S, D], the state before every step that is a
  * multiple of TQ_STATES_PIECE (past a record's length: not written).
- * TQ_E_UNSUPPORTED for S > 64, D > 2^20 or B ceil(D / 64) ceil(T / 64) >= 2^31. */
+ * TQ_E_UNSUPPORTED for S > 64, D > 2^20 or B ceil(D / 64) ceil(T / 64) >= 2^31
+ * (T = 0 counts as 1). */
 #define TQ_STATES_PIECE 16
 tq_status tq_selective_scan_workspace(int64_t B, int64_t T, int64_t D, int64_t S, size_t *bytes);
 tq_status tq_selective_scan(int32_t type, int64_t B, int64_t T, int64_t D, int64_t S, const void *x, int64_t x_batch,

@@ -21,8 +21,8 @@ void check_select(const char *call, int type, int64_t B, int64_t T, int64_t D, i
     if (S < 1) fail(TQ_E_INVALID, text(call, "a channel needs one state at least"));
     if (S > kMaxStates) fail(TQ_E_UNSUPPORTED, text(call, "S must be at most 64"));
     if (D > kMaxWidth) fail(TQ_E_UNSUPPORTED, text(call, "D must be at most 2^20"));
-    // in doubles: the product of three sizes
-    if ((double)B * (double)((D + 63) / 64) * (double)((T + 63) / 64) > kMaxIndex)
+    // in doubles: the product of three sizes; records of no steps have their states
+    if ((double)B * (double)((D + 63) / 64) * (double)((std::max<int64_t>(T, 1) + 63) / 64) > kMaxIndex)
         fail(TQ_E_UNSUPPORTED, text(call, "B * ceil(D / 64) * ceil(T / 64) must be below 2^31"));
 }
 

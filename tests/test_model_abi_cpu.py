@@ -35,7 +35,8 @@ def test_selective_scan_refusals():
                  (h0, P + 1), (n, P + 2), (y, None), (y + 1, D), (y + 2, D - 1), (h, P + 2), (states, P + 1), (ws, None),
                  (ws, P + 8), (ws + 1, need - 1)):
         refused(tq.TQ_E_INVALID, L.tq_selective_scan, *changed(ok, k, v))
-    for sizes in ((2, T, D, 65), (2, T, (1 << 20) + 1, S), (1 << 20, 1 << 20, 64, S), (1 << 31, 1, 1, 1)):
+    for sizes in ((2, T, D, 65), (2, T, (1 << 20) + 1, S), (1 << 20, 1 << 20, 64, S), (1 << 31, 1, 1, 1),
+                  ((1 << 31) - 1, 0, 65, 1)):
         refused(tq.TQ_E_UNSUPPORTED, L.tq_selective_scan, F32, *sizes, *ok[5:])
         refused(tq.TQ_E_UNSUPPORTED, L.tq_selective_scan_workspace, *sizes, ctypes.byref(ctypes.c_size_t()))
         refused(tq.TQ_E_UNSUPPORTED, L.tq_selective_scan_grad_workspace, *sizes, ctypes.byref(ctypes.c_size_t()))
