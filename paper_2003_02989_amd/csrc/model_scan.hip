@@ -443,8 +443,8 @@ template <class T, int W> __global__ __launch_bounds__(64 * W) void k_select_bac
 // the four rows of 16 lanes at once; the sums of two steps over lanes 8 apart, their
 // pairs over lanes mirrored in eight, then 2 and 1 apart, until the lanes of a row
 // hold a step each.  Three instructions for two values in place of one and an exchange
-// a value and distance: the kernel takes 517 us in place of 648 (24 x 1365 x 1024
-// bf16 on average of two cuts).
+// a value and distance: the kernel takes 517 us in place of 648 (the mean of 16 x
+// 2048 x 1024 and 32 x 1024 x 1024 bf16).
 struct LaneSums {
     float held[2][4];
     template <int N> __device__ __forceinline__ static float join(float a, float b)
@@ -817,21 +817,31 @@ int waves_of(int64_t S, int most)
     return w;
 }
 
-// Chunks of time.  Forming every exponential once more costs less than leaving half
-// of the chip idle, and several workgroups for each place of the chip even out
-// records of different lengths: forward and gradient of 8 x 4099 x 1024 bf16, ragged,
-// 425 us with up to 4096 workgroups of four wavefronts, 574 with 1024; 16 x 2048 x
-// 1024 930 and 885.  Chunks of at least 96 steps: 1 x 1000 x 200 30 us with 64, 42
-// with 128, 1 x 20000 x 64 with 64 states 294 and 252.
+// Chunks of time.  Forming every exponential once more costs less than leaving part of
+// the chip idle; a round is as many workgroups of the gradient as the chip holds.
+//  - Up to eight rounds, of chunks of at least 96 steps, and whole ones: forward and
+//    gradient of 4 x 4096 x 512 bf16 258 us in two rounds, 280 in 2.7.
+//  - Records of different lengths are evened out by more workgroups, of 64 steps, and
+//    so gain from chunks where there are more channels: 8 x 4099 x 1024 bf16 410 us
+//    (574 in two rounds); 20 x 1200 x 1200, three quarters of a round, 551 and 711
+//    without chunks (alike: 859 and 788), 64 x 512 x 512 fp32, a whole one, 397 and 303.
+//  - Where that is less than a round, one round of shorter chunks: 8 x 256 x 128 with 8
+//    states 59 us in place of 118, the scan of 1 x 1000 x 200 23 in place of 34; below
+//    96 steps there is nothing to gain (2 x 60 x 130: 59 and 51 us without).
 struct Cut {
     int chunks;
     int64_t chunk;
 };
-Cut cut_of(int64_t B, int64_t T, int64_t D, int64_t S)
+Cut cut_of(int64_t B, int64_t T, int64_t D, int64_t S, bool ragged)
 {
-    const int64_t rows = std::max<int64_t>(1, B * slabs_of(D)), unit = 1024 / waves_of(S, 8);
+    const int64_t rows = std::max<int64_t>(1, B * slabs_of(D)), round = 2048 / waves_of(S, 8);
     int64_t n = 1;
-    if (rows * 3 <= 4 * unit) n = std::min((16 * unit + rows - 1) / rows, (T + 95) / 96);
+    if (ragged ? rows * 6 <= round * 5 : rows * 3 <= round * 2) {
+        const int64_t least = ragged ? 64 : 96;
+        n = std::min((8 * round + rows - 1) / rows, (T + least - 1) / least);
+        if (rows * n < round) n = T < 96 ? 1 : std::min(round / rows, T / kTile);
+        else if (!ragged) n = rows * n / round * round / rows;
+    }
     if (n < 3) n = 1;
     const int64_t chunk = std::max<int64_t>(kTile, ((T + n - 1) / n + kTile - 1) / kTile * kTile);
     return {(int)std::max<int64_t>(1, (T + chunk - 1) / chunk), chunk};
@@ -843,10 +853,11 @@ int64_t grad_rows(int64_t B, const Cut &c, int64_t D)
     return std::min(B * c.chunks, std::max<int64_t>(1, 4096 / slabs_of(D)));
 }
 
-size_t place(const SelectArgs &a, bool grad, Geom &g)
+// (Records of different lengths are cut into no fewer chunks, and need no less space.)
+size_t place(const SelectArgs &a, bool grad, bool ragged, Geom &g)
 {
     Carver ws;
-    const Cut c = cut_of(a.B, a.T, a.D, a.S);
+    const Cut c = cut_of(a.B, a.T, a.D, a.S, ragged);
     const size_t f = sizeof(float), bsd = (size_t)a.B * a.S * a.D;
     g.chunks = c.chunks, g.chunk = c.chunk;
     g.slabs = (uint32_t)slabs_of(a.D);
@@ -903,7 +914,7 @@ template <class T> hipError_t select_t(const SelectArgs &a, hipStream_t s)
         default: return step_l<T, 16>(a, s);
         }
     Geom g{};
-    place(a, false, g);
+    if (place(a, false, a.lengths, g) > select_workspace(a.B, a.T, a.D, a.S)) return hipErrorInvalidValue;
     switch (waves_of(a.S, 16)) {
     case 1: return select_w<T, 1>(a, g, s);
     case 2: return select_w<T, 2>(a, g, s);
@@ -935,7 +946,7 @@ template <class T, int W> void back_w(const SelectArgs &a, Geom g, hipStream_t s
 template <class T> hipError_t grad_t(const SelectArgs &a, hipStream_t s)
 {
     Geom g{};
-    place(a, true, g);
+    if (place(a, true, a.lengths, g) > select_grad_workspace(a.B, a.T, a.D, a.S)) return hipErrorInvalidValue;
     if (g.chunks > 1 && g.rows) switch (waves_of(a.S, 16)) {
         case 1: back_w<T, 1>(a, g, s); break;
         case 2: back_w<T, 2>(a, g, s); break;
@@ -964,7 +975,7 @@ size_t select_workspace(int64_t B, int64_t T, int64_t D, int64_t S)
     SelectArgs a{};
     a.B = B, a.T = T, a.D = D, a.S = (int)S;
     Geom g{};
-    return place(a, false, g);
+    return place(a, false, true, g);
 }
 
 size_t select_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t S)
@@ -972,7 +983,7 @@ size_t select_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t S)
     SelectArgs a{};
     a.B = B, a.T = T, a.D = D, a.S = (int)S;
     Geom g{};
-    return place(a, true, g);
+    return place(a, true, true, g);
 }
 
 hipError_t launch_select(int32_t type, const SelectArgs &a, hipStream_t s)

@@ -90,7 +90,8 @@ class Scan:
 
 
 SCANS = [(1, 1, 5, 1), (3, 1, 70, 16), (2, 7, 64, 4), (4, 16, 65, 16), (3, 17, 130, 5), (3, 40, 33, 64), (4, 33, 70, 33),
-         (5, 3, 66, 40), (3, 4, 9, 7), (2, 5, 40, 16), (2, 50, 10, 20), (1, 300, 20, 16), (2, 1000, 9, 3), (5, 450, 66, 9), (3, 0, 7, 4), (70, 2, 3, 2)]
+         (5, 3, 66, 40), (3, 4, 9, 7), (2, 5, 40, 16), (2, 50, 10, 20), (1, 300, 20, 16), (2, 1000, 9, 3),
+         (5, 450, 66, 9), (3, 0, 7, 4), (70, 2, 3, 2), (9, 1300, 140, 5)]
 
 
 @pytest.mark.parametrize("ty", TYPES)
@@ -105,7 +106,7 @@ def test_selective_scan_and_gradients(ty, B, T, D, S):
 
 
 @pytest.mark.parametrize("ty", TYPES)
-@pytest.mark.parametrize("B,T,D,S", [(2, 37, 70, 16), (1, 400, 12, 6), (3, 1, 9, 16)])
+@pytest.mark.parametrize("B,T,D,S", [(2, 37, 70, 16), (1, 400, 12, 6), (3, 1, 9, 16), (4, 120, 200, 7), (9, 1300, 300, 5)])
 def test_selective_scan_without_the_optional_inputs(ty, B, T, D, S):
     c = Scan(ty, B, T, D, S, ragged=False, gated=False, seed=1)
     y, h, states = c.forward(h0=False, keep=True)

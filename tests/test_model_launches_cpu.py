@@ -118,6 +118,18 @@ def test_largest_sizes(tmp_path):
     run(calls, tmp_path)
 
 
+def test_scans_find_room_in_their_workspace(tmp_path):
+    """With lengths and without, which are cut into chunks by different rules; a launch
+    that needs more than the workspace function gives is refused."""
+    calls = []
+    for S in (3, 16, 40, 64):
+        for B, D in ((1, 5), (1, 1000), (7, 64), (9, 300), (20, 1200), (25, 1100), (64, 512), (300, 40), (3000, 64)):
+            for T in (2, 17, 64, 95, 96, 100, 350, 1200, 5000):
+                for call, at in ((scan(0, B, T, D, S), 25), (scan_grad(0, B, T, D, S), 25)):
+                    calls += [call, (*call[:at], None, *call[at + 1:])]
+    run(calls, tmp_path)
+
+
 def test_no_kernel_is_left_that_no_call_reaches(tmp_path):
     calls = []
     for ty in range(3):
