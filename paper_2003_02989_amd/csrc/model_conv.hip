@@ -4,10 +4,11 @@
 //
 // channel by channel, the K - 1 inputs before the first step being the record's
 // state.  Bound by memory: x is read and y written once.  A thread holds a piece of
-// a row (16 bytes; 2 elements for the gradient, which holds more per element: 3 x
-// 20011 x 331 f16, forward and gradient, 68 us, with 4 elements 82) over a run of
-// steps, the last K - 1 inputs in registers, the next batch of steps on its way while
-// one is worked on.  16 x 2048 x 2112 bf16, 4 taps: 62 us, 4.5 TB/s.
+// a row over a run of steps, the last K - 1 inputs in registers, the next batch of
+// steps on its way while one is worked on.  A piece is 16 bytes (16 x 2048 x 2112 bf16,
+// 4 taps: 63 us, 4.4 TB/s); for the gradient, which holds more per element, 2 elements:
+// forward and gradient of 8 x 1024 x 512 fp32 31 us, with 4 elements 36, and 16-bit
+// ones with 4 do not fit the registers that four wavefronts per SIMD have.
 //
 // The gradient walks a run forwards, forms u again and with it g_t = dy_t silu'(u_t);
 //   dx_t = sum_k w_k g_{t+K-1-k}
