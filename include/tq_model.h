@@ -58,7 +58,8 @@ tq_status tq_selective_scan(int32_t type, int64_t B, int64_t T, int64_t D, int64
  * and dB, dC [B, T, S] have the inputs' type and strides of their own; dA, dskip,
  * ddt_bias and dh0 are float as the tensors that they belong to.  dz goes with z;
  * dskip, ddt_bias and dh0 may be NULL: not wanted.  `states` are the ones that
- * tq_selective_scan wrote for the same inputs. */
+ * tq_selective_scan wrote for the same inputs.  For D = 0 nothing is enqueued: dB and
+ * dC, sums over no channels, are the caller's to clear. */
 tq_status tq_selective_scan_grad_workspace(int64_t B, int64_t T, int64_t D, int64_t S, size_t *bytes);
 tq_status tq_selective_scan_grad(int32_t type, int64_t B, int64_t T, int64_t D, int64_t S, const void *x,
                                  int64_t x_batch, int64_t x_step, const void *dt, int64_t dt_batch, int64_t dt_step,

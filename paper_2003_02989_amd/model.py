@@ -166,6 +166,9 @@ def selective_scan_grad(x, dt, A, B, C, states, dy, skip=None, z=None, dt_bias=N
     ws = _space(x, n)
     _call((_lib or lib()).tq_selective_scan_grad, *sizes, *args, sp, lp, *dys, dhp, *dxs, *ddts, *dzs, *dBs, *dCs,
           dA.data_ptr(), _ptr(dskip), _ptr(dbias), dh0.data_ptr(), _ptr(ws), n, _raw_stream(dev))
+    if D == 0:  # sums over no channels, which the call leaves as they are
+        dB.zero_()
+        dC.zero_()
     return SelectiveGrads(dx, ddt, dA, dB, dC, dskip, dz, dbias, dh0)
 
 
