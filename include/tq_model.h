@@ -108,9 +108,11 @@ tq_status tq_causal_conv_grad(int32_t type, int64_t B, int64_t T, int64_t D, int
  * grads, outs, counts, types and out_types are HOST arrays of n entries, read
  * during the call: device pointers, numbers of elements and tq_dtypes.  outs[i] may
  * be grads[i] where both have one type.  Squares are summed in 64 bits; norm, float
- * on the device, is written always.  An infinite norm gives zeros for finite
- * elements and NaN for infinite ones, a norm of NaN gives NaN.  max_norm >= 0 (it may
- * be infinite), scale > 0 and finite (1 over the factor that a loss was scaled by).
+ * on the device, is written always, infinite where the norm is past the range of fp32;
+ * the factor is formed from the norm in 64 bits.  An infinite norm above max_norm gives
+ * zeros for finite elements and NaN for infinite ones, a norm of NaN gives NaN.
+ * max_norm >= 0 (infinite: nothing is cut, the factor is `scale` for an infinite norm
+ * too), scale > 0 and finite (1 over the factor that a loss was scaled by).
  * TQ_E_UNSUPPORTED for n >= 2^20 or a tensor of 2^40 elements. */
 tq_status tq_clip_grad_norm_workspace(int64_t n, const int64_t *counts, size_t *bytes);
 tq_status tq_clip_grad_norm(int64_t n, const void *const *grads, const int64_t *counts, const int32_t *types,

@@ -132,6 +132,13 @@ template <class T, class O> __device__ __forceinline__ void scaled(const T *p, O
     }
 }
 
+// The same with a factor that fp32 holds as a subnormal number or not at all: elements
+// near the largest ones still give products that are numbers, formed in 64 bits.
+template <class T, class O> __device__ __forceinline__ void scaled_far(const T *p, O *o, int64_t n, double f)
+{
+    for (int i = threadIdx.x & 63; i < min(n, (int64_t)kChunk); i += 64) o[i] = (O)(float)((double)(float)p[i] * f);
+}
+
 // A wavefront's sum over its run.
 __device__ __forceinline__ double sum_run(const Tensors &t, Run r)
 {
@@ -150,9 +157,11 @@ __device__ __forceinline__ double sum_run(const Tensors &t, Run r)
 }
 
 // A run from its end.  Where nothing changes, in place, nothing is written.
-__device__ __forceinline__ void scale_run(const Tensors &t, Run r, float c)
+__device__ __forceinline__ void scale_run(const Tensors &t, Run r, double f)
 {
     if (r.from >= r.to) return;
+    const float c = (float)f;
+    const bool far = f > 0. && f < 0x1p-126;
     int i = tensor_of(t, r.to - 1);
     for (uint32_t k = r.to; k-- > r.from;) {
         while (k < t.first[i]) i--;
@@ -160,7 +169,10 @@ __device__ __forceinline__ void scale_run(const Tensors &t, Run r, float c)
         const int64_t at = (int64_t)(k - t.first[i]) * kChunk;
         by_type(t.in_type[i], [&](auto x) {
             by_type(t.out_type[i], [&](auto y) {
-                scaled((const decltype(x) *)t.in[i] + at, (decltype(y) *)t.out[i] + at, t.count[i] - at, c);
+                const auto *in = (const decltype(x) *)t.in[i] + at;
+                auto *out = (decltype(y) *)t.out[i] + at;
+                if (far) scaled_far(in, out, t.count[i] - at, f);
+                else scaled(in, out, t.count[i] - at, c);
             });
         });
     }
@@ -168,11 +180,11 @@ __device__ __forceinline__ void scale_run(const Tensors &t, Run r, float c)
 
 // The factor of the elements from the sum of their squares; a norm that is not a
 // number gives factors that are none, an infinite one zeros.
-__device__ __forceinline__ float factor(const ClipArgs &a, double sum, float *norm)
+__device__ __forceinline__ double factor(const ClipArgs &a, double sum, float *norm)
 {
     const double n = sqrt(sum) * (double)a.scale;
     if (norm) *norm = (float)n;
-    return (float)((double)a.scale * (n <= (double)a.max_norm ? 1. : (double)a.max_norm / n));
+    return (double)a.scale * (n <= (double)a.max_norm ? 1. : (double)a.max_norm / n);
 }
 
 __global__ __launch_bounds__(kThreads) void k_clip_sum(Tensors t, double *part)
@@ -196,8 +208,8 @@ __global__ __launch_bounds__(kThreads) void k_clip_scale(Tensors t, ClipArgs a, 
     if ((threadIdx.x & 63) == 0) red[wave] = s;
     __syncthreads();
     s = (red[0] + red[1]) + (red[2] + red[3]);
-    const float c = factor(a, s, blockIdx.x == 0 && threadIdx.x == 0 ? norm : nullptr);
-    scale_run(t, Run(t.first[t.n], blockIdx.x * kWaves + wave, gridDim.x * kWaves), c);
+    const double f = factor(a, s, blockIdx.x == 0 && threadIdx.x == 0 ? norm : nullptr);
+    scale_run(t, Run(t.first[t.n], blockIdx.x * kWaves + wave, gridDim.x * kWaves), f);
 }
 
 __global__ __launch_bounds__(kFew) void k_clip_few(Tensors t, ClipArgs a)

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2003_02989_amd import model
-from test_gpu_seq import TYPES
+from test_gpu_seq import TYPES, U, check, rounded
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,40 @@ def test_scan_gradient_of_no_channels(ty, ragged):
     g = model.selective_scan_grad(x, x, A, s, s, states, x, lengths=lengths, stream=side)
     side.synchronize()
     assert torch.all(g.dB == 0) and torch.all(g.dC == 0)
+
+
+@pytest.mark.parametrize("n", [4, 5003, 300000])
+@pytest.mark.parametrize("max_norm,scale", [(1.0, 1.0), (1e-10, 1e-30), (2.0 ** -120, 2.0 ** -20), (1e-3, 3.0)])
+def test_clipping_by_factors_below_the_normal_numbers(n, max_norm, scale):
+    """Elements near the largest value and a norm above it: the factor is no normal
+    fp32 number, the outputs are; they are as near as with any other factor."""
+    kinds = list(TYPES.values())
+    sign = torch.where(torch.arange(n) % 3 == 1, -1.0, 1.0)
+    values = [(3e38 * sign).to(torch.float32), (1e38 * sign).to(torch.bfloat16), torch.full((5,), 6e4).to(torch.float16)]
+    total = sum(float((v.double() ** 2).sum()) for v in values)
+    factor = float(torch.tensor(max_norm).double()) / total ** 0.5  # of the elements: the scale is in the norm too
+    for swap in range(3):
+        outs = [torch.full(v.shape, 9.0, dtype=kinds[(k + swap) % 3][0], device="cuda") for k, v in enumerate(values)]
+        norm, _ = model.clip_grad_norm([v.cuda() for v in values], max_norm, scale=scale, out=outs)
+        want_norm = torch.tensor(float(torch.tensor(scale).double()) * total ** 0.5, dtype=torch.float64).float()
+        assert torch.isclose(norm.cpu(), want_norm, rtol=2 * U, atol=0)
+        for k, (o, v) in enumerate(zip(outs, values)):
+            w = v.double() * factor
+            _, u, tiny = kinds[(k + swap) % 3]
+            # the factor, the product and the output's type, each rounded once
+            check("output", o, w.numpy(), rounded(w.numpy(), 2.1 * U * w.abs().numpy() + 2.0 ** -149, u, tiny))
+    grads = [v.cuda() for v in values]
+    model.clip_grad_norm(grads, max_norm, scale=scale)
+    for k, (o, v) in enumerate(zip(grads, values)):
+        w = v.double() * factor
+        _, u, tiny = kinds[k]
+        check("in place", o, w.numpy(), rounded(w.numpy(), 2.1 * U * w.abs().numpy() + 2.0 ** -149, u, tiny))
+
+
+def test_clipping_by_an_infinite_bound():
+    """max_norm = infinity cuts nothing, whatever the norm: the elements are scaled."""
+    g = torch.tensor([3e38, -3e38, float("inf"), 0.0], device="cuda")
+    norm, (o,) = model.clip_grad_norm([g], float("inf"), scale=0.5, out=[torch.empty_like(g)])
+    assert float(norm) == float("inf") and torch.equal(o, g * 0.5)
+    norm, (o,) = model.clip_grad_norm([g[:2]], float("inf"), out=[torch.empty_like(g[:2])])
+    assert float(norm) == float("inf") and torch.equal(o, g[:2])  # 4.2e38 is no fp32 number
