@@ -107,8 +107,9 @@ tq_status tq_causal_conv_grad(int32_t type, int64_t B, int64_t T, int64_t D, int
  *     outs[i] = grads[i] scale (norm <= max_norm ? 1 : max_norm / norm).
  * grads, outs, counts, types and out_types are HOST arrays of n entries, read
  * during the call: device pointers, numbers of elements and tq_dtypes.  outs[i] may
- * be grads[i] where both have one type.  Squares are summed in 64 bits; norm, float
- * on the device, is written always, infinite where the norm is past the range of fp32;
+ * be grads[i] where both have one type, but no other one of them (a tensor that is
+ * listed twice cannot be cut in place).  Squares are summed in 64 bits; norm, float on
+ * the device, is written always, infinite where the norm is past the range of fp32;
  * the factor is formed from the norm in 64 bits.  An infinite norm above max_norm gives
  * zeros for finite elements and NaN for infinite ones, a norm of NaN gives NaN.
  * max_norm >= 0 (infinite: nothing is cut, the factor is `scale` for an infinite norm

@@ -2,6 +2,8 @@
 // checked here, on the host, before anything is enqueued.
 #include <algorithm>
 #include <cmath>
+#include <utility>
+#include <vector>
 
 #include "abi_checks.h"
 #include "model.h"
@@ -63,6 +65,23 @@ void check_counts(const char *call, const char *name, int64_t n, const int64_t *
     for (int64_t i = 0; i < n; i++) {
         if (counts[i] < 0) fail(TQ_E_INVALID, text(call, name) + " must not be negative");
         if (counts[i] >= (int64_t)1 << 40) fail(TQ_E_UNSUPPORTED, text(call, name) + " must be below 2^40");
+    }
+}
+
+// Outputs may be their own inputs at most: one that is another entry's input is
+// written while that is read.
+void check_own(const char *call, int64_t n, const void *const *ins, void *const *outs, const int64_t *sizes)
+{
+    std::vector<std::pair<const void *, int64_t>> at;
+    at.reserve(n);
+    for (int64_t i = 0; i < n; i++)
+        if (sizes[i]) at.emplace_back(ins[i], i);
+    std::sort(at.begin(), at.end());
+    for (int64_t i = 0; i < n; i++) {
+        if (sizes[i] == 0) continue;
+        auto k = std::lower_bound(at.begin(), at.end(), std::pair<const void *, int64_t>(outs[i], 0));
+        for (; k != at.end() && k->first == outs[i]; ++k)
+            if (k->second != i) fail(TQ_E_INVALID, text(call, "an output is another entry's input"));
     }
 }
 
@@ -289,6 +308,7 @@ tq_status tq_clip_grad_norm(int64_t n, const void *const *grads, const int64_t *
             if (grads[i] == outs[i] && types[i] != out_types[i])
                 fail(TQ_E_INVALID, text(call, "a tensor in place keeps its type"));
         }
+        check_own(call, n, grads, outs, counts);
         check_array(call, "norm", norm, 4);
         check_space(call, workspace, workspace_bytes, clip_workspace(n, counts));
         hip_check(launch_clip({n, grads, outs, counts, types, out_types, max_norm, scale, norm, workspace},

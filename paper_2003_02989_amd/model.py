@@ -254,13 +254,22 @@ def _tensors(ts, name, like=None):
     return ptrs, codes
 
 
+def _apart(ptrs, sizes, name):
+    """Refuses outputs of which two are one."""
+    if len(set(ptrs)) < len(ptrs):
+        some = [p for p, n in zip(ptrs, sizes) if n]
+        if len(set(some)) < len(some):
+            raise ValueError(f"{name} must be different tensors")
+
+
 @_on_stream
 def clip_grad_norm(grads, max_norm, scale=1.0, out=None):
     """(norm, outputs): the norm of all tensors of the list `grads` together, a
     float32 scalar on the device, times `scale`, and the tensors times scale, cut
     to max_norm where the norm is above it (tq_clip_grad_norm).  The outputs are
-    the contiguous gradients themselves, or the tensors of the list `out`, of their
-    shapes and any of the types."""
+    the contiguous gradients themselves, each of them once, or the tensors of the
+    list `out`, of their shapes and any of the types; none may be another one's
+    gradient."""
     grads = list(grads)
     outs = grads if out is None else list(out)
     if len(outs) != len(grads):
@@ -271,7 +280,9 @@ def clip_grad_norm(grads, max_norm, scale=1.0, out=None):
     ptrs, codes = _tensors(grads, "grads")
     dev = grads[0].get_device()
     out_ptrs, out_codes = (ptrs, codes) if out is None else _tensors(outs, "out", grads)
-    counts = _list(ctypes.c_int64, [t.numel() for t in grads])
+    sizes = [t.numel() for t in grads]
+    _apart(out_ptrs, sizes, "grads" if out is None else "out")
+    counts = _list(ctypes.c_int64, sizes)
     norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
     need = ctypes.c_size_t()
     L = _lib or lib()

@@ -3,8 +3,12 @@ allows, without a GPU."""
 import pytest
 import torch
 
+import launches as la
 from paper_2003_02989_amd import model
 from test_model_binding_cpu import fake
+from test_model_launches_cpu import _lists, run  # noqa: F401 (the fixture serves here too)
+
+P, ALL = la.P, la.ALL
 
 
 @pytest.mark.parametrize("given", [False, True])
@@ -27,3 +31,30 @@ def test_no_channels_still_give_gradients_of_b_and_c(monkeypatch, given):
     for got in (g.dB, g.dC):
         assert got.shape == (2, 40, 5) and bool((got == 0).all())
     assert not given or (g.dB is out["dB"] and bool(torch.isnan(room[..., 10:]).all()))
+
+
+def clip(grads, outs, counts):
+    n = len(grads)
+    return ("tq_clip_grad_norm", n, grads, counts, [0] * n, 1.0, 1.0, outs, [0] * n, P, P, ALL, None)
+
+
+def test_clipping_refuses_outputs_that_are_other_gradients(tmp_path):
+    """One workgroup would read what another has written."""
+    a, b, c = P, 2 * P, 3 * P
+    good = [clip([a, b], [a, b], [9, 9]), clip([a, b, c], [a, 4 * P, c], [9, 70000, 9]), clip([a, a], [b, c], [9, 9]),
+            clip([a, a], [a, a], [9, 0]), clip([a, b], [b, a], [0, 9]), clip([a, None, b], [b, None, 4 * P], [9, 0, 0])]
+    run(good, tmp_path)
+    bad = [clip([a, b], [b, c], [9, 9]), clip([a, b], [b, a], [9, 9]), clip([a, a], [a, a], [9, 9]),
+           clip([a, b, a], [a, b, c], [9, 9, 9]), clip([a, b, c], [4 * P, 5 * P, a], [9, 70000, 9])]
+    assert all(g["rc"] == 1 and not g["kernels"] for g in la.recorded(bad, tmp_path)[0])
+
+
+def test_clipping_refuses_a_tensor_twice(monkeypatch):
+    monkeypatch.setattr(model, "_call", lambda f, *a: None)
+    monkeypatch.setattr(model, "_raw_stream", lambda dev: None)
+    x, y, o, none = fake(3, 4), fake(3, 4), fake(3, 4), fake(0)
+    model.clip_grad_norm([x, y, none, none], 1.0)
+    model.clip_grad_norm([x, x], 1.0, out=[o, y])
+    for grads, out in (([x, x], None), ([x, y], [o, o]), ([x, y, none], [o, o, none])):
+        with pytest.raises(ValueError):
+            model.clip_grad_norm(grads, 1.0, out=out)
