@@ -146,8 +146,8 @@ tq_status tq_beam_select(int32_t type, int64_t R, int64_t W, int64_t V, int64_t 
  * outs[i][r, k] = ins[i][r, parents[r, k]] for rows of row_bytes[i] bytes, ins[i]
  * [R, W] and outs[i] [R, K] of them; zeros where a parent is not in [0, W).  ins,
  * outs and row_bytes are HOST arrays of n entries, read during the call; parents
- * int32 [R, K] lies on the device.  TQ_E_UNSUPPORTED for n >= 2^20, R K >= 2^31,
- * rows of 2^40 bytes or R K ceil(row_bytes / 8192) >= 2^33. */
+ * int32 [R, K] lies on the device.  No outs[i] may be any of ins.  TQ_E_UNSUPPORTED
+ * for n >= 2^20, R K >= 2^31, rows of 2^40 bytes or R K ceil(row_bytes / 8192) >= 2^33. */
 tq_status tq_beam_reorder(int64_t n, const void *const *ins, void *const *outs, const int64_t *row_bytes, int64_t R,
                           int64_t W, int64_t K, const int32_t *parents, void *stream);
 

@@ -370,6 +370,7 @@ tq_status tq_beam_reorder(int64_t n, const void *const *ins, void *const *outs, 
             check_array(call, "outs", outs[i], 1);
             if (ins[i] == outs[i]) fail(TQ_E_INVALID, text(call, "rows are not reordered in place"));
         }
+        if (W) check_own(call, n, ins, outs, row_bytes);
         check_array(call, "parents", parents, 4);
         hip_check(launch_reorder({n, R, W, K, ins, outs, row_bytes, parents}, as_stream(stream)), "beam reorder launch");
     });

@@ -254,10 +254,10 @@ def _tensors(ts, name, like=None):
     return ptrs, codes
 
 
-def _apart(ptrs, sizes, name):
+def _apart(ptrs, ts, name):
     """Refuses outputs of which two are one."""
     if len(set(ptrs)) < len(ptrs):
-        some = [p for p, n in zip(ptrs, sizes) if n]
+        some = [p for p, t in zip(ptrs, ts) if t.numel()]
         if len(set(some)) < len(some):
             raise ValueError(f"{name} must be different tensors")
 
@@ -280,9 +280,8 @@ def clip_grad_norm(grads, max_norm, scale=1.0, out=None):
     ptrs, codes = _tensors(grads, "grads")
     dev = grads[0].get_device()
     out_ptrs, out_codes = (ptrs, codes) if out is None else _tensors(outs, "out", grads)
-    sizes = [t.numel() for t in grads]
-    _apart(out_ptrs, sizes, "grads" if out is None else "out")
-    counts = _list(ctypes.c_int64, sizes)
+    _apart(out_ptrs, outs, "grads" if out is None else "out")
+    counts = _list(ctypes.c_int64, [t.numel() for t in grads])
     norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
     need = ctypes.c_size_t()
     L = _lib or lib()
@@ -328,7 +327,7 @@ def beam_reorder(states, parents, out=None):
     """The states that go with beam_select's choice (tq_beam_reorder): for every
     tensor [R, W, ...] of the list `states`, of any type, the rows
     states[i][r, parents[r, k]] as a tensor [R, K, ...], new or that of the list
-    `out`; zeros where a parent is not one of the W."""
+    `out`, which holds none of the states; zeros where a parent is not one of the W."""
     states = list(states)
     _tensor(parents, "parents", torch.int32)
     pp = _dense(parents, "parents", torch.int32)
@@ -355,6 +354,7 @@ def beam_reorder(states, parents, out=None):
         ins.append(_dense(t, "states", None))
         outs.append(_dense(o, "out", t.dtype, (R, K) + row))
         rows.append(math.prod(row) * t.element_size())
+    _apart(outs, out, "out")
     _call((_lib or lib()).tq_beam_reorder, len(states), _list(ctypes.c_void_p, ins), _list(ctypes.c_void_p, outs),
           _list(ctypes.c_int64, rows), R, W, K, pp, _raw_stream(parents.get_device()))
     return out

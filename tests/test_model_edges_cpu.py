@@ -58,3 +58,27 @@ def test_clipping_refuses_a_tensor_twice(monkeypatch):
     for grads, out in (([x, x], None), ([x, y], [o, o]), ([x, y, none], [o, o, none])):
         with pytest.raises(ValueError):
             model.clip_grad_norm(grads, 1.0, out=out)
+
+
+def reorder(ins, outs, rows, R=2, W=3, K=3):
+    return ("tq_beam_reorder", len(ins), ins, outs, rows, R, W, K, P, None)
+
+
+def test_reordering_refuses_outputs_that_are_states(tmp_path):
+    a, b, c = P, 2 * P, 3 * P
+    run([reorder([a, a], [b, c], [8, 8]), reorder([a, b], [c, a], [8, 0]), reorder([a, b], [c, a], [0, 8]),
+         reorder([None, None], [a, b], [8, 8], W=0)], tmp_path)
+    bad = [reorder([a, b], [c, a], [8, 8]), reorder([a, b], [b, a], [8, 8]), reorder([a, b, 4 * P], [c, 5 * P, b], [1, 9000, 5])]
+    assert all(g["rc"] == 1 and not g["kernels"] for g in la.recorded(bad, tmp_path)[0])
+
+
+def test_reordering_refuses_an_output_twice(monkeypatch):
+    monkeypatch.setattr(model, "_call", lambda f, *a: None)
+    monkeypatch.setattr(model, "_raw_stream", lambda dev: None)
+    x, y, o, p = fake(2, 3, 4), fake(2, 3, 4), fake(2, 5, 4), fake(2, 5, dtype=torch.int32)
+    none, gone = fake(2, 3, 0), fake(2, 5, 0)
+    model.beam_reorder([x, x], p)
+    model.beam_reorder([x, none, none], p, out=[o, gone, gone])
+    model.beam_reorder([x[:0], y[:0]], p[:0], out=[o[:0], o[:0]])
+    with pytest.raises(ValueError):
+        model.beam_reorder([x, y], p, out=[o, o])
