@@ -264,11 +264,12 @@ class SelectiveRecordModel(RecordModel):
         scores = torch.zeros((R, 1), device=records.device)
         found = torch.empty((R, 1, steps), dtype=torch.int64, device=records.device)
         for t in range(steps):
-            logits = (y.reshape(-1, self.width).float() @ readout).view(R, -1, self.vocab)
+            W = scores.shape[1]
+            logits = (y.reshape(-1, self.width).float() @ readout).view(R, W, self.vocab)
             logits[..., self.start] = -math.inf  # not a bitstring
-            wide = min(beams, logits.shape[1] * self.start)
+            wide = min(beams, W * self.start)
             scores, parents, tokens = ops.beam_select(logits, scores, beams=wide)
-            *state, found = ops.beam_reorder([s.view((R, -1) + s.shape[1:]) for s in state] + [found], parents)
+            *state, found = ops.beam_reorder([s.view((R, W) + s.shape[1:]) for s in state] + [found], parents)
             found[..., t] = tokens
             state = [s.flatten(0, 1) for s in state]
             y = self.advance(tokens.view(-1, 1), state, p)

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2003_02989_amd import model
+from paper_2003_02989_amd.records import SelectiveRecordModel, ising_records
 from test_gpu_seq import TYPES, U, check, rounded
 
 pytestmark = pytest.mark.gpu
@@ -66,3 +67,34 @@ def test_clipping_by_an_infinite_bound():
     assert float(norm) == float("inf") and torch.equal(o, g * 0.5)
     norm, (o,) = model.clip_grad_norm([g[:2]], float("inf"), out=[torch.empty_like(g[:2])])
     assert float(norm) == float("inf") and torch.equal(o, g[:2])  # 4.2e38 is no fp32 number
+
+
+@pytest.mark.parametrize("taps", [1, 2])
+def test_search_with_few_taps(taps):
+    """A convolution of one tap carries no inputs along: its state has no elements.
+    With a beam for every continuation the scores are those of all of them."""
+    n, R, steps = 1, 2, 3
+    m = SelectiveRecordModel(n, 16, states=3, taps=taps, dtype=torch.float32, seed=5)
+    m.params["readout"] *= 40
+    records = ising_records(n, 6, R, seed=3)
+    scores, found = m.most_likely(records, steps, 2 ** steps)
+    assert found.shape == (R, 2 ** steps, steps)
+    p = m.working()
+    for r in range(R):
+        rows = torch.cat((records[r].expand(2 ** steps, -1), found[r]), 1)
+        y = m.advance(m.inputs(rows), m.beginning(2 ** steps), p)
+        z = (y.double() @ p["readout"].double().t())[..., :2]
+        want = torch.log_softmax(z, -1).gather(-1, rows[..., None])[:, 6:, 0].sum(1)
+        # sums of three scores in fp32, of logits that are fp32 products of 16
+        assert torch.allclose(scores[r].double(), want, atol=1e-4, rtol=1e-5)
+        assert len({tuple(f) for f in found[r].tolist()}) == 2 ** steps
+
+
+@pytest.mark.parametrize("taps", [1, 4])
+def test_search_of_no_records(taps):
+    m = SelectiveRecordModel(2, 16, states=3, taps=taps, dtype=torch.float32, seed=5)
+    none = torch.zeros((0, 6), dtype=torch.int64, device="cuda")
+    scores, found = m.most_likely(none, 2, 3)
+    assert scores.shape == (0, 3) and found.shape == (0, 3, 2)
+    scores, found = m.most_likely(none, 0, 3)
+    assert found.shape[0] == 0 and found.shape[2] == 0
