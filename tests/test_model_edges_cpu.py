@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import launches as la
-from paper_2003_02989_amd import model
+from paper_2003_02989_amd import model, seq
 from test_model_binding_cpu import fake
 from test_model_launches_cpu import _lists, run  # noqa: F401 (the fixture serves here too)
 
@@ -82,3 +82,12 @@ def test_reordering_refuses_an_output_twice(monkeypatch):
     model.beam_reorder([x[:0], y[:0]], p[:0], out=[o[:0], o[:0]])
     with pytest.raises(ValueError):
         model.beam_reorder([x, y], p, out=[o, o])
+
+
+def test_arrays_of_no_elements_may_have_any_strides():
+    """Views of every second column, as a table's without steps or records are."""
+    for shape in ((2, 0, 8), (0, 3, 8)):
+        t = fake(*shape)[..., ::2]
+        assert seq._steps(t, "x", None, t.shape)[1:] == t.stride()[:2]
+    with pytest.raises(ValueError):
+        seq._steps(fake(2, 3, 8)[..., ::2], "x", None, (2, 3, 4))
