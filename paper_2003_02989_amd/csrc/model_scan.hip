@@ -755,7 +755,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_select_join(SelectArgs a, G
 // ------------------------------------------------------------------ one step
 // Bound by memory: the state is read and written.  L lanes hold a channel, four
 // states each, so that a record's state is read in one piece; a thread takes the same
-// channel of N records.  1024 x 512 x 16 bf16: 20.8 us, 3.4 TB/s.
+// channel of N records.  1024 x 512 x 16 bf16: 17.6 us from a cache, 22.5 us, 3.2 TB/s,
+// from memory; 4096 records 75 us, 3.8 TB/s.
 template <class T, int L, int N> __global__ __launch_bounds__(256) void k_select_step(SelectArgs a, uint32_t blocks)
 {
     constexpr int PER = 256 / L;
@@ -890,23 +891,31 @@ template <class T, int W> hipError_t select_w(const SelectArgs &a, Geom g, hipSt
     return hipGetLastError();
 }
 
+// In fp32 a thread takes the same channel of four records where that leaves eight
+// workgroups to a compute unit: states that come from memory take 63.7 us in place of
+// 80.3 (4096 x 512 x 16), 20.6 in place of 22.6 at 8192 workgroups of one record each,
+// at 4096 the same; from a cache 17.7 and 17.9 us, 10.9 and 10.2.  Where a lane holds
+// a whole channel it gains nothing (4096 x 512 x 4: 23.3 and 22.6), and 16-bit inputs
+// lose (bf16 1024 x 512 x 16: 26.7 and 22.5; 4096 records 80.3 and 75.4).
 template <class T, int L> hipError_t step_l(const SelectArgs &a, hipStream_t s)
 {
-    // four records a thread where that leaves workgroups enough
     const int64_t slabs = (a.D + 256 / L - 1) / (256 / L);
-    if (a.B * slabs >= 8192) {
-        const int64_t blocks = (a.B + 3) / 4 * slabs;
-        k_select_step<T, L, 4><<<grid_of(blocks), 256, 0, s>>>(a, (uint32_t)blocks);
-    } else {
-        const int64_t blocks = a.B * slabs;
-        k_select_step<T, L, 1><<<grid_of(blocks), 256, 0, s>>>(a, (uint32_t)blocks);
-    }
+    if constexpr (sizeof(T) == 4 && L > 1)
+        if (a.B * slabs >= 8192) {
+            const int64_t blocks = (a.B + 3) / 4 * slabs;
+            k_select_step<T, L, 4><<<grid_of(blocks), 256, 0, s>>>(a, (uint32_t)blocks);
+            return hipGetLastError();
+        }
+    const int64_t blocks = a.B * slabs;
+    k_select_step<T, L, 1><<<grid_of(blocks), 256, 0, s>>>(a, (uint32_t)blocks);
     return hipGetLastError();
 }
 
 template <class T> hipError_t select_t(const SelectArgs &a, hipStream_t s)
 {
-    if (a.T == 1 && !a.states) switch (waves_of(a.S, 16)) {  // lanes of a channel
+    const int lanes = waves_of(a.S, 16);  // of a channel
+    // (more workgroups than are counted in 31 bits: the tiles have fewer, and give the same bits)
+    if (a.T == 1 && !a.states && a.B * ((a.D + 256 / lanes - 1) / (256 / lanes)) <= INT32_MAX) switch (lanes) {
         case 1: return step_l<T, 1>(a, s);
         case 2: return step_l<T, 2>(a, s);
         case 4: return step_l<T, 4>(a, s);

@@ -57,12 +57,21 @@ def test_scans_have_chunks_and_workgroups_with_several_items(tmp_path):
     assert several >= 6 and most > 2 * 32  # items in turn; starts of chunks read 32 together
 
 
-def test_single_steps_take_several_records_a_thread(tmp_path):
-    calls = [scan(0, B, 1, D, S) for B, D, S in sizes.STEPS]
+def test_single_steps_in_fp32_take_several_records_a_thread(tmp_path):
+    calls = [scan(ty, B, 1, D, S) for ty in range(3) for B, D, S in sizes.STEPS]
     got, _ = run(calls, tmp_path)
-    for (B, D, S), g in zip(sizes.STEPS, got):
+    for c, g in zip(calls, got):
+        ty, B, D, S = c[1], c[2], c[4], c[5]
         lanes = 1
         while 4 * lanes < S:
             lanes *= 2
         slabs = up(D, 256 // lanes)
-        assert B * slabs >= 8192 and B % 4 and grid(g, "k_select_step") == up(B, 4) * slabs
+        assert B * slabs >= 8192 and B % 4
+        assert grid(g, "k_select_step") == (up(B, 4) if ty == 0 and lanes > 1 else B) * slabs
+
+
+def test_single_steps_of_more_workgroups_than_31_bits_go_by_tiles(tmp_path):
+    most = (1 << 31) - 1
+    got, _ = run([scan(ty, most, 1, D, S) for ty in range(3) for D, S in ((64, 64), (1, 64), (64, 4), (17, 64))], tmp_path)
+    for g, step in zip(got, [False, True, True, False] * 3):
+        assert [("k_select_step" in k[0]) for k in g["kernels"]] == [step], g
