@@ -133,10 +133,17 @@ template <class T, class O> __device__ __forceinline__ void scaled(const T *p, O
 }
 
 // The same with a factor that fp32 holds as a subnormal number or not at all: elements
-// near the largest ones still give products that are numbers, formed in 64 bits.
-template <class T, class O> __device__ __forceinline__ void scaled_far(const T *p, O *o, int64_t n, double f)
+// near the largest ones still give products that are numbers, formed in 64 bits.  One
+// loop for all types: it is seldom taken, and a small kernel waits for its code.
+__device__ __forceinline__ void scaled_far(const Tensors &t, int i, int64_t at, double f)
 {
-    for (int i = threadIdx.x & 63; i < min(n, (int64_t)kChunk); i += 64) o[i] = (O)(float)((double)(float)p[i] * f);
+    const int64_t to = min(at + kChunk, t.count[i]);
+    for (int64_t k = at + (threadIdx.x & 63); k < to; k += 64) {
+        float v;
+        by_type(t.in_type[i], [&](auto x) { v = (float)((const decltype(x) *)t.in[i])[k]; });
+        const float o = (float)((double)v * f);
+        by_type(t.out_type[i], [&](auto y) { ((decltype(y) *)t.out[i])[k] = (decltype(y))o; });
+    }
 }
 
 // A wavefront's sum over its run.
@@ -167,12 +174,13 @@ __device__ __forceinline__ void scale_run(const Tensors &t, Run r, double f)
         while (k < t.first[i]) i--;
         if (c == 1.f && t.in[i] == t.out[i]) continue;
         const int64_t at = (int64_t)(k - t.first[i]) * kChunk;
+        if (far) {
+            scaled_far(t, i, at, f);
+            continue;
+        }
         by_type(t.in_type[i], [&](auto x) {
             by_type(t.out_type[i], [&](auto y) {
-                const auto *in = (const decltype(x) *)t.in[i] + at;
-                auto *out = (decltype(y) *)t.out[i] + at;
-                if (far) scaled_far(in, out, t.count[i] - at, f);
-                else scaled(in, out, t.count[i] - at, c);
+                scaled((const decltype(x) *)t.in[i] + at, (decltype(y) *)t.out[i] + at, t.count[i] - at, c);
             });
         });
     }
