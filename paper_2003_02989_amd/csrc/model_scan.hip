@@ -3,12 +3,12 @@
 //   d_t = softplus(dt_t + bias),  h_t = exp(d_t A) h_{t-1} + d_t x_t B_t,
 //   y_t = (C_t . h_t + skip x_t) silu(z_t),
 //
-// D channels of S states each.  What bounds it is the exponential of every
-// channel, state and step, which takes four of the eight issue slots that an
-// element of state costs.  So an element's exponential is formed once, and nothing
-// else is done per state that can be done per channel: a lane holds a channel with
-// four of its states in registers, and a workgroup of W wavefronts holds 64
-// channels with up to 4 W states.  Steps go in tiles of 16: the wavefronts share
+// D channels of S states each.  What bounds it are the vector units: an element of
+// state, that is a channel, state and step, costs some nine issue slots, two of them
+// its exponential, which runs at half rate.  So an element's exponential is formed
+// once, and nothing else is done per state that can be done per channel: a lane holds
+// a channel with four of its states in registers, and a workgroup of W wavefronts
+// holds 64 channels with up to 4 W states.  Steps go in tiles of 16: the wavefronts share
 // out the steps to form d, d x and the gates, leave them and the B and C of all
 // states in LDS, step through the tile with their own states, and leave their parts
 // of C . h in LDS, which the wavefront that a step belongs to adds up.
@@ -78,6 +78,9 @@ struct Place {
 
 // The decays' exponents to base 2 of a lane's states, and the others at zero: a
 // padded step has d = 0, and exp2(0) = 1 has to come out of A = -infinity too.
+// A log2 e is rounded, as the product with d is: a decay is off by up to |d A| 2^-24
+// more than exp(d A) would be.  Putting the lost part back, as exp_of does for what is
+// formed once per channel, would take one more instruction per element of state.
 __device__ __forceinline__ float exponent(float A)
 {
     const float v = A * kLog2e;
@@ -507,6 +510,9 @@ struct LaneSums {
 
 // N: the steps of a tile that are worked on: all of them, or the first four for records of
 // no more (1000 x 1 x 2000 fp16: 945 us with all, 692 with four).
+// All 256 registers are taken, and a lane spills 44 (W = 8) to 632 bytes (W = 1), for the
+// 16 states a channel of most models 132 (W = 4): 16 steps of decays and states are 132
+// registers, the nine values that each of a wavefront's 16 / W steps keeps as many as 144.
 template <class T, int W, int R, int N> __global__ __launch_bounds__(64 * W, 2) void k_select_grad(SelectArgs a, Geom g)
 {
     constexpr int PER = kTile / W;
@@ -822,10 +828,13 @@ int waves_of(int64_t S, int most)
 // the chip idle; a round is as many workgroups of the gradient as the chip holds.
 //  - Up to eight rounds, of chunks of at least 96 steps, and whole ones: forward and
 //    gradient of 4 x 4096 x 512 bf16 258 us in two rounds, 280 in 2.7.
-//  - Records of different lengths are evened out by more workgroups, of 64 steps, and
-//    so gain from chunks where there are more channels: 8 x 4099 x 1024 bf16 410 us
-//    (574 in two rounds); 20 x 1200 x 1200, three quarters of a round, 551 and 711
-//    without chunks (alike: 859 and 788), 64 x 512 x 512 fp32, a whole one, 397 and 303.
+//    The forward call alone is cut as its gradient is; it gains nothing from more
+//    chunks where there are more channels (400 x 1024 x 64 176 us whole, 204 cut).
+//  - Records of different lengths are evened out by more workgroups and gain from
+//    chunks where there are more channels: 20 x 1200 x 1200, three quarters of a round,
+//    581 us and 709 without chunks (alike: 859 and 788); 64 x 512 x 512 fp32, a whole
+//    one, 397 and 303.  Chunks of 64 steps or whole rounds of longer ones are the same
+//    there (8 x 4099 x 1024 504 and 502 us, 12 x 3000 x 700 439 and 430).
 //  - Where that is less than a round, one round of shorter chunks: 8 x 256 x 128 with 8
 //    states 59 us in place of 118, the scan of 1 x 1000 x 200 23 in place of 34; below
 //    96 steps there is nothing to gain (2 x 60 x 130: 59 and 51 us without).
